@@ -470,6 +470,80 @@ wsvd_status wsvd_linear_w4a8_split(wsvd_ctx *ctx, const int8_t *x, const void *x
                                    const void *w_scale_f16, int64_t M, int64_t K, int64_t N, int64_t n_first,
                                    void *out_first, void *out_rest, int32_t out_dtype, void *hip_stream);
 
+/*
+ * Dense layers: attention layers of the same decoder whose keys and values stay uncompressed (layers that a rank budget
+ * leaves alone, and the backbone the latent layers are compared with), over a paged cache of plain 16-bit rows, with the
+ * same page tables as the latent layers' pools.
+ *
+ *   dtype   BF16 or F16: queries, keys, values and outputs.  Scores, softmax statistics and sums are fp32.
+ *   Heads   n_q_heads / n_kv_heads in 1..16, d_head 64 or 128, at most 1024 query heads.
+ *   Rows    packed tensors are [tokens][ld] with a token's heads side by side from the pointer on; ld in elements, a multiple
+ *           of 8, at least heads * d_head (so the three parts of one projection's output can be passed as they lie).
+ *   Cache   wsvd_paged_cache with k_codes / v_codes the pools [n_pages][n_kv_heads][page_rows][d_head] of dtype, k_meta /
+ *           v_meta unused (may be NULL); page_rows a multiple of 16, at most 4096, max_pages * page_rows at most 2^27.
+ *           seq_lens[b] = rows of sequence b, the tokens of the call COUNTED; these entry points only read it (a caller that
+ *           keeps latent layers beside dense ones may pass the lengths that wsvd_latent_append_paged has advanced).
+ *           Table entries of pages that a sequence does not reach are not read for results.  An entry outside
+ *           [0, n_pages) of a page that it does reach records WSVD_E_SHAPE in the status word (wsvd_check): an append stores
+ *           nothing there, an attention reads page 0 in its place.
+ *   Packed sequences   cu_*[batch + 1] (DEVICE): tokens of sequence b are [cu[b], cu[b + 1]), any number of them, also none.
+ *           Packed tokens from cu[batch] on belong to nobody: nothing is written for them.
+ */
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, d_head;
+  int32_t dtype;   /* BF16 | F16 */
+  float sm_scale;  /* softmax scale; 0 means 1/sqrt(d_head) */
+} wsvd_dense_desc;
+
+/* Scratch of wsvd_dense_decode_attn_paged (HOST output); a context's workspace may serve latent and dense layers in turn. */
+wsvd_status wsvd_dense_workspace_bytes(const wsvd_dense_desc *desc, size_t *bytes);
+
+/*
+ * Rotary embedding and cache update of the new tokens: token i of the n_b that sequence b has in this call is row
+ * p = seq_lens[b] - n_b + i of its cache.
+ *   q_out = rot(q), cache row p of every kv head = (rot(k), v), k_out = rot(k) (if not NULL: what
+ *   wsvd_dense_prefill_attn takes).  q and q_out may both be NULL (keys only); q_out may be q and k_out may be k.
+ *   rot: dims (i, i + d_head/2) turned by position * inv_freq[i] ("rotate-half" pairing), inv_freq DEVICE double
+ *   [d_head/2] in radians per position (base^(-2i/d_head), or whatever scaling the model uses); the angle is formed in 64
+ *   bits, the rotation in fp32, rounded once.  NULL: no rotation.  position = positions[token] (DEVICE [n_tokens]), or p
+ *   where positions is NULL.
+ *   cu_tokens [batch + 1], or NULL: one token per sequence (n_tokens == batch).
+ * A row outside [0, max_pages * page_rows) stores nothing and records WSVD_E_SHAPE (below) or WSVD_E_CAPACITY (above).
+ * n_tokens at most 2^24.
+ */
+wsvd_status wsvd_dense_append_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld, const void *k,
+                                    int64_t k_ld, const void *v, int64_t v_ld, int64_t n_tokens, const int32_t *cu_tokens,
+                                    const int32_t *positions, const double *inv_freq, void *q_out, int64_t q_out_ld,
+                                    void *k_out, int64_t k_out_ld, wsvd_paged_cache *cache, void *hip_stream);
+
+/*
+ * Attention of one new token per sequence over its pages:
+ *   out[b,h,:] = softmax_t( sm_scale * q[b,h,:] . K[b,kv(h),t,:] ) . V[b,kv(h),:,:]   over t < seq_lens[b]; no row gives zeros
+ * (as does a row whose scores are all -inf).  q [batch][q_ld], out [batch][n_q_heads][d_head] of dtype.  The rows of all
+ * sequences are divided over the chip by the lengths found on the device and joined in a fixed order, so the result does
+ * not depend on timing; max_seq_len is a HOST upper bound, at most max_pages * page_rows (a longer sequence records
+ * WSVD_E_SHAPE and is attended over its first max_seq_len rows).
+ */
+wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld,
+                                         const wsvd_paged_cache *cache, int32_t max_seq_len, void *out, void *hip_stream);
+
+/*
+ * Attention of whole prompts packed one behind another: queries of sequence b are tokens [cu_q[b], cu_q[b+1]) of q, its keys
+ * and values tokens [cu_kv[b], cu_kv[b+1]) of k and v (cu_kv NULL: cu_q, and n_kv == n_q).  causal 1: of n queries over t
+ * keys, query i sees keys up to i + t - n (the last query sees them all); 0: every query sees all keys.  A query that sees
+ * no key (or only scores of -inf) gives zeros; what a masked key or value holds, infinities and NaN included, has no effect.
+ * out [n_q][out_ld].  n_q at most 2^24, n_kv at most 2^27.
+ */
+wsvd_status wsvd_dense_prefill_attn(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld, const void *k,
+                                    int64_t k_ld, const void *v, int64_t v_ld, int64_t n_q, int64_t n_kv, const int32_t *cu_q,
+                                    const int32_t *cu_kv, int32_t causal, void *out, int64_t out_ld, void *hip_stream);
+
+/* The same, causal, with keys and values from the pages: the n_b packed queries of sequence b are its last n_b rows (the next
+ * piece of a prompt, or a few draft tokens, behind what is cached), query i seeing rows up to seq_lens[b] - n_b + i. */
+wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld, int64_t n_q,
+                                          const int32_t *cu_q, const wsvd_paged_cache *cache, void *out, int64_t out_ld,
+                                          void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

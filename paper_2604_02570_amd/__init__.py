@@ -29,7 +29,9 @@ EXPORTS = ["wsvd_create", "wsvd_destroy", "wsvd_cache_bytes", "wsvd_workspace_by
            "wsvd_factor_a_bytes", "wsvd_pack_factor_a", "wsvd_quantize_rows", "wsvd_cache_import", "wsvd_cache_export", "wsvd_quantize_act_i8", "wsvd_linear_w4a8",
            "wsvd_linear_w4a8_split", "wsvd_probe_stream_read", "wsvd_test_step_attention", "wsvd_test_shared_plan", "wsvd_fold_qk", "wsvd_fold_vo", "wsvd_decode_attn_latent",
            "wsvd_rmsnorm_quant_i8", "wsvd_swiglu_quant_i8", "wsvd_prefill_append",
-           "wsvd_prefill_attn", "wsvd_shared_workspace_bytes", "wsvd_decode_attn_shared", "wsvd_timeline_set_buffer"]
+           "wsvd_prefill_attn", "wsvd_shared_workspace_bytes", "wsvd_decode_attn_shared", "wsvd_timeline_set_buffer",
+           "wsvd_dense_workspace_bytes", "wsvd_dense_append_paged", "wsvd_dense_decode_attn_paged", "wsvd_dense_prefill_attn",
+           "wsvd_dense_prefill_attn_paged"]
 
 
 class WsvdError(RuntimeError):
@@ -54,6 +56,11 @@ class PagedCache(ctypes.Structure):
     _fields_ = [("k_codes", c_void_p), ("v_codes", c_void_p), ("k_meta", c_void_p), ("v_meta", c_void_p),
                 ("seq_lens", c_void_p), ("block_table", c_void_p), ("page_rows", c_int32), ("max_pages", c_int32),
                 ("n_pages", c_int32)]
+
+
+class DenseDesc(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("d_head", c_int32), ("dtype", c_int32),
+                ("sm_scale", c_float)]
 
 
 _lib = None
@@ -141,6 +148,15 @@ def lib():
         L.wsvd_rmsnorm_quant_i8.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_float, c_int64, c_int64, c_void_p,
                                             c_void_p, c_void_p, c_void_p]
         L.wsvd_swiglu_quant_i8.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p]
+        L.wsvd_dense_workspace_bytes.argtypes = [POINTER(DenseDesc), POINTER(c_size_t)]
+        L.wsvd_dense_append_paged.argtypes = [c_void_p, POINTER(DenseDesc), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int64,
+                                              c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, POINTER(PagedCache), c_void_p]
+        L.wsvd_dense_decode_attn_paged.argtypes = [c_void_p, POINTER(DenseDesc), c_void_p, c_int64, POINTER(PagedCache), c_int32, c_void_p,
+                                                   c_void_p]
+        L.wsvd_dense_prefill_attn.argtypes = [c_void_p, POINTER(DenseDesc), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int64,
+                                              c_int64, c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p]
+        L.wsvd_dense_prefill_attn_paged.argtypes = [c_void_p, POINTER(DenseDesc), c_void_p, c_int64, c_int64, c_void_p, POINTER(PagedCache),
+                                                    c_void_p, c_int64, c_void_p]
         for name in EXPORTS:
             if name not in ("wsvd_status_str",):
                 getattr(L, name).restype = c_int
@@ -402,3 +418,36 @@ def wsvd_timeline_set_buffer(ctx, buf):
     """Profiling build only (include/wsvd_test.h); buf = int64 device tensor or None."""
     n = 0 if buf is None else buf.numel() * buf.element_size()
     _ck(lib().wsvd_timeline_set_buffer(ctx, _ptr(buf), n), "wsvd_timeline_set_buffer")
+
+
+def dense_desc(batch, n_q_heads, n_kv_heads, d_head, dtype, sm_scale=0.0) -> DenseDesc:
+    return DenseDesc(batch, n_q_heads, n_kv_heads, d_head, DTYPES[dtype] if isinstance(dtype, str) else int(dtype), float(sm_scale))
+
+
+def wsvd_dense_workspace_bytes(desc):
+    a = c_size_t()
+    _ck(lib().wsvd_dense_workspace_bytes(byref(desc), byref(a)), "wsvd_dense_workspace_bytes")
+    return a.value
+
+
+def wsvd_dense_append_paged(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_tokens, cu_tokens, positions, inv_freq, q_out, q_out_ld, k_out, k_out_ld,
+                            cache, stream=None):
+    _ck(lib().wsvd_dense_append_paged(ctx, byref(desc), _ptr(q), int(q_ld), _ptr(k), int(k_ld), _ptr(v), int(v_ld), int(n_tokens),
+                                      _ptr(cu_tokens), _ptr(positions), _ptr(inv_freq), _ptr(q_out), int(q_out_ld), _ptr(k_out),
+                                      int(k_out_ld), byref(cache), _stream(stream)), "wsvd_dense_append_paged")
+
+
+def wsvd_dense_decode_attn_paged(ctx, desc, q, q_ld, cache, max_seq_len, out, stream=None):
+    _ck(lib().wsvd_dense_decode_attn_paged(ctx, byref(desc), _ptr(q), int(q_ld), byref(cache), int(max_seq_len), _ptr(out),
+                                           _stream(stream)), "wsvd_dense_decode_attn_paged")
+
+
+def wsvd_dense_prefill_attn(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_q, n_kv, cu_q, cu_kv, causal, out, out_ld, stream=None):
+    _ck(lib().wsvd_dense_prefill_attn(ctx, byref(desc), _ptr(q), int(q_ld), _ptr(k), int(k_ld), _ptr(v), int(v_ld), int(n_q), int(n_kv),
+                                      _ptr(cu_q), _ptr(cu_kv), int(causal), _ptr(out), int(out_ld), _stream(stream)),
+        "wsvd_dense_prefill_attn")
+
+
+def wsvd_dense_prefill_attn_paged(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, stream=None):
+    _ck(lib().wsvd_dense_prefill_attn_paged(ctx, byref(desc), _ptr(q), int(q_ld), int(n_q), _ptr(cu_q), byref(cache), _ptr(out),
+                                            int(out_ld), _stream(stream)), "wsvd_dense_prefill_attn_paged")
