@@ -16,8 +16,14 @@ namespace {
 
 constexpr int kKeys = 64;                            // keys of a staged block
 
+// lds_copy16 without the compiler's knowledge: it would let every later read of LDS wait for the copy (the next block's, while
+// this one is worked on).  The copies are waited for by lds_copy_wait_barrier alone.
+WSVD_DEV void copy16(uint32_t lds, const uint8_t* base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+
 template <class T, int D, bool PAGED, int NW>
-__global__ __launch_bounds__(64 * NW) void k_dense_prompt(DensePromptParams p) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_prompt(DensePromptParams p) {
   constexpr int ROWS = 32 * NW;                      // query rows of a workgroup
   constexpr int PIECES = D / 8, RPI = 64 / PIECES;   // 16-byte pieces of a row; rows that one copy of a wave brings
   constexpr int COPIES = kKeys / NW / RPI;
@@ -116,8 +122,8 @@ __global__ __launch_bounds__(64 * NW) void k_dense_prompt(DensePromptParams p) {
         ks = (const uint8_t*)(p.k + first * p.k_ld + kv * D); vs = (const uint8_t*)(p.v + first * p.v_ld + kv * D);
         ko = (uint32_t)rr * (uint32_t)p.k_ld * 2u; vo = (uint32_t)rr * (uint32_t)p.v_ld * 2u;
       }
-      lds_copy16(lds0 + buf * STAGE + r0 * ROW_BYTES, ks, ko + kp * 16);
-      lds_copy16(lds0 + buf * STAGE + PLANE + r0 * ROW_BYTES, vs, vo + vp * 16);
+      copy16(lds0 + buf * STAGE + r0 * ROW_BYTES, ks, ko + kp * 16);
+      copy16(lds0 + buf * STAGE + PLANE + r0 * ROW_BYTES, vs, vo + vp * 16);
     }
   };
 
@@ -162,6 +168,7 @@ __global__ __launch_bounds__(64 * NW) void k_dense_prompt(DensePromptParams p) {
 #pragma unroll
       for (int x = 0; x < NS; x++) s[h] = T::mfma32(read_k(buf, h, x), q[x], s[h]);
     }
+    __builtin_amdgcn_sched_barrier(0);
     const int rel = limit - kb * kKeys - 4 * half;
     if (MASKED) {
 #pragma unroll
@@ -195,6 +202,7 @@ __global__ __launch_bounds__(64 * NW) void k_dense_prompt(DensePromptParams p) {
         l += a; l += c;
         w[h][i] = dense_pack<T>(a, c);
       }
+    __builtin_amdgcn_sched_barrier(0);
     uint32_t odd = 0;
 #pragma unroll
     for (int x = 0; x < 4; x++) {
@@ -236,13 +244,22 @@ __global__ __launch_bounds__(64 * NW) void k_dense_prompt(DensePromptParams p) {
     }
   };
 
-  if (n_blocks > 0) stage(0, 0);
-  for (int kb = 0; kb < n_blocks; kb++) {
+  // Blocks that all of the wave's queries see whole, then the others: two loops, since one with both forms copies the
+  // accumulators in every block.
+  const int n_whole = max(0, min(wseen, wall)) / kKeys;
+  auto next = [&](int kb) {
     lds_copy_wait_barrier<0>();                      // this block is there, and nobody reads the other stage any more
     if (kb + 1 < n_blocks) stage(kb + 1, (kb + 1) & 1);
-    if (kb * kKeys >= wseen) continue;
-    if ((kb + 1) * kKeys <= wall && (kb + 1) * kKeys <= nk) attend(kb, kb & 1, std::false_type{});
-    else attend(kb, kb & 1, std::true_type{});
+  };
+  if (n_blocks > 0) stage(0, 0);
+  int kb = 0;
+  for (; kb < n_whole; kb++) {
+    next(kb);
+    attend(kb, kb & 1, std::false_type{});
+  }
+  for (; kb < n_blocks; kb++) {
+    next(kb);
+    if (kb * kKeys < wseen) attend(kb, kb & 1, std::true_type{});
   }
   if (bad && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   l = halves_sum(l);
