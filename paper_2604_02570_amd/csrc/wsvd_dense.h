@@ -34,19 +34,17 @@ template <class T>
 WSVD_DEV float dense_high(uint32_t x) { return (float)__builtin_bit_cast(typename T::Elem, (uint16_t)(x >> 16)); }
 
 // ---------------------------------------------------------------- wave-wide integer helpers
-WSVD_DEV int wave_sum_int(int x) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-  return __builtin_amdgcn_readfirstlane(x);
-}
-WSVD_DEV int wave_prefix_int(int x, int lane) {      // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d, 64);
-    x += lane >= d ? y : 0;
-  }
+// Inclusive prefix sum over the wave: within rows of 16 lanes by shifts, then the last lanes' sums onto the rows behind.
+WSVD_DEV int wave_prefix_int(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);       // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // row_bcast 15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);      // row_bcast 31 into rows 2 and 3
   return x;
 }
+WSVD_DEV int wave_sum_int(int x) { return __builtin_amdgcn_readlane(wave_prefix_int(x), 63); }
 
 // The sequence that packed token t belongs to: the number of sequences that end at or before it (B where none is left).
 WSVD_DEV int dense_sequence_of(const int* cu, int B, int t, int lane) {
@@ -66,13 +64,24 @@ struct DensePages {
   const int* seq_lens;          // [B]
   const int* block_table;       // [B][max_pages]
   int page_rows, max_pages, n_pages;
+  uint32_t page_magic;          // dense_page_magic
 };
+// The page of a sequence's granule of 16 rows (granule / (page_rows / 16)) by a product: exact for granules below 2^23 and up to
+// 2^8 granules in a page, since granule * (magic * n - 2^32) < 2^31.  A page of one granule has a magic of 2^32, kept as 0.
+inline __host__ __device__ uint32_t dense_page_magic(int page_rows) {
+  const uint64_t n = (uint64_t)page_rows / 16;
+  return (uint32_t)((((uint64_t)1 << 32) + n - 1) / n);
+}
+inline __host__ __device__ int dense_page_index(int granule, uint32_t magic) {
+  return magic == 0 ? granule : (int)(((uint64_t)(uint32_t)granule * magic) >> 32);
+}
 
 // ---------------------------------------------------------------- how the decode attention divides its work
 // The rows of all sequences are dealt out in chunks of the same number of units (kDenseUnit rows), as many that about `target`
 // chunks come of it, none of them across two sequences: at most target + B.
 constexpr int kDenseUnit = 128;
-constexpr int kDenseWorkgroups = 512;                // two of 4 waves on each of 256 CUs
+constexpr int kDenseWaves = 8;
+constexpr int kDenseWorkgroups = 256;                // one of 8 waves on each of 256 CUs
 inline __host__ __device__ int dense_target(int Hkv) { return kDenseWorkgroups / Hkv > 1 ? kDenseWorkgroups / Hkv : 1; }
 
 struct DenseAppendParams {

@@ -96,18 +96,15 @@ __global__ __launch_bounds__(256) void k_dense_append(DenseAppendParams p) {
 // A chunk's place: sequence, chunk of it, chunks it has; false for a workgroup that has none.
 struct DensePlace { int b, chunk, n_chunks, len, rows; };
 
+WSVD_DEV int dense_length(const DenseDecodeParams& p, int b) { return b < p.B ? min(max(p.pages.seq_lens[b], 0), p.max_len) : 0; }
 // units a chunk takes, from the lengths of all sequences
 WSVD_DEV int dense_chunk_units(const DenseDecodeParams& p, int lane) {
   int total = 0;
-  for (int base = 0; base < p.B; base += 64) {
-    const int i = base + lane;
-    const int len = i < p.B ? min(max(p.pages.seq_lens[i], 0), p.max_len) : 0;
-    total += wave_sum_int((len + kDenseUnit - 1) / kDenseUnit);
-  }
+  for (int base = 0; base < p.B; base += 64) total += wave_sum_int((dense_length(p, base + lane) + kDenseUnit - 1) / kDenseUnit);
   return max(p.min_units, (total + p.target - 1) / p.target);
 }
 WSVD_DEV int dense_chunks(const DenseDecodeParams& p, int b, int units, int& len) {
-  len = b < p.B ? min(max(p.pages.seq_lens[b], 0), p.max_len) : 0;
+  len = dense_length(p, b);
   const int u = (len + kDenseUnit - 1) / kDenseUnit;
   return b < p.B ? max(1, (u + units - 1) / units) : 0;
 }
@@ -117,7 +114,7 @@ WSVD_DEV bool dense_place(const DenseDecodeParams& p, int idx, int lane, DensePl
   for (int base = 0; base < p.B; base += 64) {
     int len;
     const int n = dense_chunks(p, base + lane, units, len);
-    const int end = first + wave_prefix_int(n, lane);
+    const int end = first + wave_prefix_int(n);
     const unsigned long long m = __ballot(end > idx);
     if (m) {
       const int l = __builtin_ctzll(m);
@@ -144,14 +141,15 @@ WSVD_DEV float quarters_sum(float x) {
 
 template <int D>
 struct DenseTile {
-  v4i k[2][D / 32];                                  // 16 rows each, operand of the score product
+  v4i k[2][D / 32];                                  // 16 rows each, as they lie in memory
   uint32_t v[8][D / 32];                             // row 4 quarter + i of either half, D / 16 dims
 };
 
 template <class T, int D>
-__global__ __launch_bounds__(256) void k_dense_decode(DenseDecodeParams p) {
-  constexpr int NK = D / 32, NJ = D / 16;
-  __shared__ float o_sh[4][16][D], m_sh[4][16], l_sh[4][16];
+__global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode(DenseDecodeParams p) {
+  constexpr int NK = D / 32, NJ = D / 16, NW = kDenseWaves;
+  extern __shared__ __attribute__((aligned(256))) float o_sh[];      // a granule pair's keys for each wave; at the end [NW][G][D]
+  __shared__ float m_sh[NW][16], l_sh[NW][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, qd = lane >> 4;
   const int kv = blockIdx.x % p.Hkv, idx = blockIdx.x / p.Hkv;
@@ -173,26 +171,44 @@ __global__ __launch_bounds__(256) void k_dense_decode(DenseDecodeParams p) {
       for (int i = 0; i < 4; i++) q[j][i] = c < G ? x[i] : 0;
     }
   }
+  // Where the wave's next 32 tiles lie, a lane for each half of one: its pages are looked up side by side, and what a tile's
+  // requests wait for is two lane reads.
   const int* table = p.pages.block_table + (size_t)at.b * p.pages.max_pages;
-  const int per_page = p.pages.page_rows >> 4, last_granule = (at.len - 1) >> 4;
+  const int last_granule = (at.len - 1) >> 4;
   bool bad = false;
-  auto load = [&](DenseTile<D>& tile, int t) {
+  uint32_t at_low = 0, at_high = 0;
+  auto look_up = [&](int t) {
+    const int granule = min((first >> 4) + 2 * (t + NW * (lane >> 1)) + (lane & 1), last_granule);
+    const int pg = dense_page_index(granule, p.pages.page_magic);
+    int page = table[pg];
+    if (page < 0 || page >= p.pages.n_pages) { bad = true; page = 0; }
+    const uint64_t at = (((uint64_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * D;
+    at_low = (uint32_t)at; at_high = (uint32_t)(at >> 32);
+  };
+  auto load = [&](DenseTile<D>& tile, int i) {       // i: the tile's number among those looked up
 #pragma unroll
     for (int g = 0; g < 2; g++) {
-      const int granule = min((first >> 4) + 2 * t + g, last_granule);
-      const int pg = granule / per_page;
-      int page = __builtin_amdgcn_readfirstlane(table[pg]);
-      bad |= page < 0 || page >= p.pages.n_pages;
-      page = page < 0 || page >= p.pages.n_pages ? 0 : page;
-      const size_t base = (((size_t)page * p.Hkv + kv) * p.pages.page_rows + (granule - pg * per_page) * 16) * D;
+      const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, 2 * i + g) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, 2 * i + g) << 32;
       const uint16_t *kp = p.pages.k + base, *vp = p.pages.v + base;
 #pragma unroll
-      for (int j = 0; j < NK; j++) tile.k[g][j] = *(const v4i*)(kp + c * D + j * 32 + qd * 8);
+      for (int j = 0; j < NK; j++) tile.k[g][j] = *(const v4i*)(kp + j * 512 + lane * 8);
 #pragma unroll
-      for (int i = 0; i < 4; i++)
-        __builtin_memcpy(tile.v[4 * g + i], __builtin_assume_aligned(vp + (4 * qd + i) * D + c * NJ, D / 8), NJ * 2);
+      for (int i2 = 0; i2 < 4; i2++)
+        __builtin_memcpy(tile.v[4 * g + i2], __builtin_assume_aligned(vp + (4 * qd + i2) * D + c * NJ, D / 8), NJ * 2);
     }
   };
+  // A wave's keys go through LDS of its own: requested in whole lines (asked for as the product's operand, 16 rows of 64 bytes
+  // per request, they cost the CU's address pipeline four times as much: 640 rows 11.8 -> 14.3 us) and read back by key, the
+  // 16-byte pieces of a row permuted so that neither side meets a bank twice.
+  const uint32_t k_lds = lds_address(o_sh) + wave * (64 * D);
+  uint32_t k_put[NK], k_get[NK];
+#pragma unroll
+  for (int j = 0; j < NK; j++) {
+    const int row = (j * 64 + lane) / (D / 8), piece = lane % (D / 8);
+    k_put[j] = k_lds + row * 2 * D + (piece ^ (D == 128 ? row : row >> 1)) * 16;
+    k_get[j] = k_lds + c * 2 * D + ((4 * j + qd) ^ (D == 128 ? c : c >> 1)) * 16;
+  }
+  typedef __attribute__((address_space(3))) v4i lds_v4i;
   float m = -INFINITY, l = 0.f;
   v4f o[NJ];
 #pragma unroll
@@ -202,10 +218,14 @@ __global__ __launch_bounds__(256) void k_dense_decode(DenseDecodeParams p) {
     const int r0 = first + t * 32;
     float s[8];
 #pragma unroll
+    for (int g = 0; g < 2; g++)
+#pragma unroll
+      for (int j = 0; j < NK; j++) *(lds_v4i*)(uintptr_t)(k_put[j] + g * 32 * D) = tile.k[g][j];
+#pragma unroll
     for (int g = 0; g < 2; g++) {
       v4f x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < NK; j++) x = T::mfma16(tile.k[g][j], q[j], x);
+      for (int j = 0; j < NK; j++) x = T::mfma16(*(const lds_v4i*)(uintptr_t)(k_get[j] + g * 32 * D), q[j], x);
 #pragma unroll
       for (int i = 0; i < 4; i++) s[4 * g + i] = x[i] * p.c_scale;
     }
@@ -252,39 +272,42 @@ __global__ __launch_bounds__(256) void k_dense_decode(DenseDecodeParams p) {
       o[j] = T::mfma16(a, lo, o[j]);
     }
   };
-  if (wave < n_tiles) {
+  for (int t = wave; t < n_tiles; t += 32 * NW) {    // 32 tiles of the wave
+    look_up(t);
+    const int n = min(32, (n_tiles - t + NW - 1) / NW);
     DenseTile<D> t0, t1;
-    load(t0, wave);
-    int t = wave;
-    for (; t + 4 < n_tiles; t += 8) {
-      load(t1, t + 4);
-      attend(t0, t);
-      load(t0, t + 8);                               // (past the end: the last rows once more)
-      attend(t1, t + 4);
+    load(t0, 0);
+    int i = 0;
+    for (; i + 1 < n; i += 2) {
+      load(t1, i + 1);
+      attend(t0, t + NW * i);
+      load(t0, min(i + 2, 31));                      // (past the end: the last rows once more)
+      attend(t1, t + NW * (i + 1));
     }
-    if (t < n_tiles) attend(t0, t);
+    if (i < n) attend(t0, t + NW * i);
   }
-  if (bad && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+  if (__ballot(bad) && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   l = quarters_sum(l);
+  __syncthreads();                                   // (the keys' LDS becomes the accumulators')
   if (c < G) {
     if (qd == 0) { m_sh[wave][c] = m; l_sh[wave][c] = l; }
 #pragma unroll
     for (int j = 0; j < NJ; j++)
 #pragma unroll
-      for (int i = 0; i < 4; i++) o_sh[wave][c][NJ * (4 * qd + i) + j] = o[j][i];
+      for (int i = 0; i < 4; i++) o_sh[(wave * G + c) * D + NJ * (4 * qd + i) + j] = o[j][i];
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < G * D; e += 256) {
+  for (int e = threadIdx.x; e < G * D; e += 64 * NW) {
     const int g = e / D, x = e % D;
     float M = m_sh[0][g];
 #pragma unroll
-    for (int w = 1; w < 4; w++) M = fmaxf(M, m_sh[w][g]);
+    for (int w = 1; w < NW; w++) M = fmaxf(M, m_sh[w][g]);
     float L = 0.f, U = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; w++) {
+    for (int w = 0; w < NW; w++) {
       const float k = m_sh[w][g] == -INFINITY ? (l_sh[w][g] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m_sh[w][g] - M);
       L += l_sh[w][g] * k;
-      U += o_sh[w][g][x] * k;
+      U += o_sh[(w * G + g) * D + x] * k;
     }
     if (at.n_chunks == 1) {
       const float r = L == 0.f ? 0.f : U / L;
@@ -297,32 +320,68 @@ __global__ __launch_bounds__(256) void k_dense_decode(DenseDecodeParams p) {
   }
 }
 
-// The chunks of a sequence folded in their order, one workgroup per (sequence, head).
+// The chunks of a sequence joined, one workgroup per (sequence, head).  The chunks' maxima and sums first, one per thread, then
+// the rows of 4 or 2 chunks side by side, each group of D threads its own in their order, eight at a time: a chunk after the
+// other, each waiting for its row, took 68 us for 127 chunks.
 template <class T, int D>
-__global__ __launch_bounds__(D) void k_dense_join(DenseDecodeParams p) {
-  const int lane = threadIdx.x & 63, Hq = p.Hkv * p.G, b = blockIdx.x / Hq, h = blockIdx.x % Hq;
+__global__ __launch_bounds__(256) void k_dense_join(DenseDecodeParams p) {
+  constexpr int GROUPS = 256 / D;
+  __shared__ float w_sh[kDenseWorkgroups], red_sh[4], u_sh[GROUPS][D];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, Hq = p.Hkv * p.G, b = blockIdx.x / Hq, h = blockIdx.x % Hq;
   const int units = dense_chunk_units(p, lane);
   int first = 0, n = 0;
   for (int base = 0; base <= b; base += 64) {
     int len;
     const int k = dense_chunks(p, base + lane, units, len);
-    const int end = wave_prefix_int(k, lane);
+    const int end = wave_prefix_int(k);
     if (b - base < 64) { n = __builtin_amdgcn_readlane(k, b - base); first += __builtin_amdgcn_readlane(end, b - base) - n; }
     else first += __builtin_amdgcn_readlane(end, 63);
   }
   if (n <= 1) return;
-  const size_t step = (size_t)p.Hkv * p.G * (D + 2);
+  const size_t step = (size_t)Hq * (D + 2);
   const float* part = p.parts + (size_t)first * step + (size_t)h * (D + 2);
-  float M = -INFINITY, L = 0.f, U = 0.f;
-  for (int i = 0; i < n; i++, part += step) {
-    const float m = part[0], l = part[1], u = part[2 + threadIdx.x];
-    const float mn = fmaxf(M, m);
-    const float keep = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mn), e = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-    L = L * keep + l * e;                            // (nothing seen yet: L and U are 0, or NaN)
-    U = U * keep + u * e;
-    M = mn;
+  float m[2], l[2], M = -INFINITY;                   // (at most kDenseWorkgroups + 1 chunks)
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const int at = tid + 256 * i;
+    m[i] = at < n ? part[at * step] : -INFINITY;
+    l[i] = at < n ? part[at * step + 1] : 0.f;
+    M = fmaxf(M, m[i]);
   }
-  p.out[((int64_t)b * Hq + h) * D + threadIdx.x] = (uint16_t)dense_pack<T>(L == 0.f ? 0.f : U / L, 0.f);
+  M = wave_max(M);
+  if (lane == 0) red_sh[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(red_sh[0], red_sh[1]), fmaxf(red_sh[2], red_sh[3]));
+  float L = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const float e = m[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - M);    // (nothing seen: l and the row are 0, or NaN)
+    if (tid + 256 * i < n) w_sh[tid + 256 * i] = e;
+    L += l[i] * e;
+  }
+  L = wave_sum(L);
+  __syncthreads();
+  if (lane == 0) red_sh[wave] = L;
+  __syncthreads();
+  L = (red_sh[0] + red_sh[1]) + (red_sh[2] + red_sh[3]);
+  const int g = tid / D, x = tid % D;
+  float U = 0.f;
+  for (int i0 = g; i0 < n; i0 += 8 * GROUPS) {
+    float u[8];
+#pragma unroll
+    for (int k = 0; k < 8; k++) u[k] = part[(size_t)min(i0 + k * GROUPS, n - 1) * step + 2 + x];
+#pragma unroll
+    for (int k = 0; k < 8; k++)
+      if (i0 + k * GROUPS < n) U += u[k] * w_sh[i0 + k * GROUPS];
+  }
+  u_sh[g][x] = U;
+  __syncthreads();
+  if (tid < D) {
+    U = u_sh[0][tid];
+#pragma unroll
+    for (int k = 1; k < GROUPS; k++) U += u_sh[k][tid];
+    p.out[((int64_t)b * Hq + h) * D + tid] = (uint16_t)dense_pack<T>(L == 0.f ? 0.f : U / L, 0.f);
+  }
 }
 
 template <class T, int D>
@@ -333,8 +392,14 @@ hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
 }
 template <class T, int D>
 hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
-  k_dense_decode<T, D><<<(p.target + p.B) * p.Hkv, 256, 0, s>>>(p);
-  if (p.max_len > p.min_units * kDenseUnit) k_dense_join<T, D><<<p.B * p.Hkv * p.G, D, 0, s>>>(p);
+  const int lds = kDenseWaves * D * 4 * (p.G > 16 ? p.G : 16);      // 16 rows of fp32 are as much as 32 keys
+  static LdsLimit limit;
+  if (lds + kDenseWaves * 16 * 8 > 65536) {
+    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode<T, D>, kDenseWaves * 16 * D * 4);
+    if (e != hipSuccess) return e;
+  }
+  k_dense_decode<T, D><<<(p.target + p.B) * p.Hkv, 64 * kDenseWaves, lds, s>>>(p);
+  if (p.max_len > p.min_units * kDenseUnit) k_dense_join<T, D><<<p.B * p.Hkv * p.G, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 

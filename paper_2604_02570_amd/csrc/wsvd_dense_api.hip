@@ -35,7 +35,8 @@ wsvd_status check_rows(const void* p, int64_t ld, int64_t width) {
 }
 
 DensePages pages_of(const wsvd_paged_cache* c) {
-  return {(uint16_t*)c->k_codes, (uint16_t*)c->v_codes, c->seq_lens, c->block_table, c->page_rows, c->max_pages, c->n_pages};
+  return {(uint16_t*)c->k_codes, (uint16_t*)c->v_codes, c->seq_lens, c->block_table, c->page_rows, c->max_pages, c->n_pages,
+          dense_page_magic(c->page_rows)};
 }
 float scale_of(const wsvd_dense_desc* d) {
   const float s = d->sm_scale != 0.f ? d->sm_scale : 1.f / __builtin_sqrtf((float)d->d_head);
@@ -103,7 +104,7 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   p.q = (const uint16_t*)q; p.q_ld = q_ld; p.out = (uint16_t*)out; p.pages = pages_of(cache);
   p.parts = (float*)ctx->ws + kWsCounterInts;
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads;
-  p.max_len = max_seq_len; p.target = dense_target(p.Hkv); p.min_units = 2;
+  p.max_len = max_seq_len; p.target = dense_target(p.Hkv); p.min_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : 4;
   p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
   return launched(wsvd_launch_dense_decode(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
 }

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     for (int base = 0; base < p.B; base += 64) {
       int start, k = 0;
       if (base + lane < p.B) k = (bounds(p.cu_q, base + lane, p.n_q, start) * p.G + ROWS - 1) / ROWS;
-      const int end = before + wave_prefix_int(k, lane);
+      const int end = before + wave_prefix_int(k);
       const unsigned long long m = __ballot(end > idx);
       if (m) {
         const int l = __builtin_ctzll(m);
@@ -109,11 +109,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const uint8_t *ks, *vs;
       uint32_t ko, vo;
       if (PAGED) {
-        const int granule = min((kb * kKeys + r0) >> 4, (nk - 1) >> 4), per_page = p.pages.page_rows >> 4, pg = granule / per_page;
+        const int granule = min((kb * kKeys + r0) >> 4, (nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
         int page = __builtin_amdgcn_readfirstlane(table[pg]);
         bad |= page < 0 || page >= p.pages.n_pages;
         page = page < 0 || page >= p.pages.n_pages ? 0 : page;
-        const size_t base = (((size_t)page * p.Hkv + kv) * p.pages.page_rows + (granule - pg * per_page) * 16) * ROW_BYTES;
+        const size_t base = (((size_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * ROW_BYTES;
         ks = (const uint8_t*)p.pages.k + base; vs = (const uint8_t*)p.pages.v + base;
         ko = vo = (uint32_t)((r & 15) * ROW_BYTES);
       } else {
