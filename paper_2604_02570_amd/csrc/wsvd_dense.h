@@ -44,6 +44,7 @@ WSVD_DEV int wave_prefix_int(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);      // row_bcast 31 into rows 2 and 3
   return x;
 }
+WSVD_DEV int wave_max_int(int x) { return (int)wave_max((float)x); }     // for numbers below 2^24
 WSVD_DEV int wave_sum_int(int x) { return __builtin_amdgcn_readlane(wave_prefix_int(x), 63); }
 
 // The sequence that packed token t belongs to: the number of sequences that end at or before it (B where none is left).
@@ -77,12 +78,34 @@ inline __host__ __device__ int dense_page_index(int granule, uint32_t magic) {
 }
 
 // ---------------------------------------------------------------- how the decode attention divides its work
-// The rows of all sequences are dealt out in chunks of the same number of units (kDenseUnit rows), as many that about `target`
-// chunks come of it, none of them across two sequences: at most target + B.
-constexpr int kDenseUnit = 128;
-constexpr int kDenseWaves = 8;
-constexpr int kDenseWorkgroups = 256;                // one of 8 waves on each of 256 CUs
+// A CU holds one workgroup of kDenseWaves waves.  Sequences are cut into chunks of whole units (kDenseUnit rows), all of one
+// sequence about equal, none with more than dense_units: no more than `target` chunks per kv head in all, where there are fewer
+// sequences than that, and at most target + B in any case (u / units + 1 chunks for a sequence of u units, total / units <= target).
+constexpr int kDenseWaves = 8, kDenseUnit = 128, kDenseWorkgroups = 256;
 inline __host__ __device__ int dense_target(int Hkv) { return kDenseWorkgroups / Hkv > 1 ? kDenseWorkgroups / Hkv : 1; }
+inline __host__ __device__ int dense_units_of(int len) { return (int)(((unsigned)len + kDenseUnit - 1) / kDenseUnit); }
+inline __host__ __device__ int dense_chunks(int u, int units) { return u > units ? (u + units - 1) / units : 1; }
+// The most units of a chunk: all, where the longest sequence has no more than alone_units (one CU streams 74 GB/s, so that 330 KB
+// take as long as the hand-over that a cut costs); else at least min_units, and for up to 64 sequences the least at which there
+// are at most `target` chunks (a chunk too many is a second round of workgroups: 23 ragged sequences of up to 3001 rows, 8 kv
+// heads: 43.8 -> 36.5 us).  count(units): the chunks of all sequences.
+template <class Count>
+inline __host__ __device__ int dense_units(int total, int most, int B, int target, int alone_units, int min_units, Count count) {
+  if (most <= alone_units) return alone_units;
+  int units = (int)(((int64_t)total + target - 1) / target);
+  units = units > min_units ? units : min_units;
+  if (B > 64 || B > target || units >= most || count(units) <= target) return units;
+  int low = units, high = most;                      // at `most` there are B chunks
+  while (high - low > 1) {
+    const int mid = (low + high) / 2;
+    if (count(mid) <= target) high = mid; else low = mid;
+  }
+  return high;
+}
+// Partial results are folded by groups of kDenseFold chunks and then by groups of those: kDenseFold^2 chunks at most, which no
+// sequence exceeds (of total / target units or more a chunk, it has at most `target`).
+constexpr int kDenseFold = 16;
+static_assert(kDenseWorkgroups <= kDenseFold * kDenseFold, "");
 
 struct DenseAppendParams {
   const uint16_t *q, *k, *v;
@@ -99,8 +122,8 @@ struct DenseDecodeParams {
   int64_t q_ld;
   uint16_t* out;
   DensePages pages;
-  float* parts;                 // [chunk][Hkv][G][d + 2]
-  int B, Hkv, G, max_len, target, min_units;
+  unsigned long long* parts;    // words {value, tag} [chunk][Hkv][G][d + 2]: maximum, sum, row
+  int B, Hkv, G, max_len, target, alone_units, min_units;
   float c_scale;                // sm_scale * log2(e)
   int* err_word;
 };

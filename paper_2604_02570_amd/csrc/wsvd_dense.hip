@@ -1,5 +1,6 @@
 // Dense layers next to latent ones: rotary embedding with the append to a paged cache of plain keys and values, and the
 // attention of one new token per sequence over it.
+#include "wsvd_attn_common.h"
 #include "wsvd_dense.h"
 
 namespace {
@@ -93,27 +94,28 @@ __global__ __launch_bounds__(256) void k_dense_append(DenseAppendParams p) {
 }
 
 // ---------------------------------------------------------------- decode attention
-// A chunk's place: sequence, chunk of it, chunks it has; false for a workgroup that has none.
+// A workgroup's place: sequence, chunk of it, chunks it has, its length, the rows of a chunk; false for a workgroup that has none.
 struct DensePlace { int b, chunk, n_chunks, len, rows; };
 
 WSVD_DEV int dense_length(const DenseDecodeParams& p, int b) { return b < p.B ? min(max(p.pages.seq_lens[b], 0), p.max_len) : 0; }
-// units a chunk takes, from the lengths of all sequences
-WSVD_DEV int dense_chunk_units(const DenseDecodeParams& p, int lane) {
-  int total = 0;
-  for (int base = 0; base < p.B; base += 64) total += wave_sum_int((dense_length(p, base + lane) + kDenseUnit - 1) / kDenseUnit);
-  return max(p.min_units, (total + p.target - 1) / p.target);
-}
-WSVD_DEV int dense_chunks(const DenseDecodeParams& p, int b, int units, int& len) {
-  len = dense_length(p, b);
-  const int u = (len + kDenseUnit - 1) / kDenseUnit;
-  return b < p.B ? max(1, (u + units - 1) / units) : 0;
-}
+
+// Every wave finds its workgroup's place from the lengths of all sequences: the most units a chunk may take (dense_units), the
+// sequences' chunks, and their prefix sums.
 WSVD_DEV bool dense_place(const DenseDecodeParams& p, int idx, int lane, DensePlace& at) {
-  const int units = dense_chunk_units(p, lane);
+  const int mine = dense_length(p, lane);            // (the first 64 sequences' lengths are read once)
+  auto length = [&](int base) { return base == 0 ? mine : dense_length(p, base + lane); };
+  int total = 0, most = 0;
+  for (int base = 0; base < p.B; base += 64) {
+    const int u = dense_units_of(length(base));
+    total += wave_sum_int(u);
+    most = max(most, wave_max_int(u));
+  }
+  const int units = dense_units(total, most, p.B, p.target, p.alone_units, p.min_units, [&](int units) {
+    return wave_sum_int(lane < p.B ? dense_chunks(dense_units_of(mine), units) : 0);
+  });
   int first = 0;
   for (int base = 0; base < p.B; base += 64) {
-    int len;
-    const int n = dense_chunks(p, base + lane, units, len);
+    const int len = length(base), u = dense_units_of(len), n = base + lane < p.B ? dense_chunks(u, units) : 0;
     const int end = first + wave_prefix_int(n);
     const unsigned long long m = __ballot(end > idx);
     if (m) {
@@ -122,7 +124,7 @@ WSVD_DEV bool dense_place(const DenseDecodeParams& p, int idx, int lane, DensePl
       at.n_chunks = __builtin_amdgcn_readlane(n, l);
       at.chunk = idx - (__builtin_amdgcn_readlane(end, l) - at.n_chunks);
       at.len = __builtin_amdgcn_readlane(len, l);
-      at.rows = units * kDenseUnit;
+      at.rows = (__builtin_amdgcn_readlane(u, l) + at.n_chunks - 1) / at.n_chunks * kDenseUnit;
       return true;
     }
     first = __builtin_amdgcn_readlane(end, 63);
@@ -137,6 +139,93 @@ WSVD_DEV float quarters_max(float x) {
 WSVD_DEV float quarters_sum(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// ---------------------------------------------------------------- joining the chunks of a sequence
+// A chunk's partial results (maximum, sum and un-normalised row of every head of the group) go to the workgroup of the last chunk
+// of its group of kDenseFold, and where there are several groups, their results to the workgroup of the sequence's last chunk: as
+// words {value, tag}, as the latent attention's splits hand theirs over (attn_merge_splits: who waits has a higher workgroup
+// number than those it waits for, and the wait is bounded).  The fold is in the order of the chunks.  Words are cleared
+// where they are read.  (A join by a second launch: 3.4 us more for 2 chunks of 32 heads; by the workgroup that draws the last
+// ticket: 2.9.)
+WSVD_DEV unsigned long long* dense_part(const DenseDecodeParams& p, int chunk, int kv, int d) {
+  return p.parts + ((size_t)chunk * p.Hkv + kv) * p.G * (d + 2);
+}
+WSVD_DEV void dense_push(unsigned long long* to, float v) { __hip_atomic_store(to, split_word(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// the words from[k * stride], k < n <= N; false: they have not come within the bound
+template <int N>
+WSVD_DEV bool dense_pull(const unsigned long long* from, size_t stride, int n, float (&v)[N]) {
+  for (int budget = 1 << 14; budget; budget--) {
+    unsigned long long w[N];
+    bool all = true;
+#pragma unroll
+    for (int k = 0; k < N; k++)
+      w[k] = k < n ? __hip_atomic_load(from + k * stride, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : split_word(0.f);
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+      all = all && (uint32_t)(w[k] >> 32) == kSplitTag;
+      v[k] = __uint_as_float((uint32_t)w[k]);
+    }
+    if (all) return true;
+    __builtin_amdgcn_s_sleep(1);
+  }
+  return false;
+}
+
+// What a workgroup holds of its chunk, or of its group's chunks: by output e = head * D + dim, as many as a thread has.
+template <int D>
+struct DensePartial {
+  static constexpr int N = 16 * D / (64 * kDenseWaves);
+  float M[N], L[N], U[N];
+};
+
+// Takes the partial results of n < kDenseFold chunks, `step` apart from `chunk` on, in front of its own.
+template <int D>
+WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n, int kv, DensePartial<D>& own, float* sh /* [2][kDenseFold][16] */) {
+  constexpr int NF = kDenseFold - 1;
+  const int tid = threadIdx.x, G = p.G;
+  unsigned long long* const part = dense_part(p, chunk, kv, D);
+  const size_t stride = (size_t)step * p.Hkv * G * (D + 2);
+  float *m_sh = sh, *l_sh = sh + kDenseFold * 16;
+  bool came = true;
+  if (tid < n * G) {
+    const int k = tid / G, g = tid - k * G;
+    unsigned long long* const at = part + k * stride + g * (D + 2);
+    float ml[2];
+    came = dense_pull<2>(at, 1, 2, ml);
+    m_sh[k * 16 + g] = ml[0];
+    l_sh[k * 16 + g] = ml[1];
+    __hip_atomic_store(at, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(at + 1, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  float u[NF];
+  if (tid < G * D) came = dense_pull<NF>(part + tid / D * (D + 2) + 2 + tid % D, stride, n, u) && came;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < DensePartial<D>::N; i++) {
+    const int e = tid + i * 64 * kDenseWaves, g = e / D;
+    if (e < G * D) {
+      unsigned long long* const at = part + g * (D + 2) + 2 + e % D;
+      if (i > 0) came = dense_pull<NF>(at, stride, n, u) && came;
+      float M = own.M[i], L = 0.f, U = 0.f;
+      for (int k = 0; k < n; k++) M = fmaxf(M, m_sh[k * 16 + g]);
+#pragma unroll
+      for (int k = 0; k < NF; k++)
+        if (k < n) {
+          const float m = m_sh[k * 16 + g], w = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);  // (nothing seen: l and u are 0, or NaN)
+          L += l_sh[k * 16 + g] * w;
+          U += u[k] * w;
+          __hip_atomic_store(at + k * stride, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+      const float w = own.M[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(own.M[i] - M);
+      own.L[i] = L + own.L[i] * w;
+      own.U[i] = U + own.U[i] * w;
+      own.M[i] = M;
+    }
+  }
+  if (!came) atomicExch(p.err_word, (int)WSVD_E_HIP);              // never seen; keeps the wait finite
+  __syncthreads();
 }
 
 template <int D>
@@ -158,7 +247,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
   if (at.chunk == 0 && kv == 0 && threadIdx.x == 0 && p.pages.seq_lens[at.b] > p.max_len) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   const int G = p.G;
   const int first = at.chunk * at.rows, end = min(at.len, first + at.rows);
-  const int n_tiles = (end - first + 31) >> 5;
+  const int n_tiles = (max(end - first, 0) + 31) >> 5;
 
   // queries as the second operand: column c = head of the group
   v4i q[NK];
@@ -297,90 +386,48 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
       for (int i = 0; i < 4; i++) o_sh[(wave * G + c) * D + NJ * (4 * qd + i) + j] = o[j][i];
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < G * D; e += 64 * NW) {
-    const int g = e / D, x = e % D;
-    float M = m_sh[0][g];
+  DensePartial<D> r;
 #pragma unroll
-    for (int w = 1; w < NW; w++) M = fmaxf(M, m_sh[w][g]);
-    float L = 0.f, U = 0.f;
+  for (int i = 0; i < DensePartial<D>::N; i++) {
+    const int e = threadIdx.x + i * 64 * NW, g = e / D, x = e % D;
+    r.M[i] = -INFINITY; r.L[i] = r.U[i] = 0.f;
+    if (e < G * D) {
 #pragma unroll
-    for (int w = 0; w < NW; w++) {
-      const float k = m_sh[w][g] == -INFINITY ? (l_sh[w][g] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m_sh[w][g] - M);
-      L += l_sh[w][g] * k;
-      U += o_sh[(w * G + g) * D + x] * k;
-    }
-    if (at.n_chunks == 1) {
-      const float r = L == 0.f ? 0.f : U / L;
-      p.out[((int64_t)at.b * p.Hkv * G + kv * G + g) * D + x] = (uint16_t)dense_pack<T>(r, 0.f);
-    } else {
-      float* part = p.parts + (((size_t)idx * p.Hkv + kv) * G + g) * (D + 2);
-      part[2 + x] = U;
-      if (x == 0) { part[0] = M; part[1] = L; }
+      for (int w = 0; w < NW; w++) r.M[i] = fmaxf(r.M[i], m_sh[w][g]);
+#pragma unroll
+      for (int w = 0; w < NW; w++) {
+        const float k = m_sh[w][g] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_sh[w][g] - r.M[i]);
+        r.L[i] += l_sh[w][g] * k;
+        r.U[i] += o_sh[(w * G + g) * D + x] * k;
+      }
     }
   }
-}
-
-// The chunks of a sequence joined, one workgroup per (sequence, head).  The chunks' maxima and sums first, one per thread, then
-// the rows of 4 or 2 chunks side by side, each group of D threads its own in their order, eight at a time: a chunk after the
-// other, each waiting for its row, took 68 us for 127 chunks.
-template <class T, int D>
-__global__ __launch_bounds__(256) void k_dense_join(DenseDecodeParams p) {
-  constexpr int GROUPS = 256 / D;
-  __shared__ float w_sh[kDenseWorkgroups], red_sh[4], u_sh[GROUPS][D];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, Hq = p.Hkv * p.G, b = blockIdx.x / Hq, h = blockIdx.x % Hq;
-  const int units = dense_chunk_units(p, lane);
-  int first = 0, n = 0;
-  for (int base = 0; base <= b; base += 64) {
-    int len;
-    const int k = dense_chunks(p, base + lane, units, len);
-    const int end = wave_prefix_int(k);
-    if (b - base < 64) { n = __builtin_amdgcn_readlane(k, b - base); first += __builtin_amdgcn_readlane(end, b - base) - n; }
-    else first += __builtin_amdgcn_readlane(end, 63);
+  if (at.n_chunks > 1) {
+    const int c0 = idx - at.chunk, group = at.chunk / kDenseFold, n_groups = (at.n_chunks + kDenseFold - 1) / kDenseFold;
+    const bool last = at.chunk == at.n_chunks - 1, ends = last || at.chunk % kDenseFold == kDenseFold - 1;
+    __syncthreads();
+    const int folds = !ends ? 0 : last && n_groups > 1 ? 2 : 1;
+#pragma unroll 1
+    for (int i = 0; i < folds; i++)                  // the group's chunks, then the groups' results
+      dense_fold<D>(p, i == 0 ? c0 + group * kDenseFold : c0 + kDenseFold - 1, i == 0 ? 1 : kDenseFold,
+                    i == 0 ? at.chunk % kDenseFold : n_groups - 1, kv, r, o_sh);
+    if (!last) {
+      unsigned long long* const part = dense_part(p, idx, kv, D);
+#pragma unroll
+      for (int i = 0; i < DensePartial<D>::N; i++) {
+        const int e = threadIdx.x + i * 64 * NW, g = e / D, x = e % D;
+        if (e < G * D) {
+          dense_push(part + g * (D + 2) + 2 + x, r.U[i]);
+          if (x == 0) { dense_push(part + g * (D + 2), r.M[i]); dense_push(part + g * (D + 2) + 1, r.L[i]); }
+        }
+      }
+      return;
+    }
   }
-  if (n <= 1) return;
-  const size_t step = (size_t)Hq * (D + 2);
-  const float* part = p.parts + (size_t)first * step + (size_t)h * (D + 2);
-  float m[2], l[2], M = -INFINITY;                   // (at most kDenseWorkgroups + 1 chunks)
 #pragma unroll
-  for (int i = 0; i < 2; i++) {
-    const int at = tid + 256 * i;
-    m[i] = at < n ? part[at * step] : -INFINITY;
-    l[i] = at < n ? part[at * step + 1] : 0.f;
-    M = fmaxf(M, m[i]);
-  }
-  M = wave_max(M);
-  if (lane == 0) red_sh[wave] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(red_sh[0], red_sh[1]), fmaxf(red_sh[2], red_sh[3]));
-  float L = 0.f;
-#pragma unroll
-  for (int i = 0; i < 2; i++) {
-    const float e = m[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - M);    // (nothing seen: l and the row are 0, or NaN)
-    if (tid + 256 * i < n) w_sh[tid + 256 * i] = e;
-    L += l[i] * e;
-  }
-  L = wave_sum(L);
-  __syncthreads();
-  if (lane == 0) red_sh[wave] = L;
-  __syncthreads();
-  L = (red_sh[0] + red_sh[1]) + (red_sh[2] + red_sh[3]);
-  const int g = tid / D, x = tid % D;
-  float U = 0.f;
-  for (int i0 = g; i0 < n; i0 += 8 * GROUPS) {
-    float u[8];
-#pragma unroll
-    for (int k = 0; k < 8; k++) u[k] = part[(size_t)min(i0 + k * GROUPS, n - 1) * step + 2 + x];
-#pragma unroll
-    for (int k = 0; k < 8; k++)
-      if (i0 + k * GROUPS < n) U += u[k] * w_sh[i0 + k * GROUPS];
-  }
-  u_sh[g][x] = U;
-  __syncthreads();
-  if (tid < D) {
-    U = u_sh[0][tid];
-#pragma unroll
-    for (int k = 1; k < GROUPS; k++) U += u_sh[k][tid];
-    p.out[((int64_t)b * Hq + h) * D + tid] = (uint16_t)dense_pack<T>(L == 0.f ? 0.f : U / L, 0.f);
+  for (int i = 0; i < DensePartial<D>::N; i++) {
+    const int e = threadIdx.x + i * 64 * NW;
+    if (e < G * D) p.out[((int64_t)at.b * p.Hkv * G + kv * G) * D + e] = (uint16_t)dense_pack<T>(r.L[i] == 0.f ? 0.f : r.U[i] / r.L[i], 0.f);
   }
 }
 
@@ -399,7 +446,6 @@ hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   k_dense_decode<T, D><<<(p.target + p.B) * p.Hkv, 64 * kDenseWaves, lds, s>>>(p);
-  if (p.max_len > p.min_units * kDenseUnit) k_dense_join<T, D><<<p.B * p.Hkv * p.G, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
