@@ -141,11 +141,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   typedef short v4s __attribute__((ext_vector_type(4)));
-  auto read_k = [&](int buf, int kb, int s) {
-    return *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(k_at[s] + buf * STAGE + kb * 32 * ROW_BYTES);
-  };
-  auto read_v = [&](int buf, int d, int s) {         // 16 keys from 16 s, 32 dims from 32 d
-    const uint32_t at = v_at[d] + buf * STAGE + s * 16 * ROW_BYTES;
+  auto read_k = [&](int kb, int s) { return *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(k_at[s] + kb * 32 * ROW_BYTES); };
+  auto read_v = [&](int d, int s) {                  // 16 keys from 16 s, 32 dims from 32 d
+    const uint32_t at = v_at[d] + s * 16 * ROW_BYTES;
     const v2i lo = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)at));
     const v2i hi = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(at + 8 * ROW_BYTES)));
     return v4i{lo[0], lo[1], hi[0], hi[1]};
@@ -158,16 +156,27 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int i = 0; i < 16; i++) o[d][i] = 0.f;
 
-  auto attend = [&](int kb, int buf, auto masked) {
+  auto attend = [&](int kb, auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
     v16f s[2];
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int h = 0; h < 2; h++)
 #pragma unroll
       for (int i = 0; i < 16; i++) s[h][i] = 0.f;
 #pragma unroll
-      for (int x = 0; x < NS; x++) s[h] = T::mfma32(read_k(buf, h, x), q[x], s[h]);
-    }
+    for (int x = 0; x < NS; x++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) s[h] = T::mfma32(read_k(h, x), q[x], s[h]);
+    v4i v0[ND];                                      // the first values' operands come in under the softmax
+#pragma unroll
+    for (int d = 0; d < ND; d++) v0[d] = read_v(d, 0);
+    // operands are asked for AHEAD products before they are needed: left to itself the compiler asks and waits for each
+    constexpr int AHEAD = 4;
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * NS - AHEAD; i++) { __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); }
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++) { __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); __builtin_amdgcn_sched_group_barrier(0x100, ND / 2, 0); }
     __builtin_amdgcn_sched_barrier(0);
     const int rel = limit - kb * kKeys - 4 * half;
     if (MASKED) {
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const v4i pw = {(int)w[h][i], (int)w[h][i + 1], (int)w[h][i + 2], (int)w[h][i + 3]};
 #pragma unroll
       for (int d = 0; d < ND; d++) {
-        v4i a = read_v(buf, d, x);
+        v4i a = x == 0 ? v0[d] : read_v(d, x);
         if (MASKED) {                                // a value that is no number must not meet the weight 0 of a query that does not see it
 #pragma unroll
           for (int y = 0; y < 4; y++) {
@@ -222,10 +231,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         o[d] = T::mfma32(a, pw, o[d]);
       }
     }
+    if (!MASKED) {
+#pragma unroll
+      for (int i = 0; i < 3 * ND; i++) { __builtin_amdgcn_sched_group_barrier(0x100, 2, 0); __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); }
+      __builtin_amdgcn_sched_group_barrier(0x008, ND, 0);
+    }
     if (MASKED && __ballot(odd != 0)) {              // such values, for the queries that do see them
       for (int key = 0; key < kKeys; key++) {
         const bool sees = key - 4 * half <= rel;
-        const uint32_t at = lds0 + buf * STAGE + PLANE + key * ROW_BYTES;
+        const uint32_t at = lds0 + (kb & 1) * STAGE + PLANE + key * ROW_BYTES;
         const int sw = D == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2;
 #pragma unroll
         for (int d = 0; d < ND; d++)
@@ -251,15 +265,25 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     lds_copy_wait_barrier<0>();                      // this block is there, and nobody reads the other stage any more
     if (kb + 1 < n_blocks) stage(kb + 1, (kb + 1) & 1);
   };
+  auto turn = [&] {                                  // the operands' addresses to the other stage
+#pragma unroll
+    for (int s = 0; s < NS; s++) k_at[s] ^= STAGE;
+#pragma unroll
+    for (int d = 0; d < ND; d++) v_at[d] ^= STAGE;
+  };
   if (n_blocks > 0) stage(0, 0);
+#pragma unroll
+  for (int s = 0; s < NS; s++) asm volatile("" : "+v"(q[s]));      // the queries are there: no wait for them in the loops, which would be one for the copies too
   int kb = 0;
   for (; kb < n_whole; kb++) {
     next(kb);
-    attend(kb, kb & 1, std::false_type{});
+    attend(kb, std::false_type{});
+    turn();
   }
   for (; kb < n_blocks; kb++) {
     next(kb);
-    if (kb * kKeys < wseen) attend(kb, kb & 1, std::true_type{});
+    if (kb * kKeys < wseen) attend(kb, std::true_type{});
+    turn();
   }
   if (bad && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   l = halves_sum(l);
