@@ -101,29 +101,27 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int my_row = lane / PIECES, my_piece = lane % PIECES;
   bool bad = false;
   const int* table = PAGED ? p.pages.block_table + (size_t)b * p.pages.max_pages : nullptr;
-  auto stage = [&](int kb, int buf) {
+  auto stage = [&](int kb, int buf, bool keys) {
 #pragma unroll
     for (int i = 0; i < COPIES; i++) {
       const int r0 = (wave * COPIES + i) * RPI, r = r0 + my_row;
-      const int kp = my_piece ^ (D == 128 ? r & 15 : (r >> 1) & 7), vp = my_piece ^ (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
-      const uint8_t *ks, *vs;
-      uint32_t ko, vo;
+      const int sw = keys ? (D == 128 ? r & 15 : (r >> 1) & 7) : (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
+      const uint8_t* from;
+      uint32_t at;
       if (PAGED) {
         const int granule = min((kb * kKeys + r0) >> 4, (nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
         int page = __builtin_amdgcn_readfirstlane(table[pg]);
         bad |= page < 0 || page >= p.pages.n_pages;
         page = page < 0 || page >= p.pages.n_pages ? 0 : page;
         const size_t base = (((size_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * ROW_BYTES;
-        ks = (const uint8_t*)p.pages.k + base; vs = (const uint8_t*)p.pages.v + base;
-        ko = vo = (uint32_t)((r & 15) * ROW_BYTES);
+        from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) + base;
+        at = (uint32_t)((r & 15) * ROW_BYTES);
       } else {
-        const int64_t first = (int64_t)kv_start + kb * kKeys;
-        const int rr = min(r, nk - 1 - kb * kKeys);
-        ks = (const uint8_t*)(p.k + first * p.k_ld + kv * D); vs = (const uint8_t*)(p.v + first * p.v_ld + kv * D);
-        ko = (uint32_t)rr * (uint32_t)p.k_ld * 2u; vo = (uint32_t)rr * (uint32_t)p.v_ld * 2u;
+        const int64_t ld = keys ? p.k_ld : p.v_ld;
+        from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)kv_start + kb * kKeys) * ld + kv * D);
+        at = (uint32_t)min(r, nk - 1 - kb * kKeys) * (uint32_t)ld * 2u;
       }
-      copy16(lds0 + buf * STAGE + r0 * ROW_BYTES, ks, ko + kp * 16);
-      copy16(lds0 + buf * STAGE + PLANE + r0 * ROW_BYTES, vs, vo + vp * 16);
+      copy16(lds0 + buf * STAGE + (keys ? 0 : PLANE) + r0 * ROW_BYTES, from, at + (my_piece ^ sw) * 16);
     }
   };
 
@@ -141,14 +139,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   typedef short v4s __attribute__((ext_vector_type(4)));
-  auto read_k = [&](int kb, int s) { return *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(k_at[s] + kb * 32 * ROW_BYTES); };
-  auto read_v = [&](int d, int s) {                  // 16 keys from 16 s, 32 dims from 32 d
-    const uint32_t at = v_at[d] + s * 16 * ROW_BYTES;
+  auto read_k = [&](uint32_t stage, int kb, int s) {
+    return *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(k_at[s] + stage + kb * 32 * ROW_BYTES);
+  };
+  auto read_v = [&](uint32_t stage, int d, int s) {  // 16 keys from 16 s, 32 dims from 32 d
+    const uint32_t at = v_at[d] + stage + s * 16 * ROW_BYTES;
     const v2i lo = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)at));
     const v2i hi = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(at + 8 * ROW_BYTES)));
     return v4i{lo[0], lo[1], hi[0], hi[1]};
   };
 
+  struct Scores { v16f s[2]; };
   float m = -INFINITY, l = 0.f;
   v16f o[ND];
 #pragma unroll
@@ -156,42 +157,33 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int i = 0; i < 16; i++) o[d][i] = 0.f;
 
-  auto attend = [&](int kb, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
-    v16f s[2];
+  auto multiply = [&](Scores& r, uint32_t stage) {   // a block's scores
 #pragma unroll
     for (int h = 0; h < 2; h++)
 #pragma unroll
-      for (int i = 0; i < 16; i++) s[h][i] = 0.f;
+      for (int i = 0; i < 16; i++) r.s[h][i] = 0.f;
 #pragma unroll
     for (int x = 0; x < NS; x++)
 #pragma unroll
-      for (int h = 0; h < 2; h++) s[h] = T::mfma32(read_k(h, x), q[x], s[h]);
-    v4i v0[ND];                                      // the first values' operands come in under the softmax
-#pragma unroll
-    for (int d = 0; d < ND; d++) v0[d] = read_v(d, 0);
-    // operands are asked for AHEAD products before they are needed: left to itself the compiler asks and waits for each
-    constexpr int AHEAD = 4;
-    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-#pragma unroll
-    for (int i = 0; i < 2 * NS - AHEAD; i++) { __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); }
-#pragma unroll
-    for (int i = 0; i < AHEAD; i++) { __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); __builtin_amdgcn_sched_group_barrier(0x100, ND / 2, 0); }
-    __builtin_amdgcn_sched_barrier(0);
+      for (int h = 0; h < 2; h++) r.s[h] = T::mfma32(read_k(stage, h, x), q[x], r.s[h]);
+  };
+  auto hide = [&](Scores& r, int kb) {               // keys that this lane's query does not see
     const int rel = limit - kb * kKeys - 4 * half;
-    if (MASKED) {
-#pragma unroll
-      for (int h = 0; h < 2; h++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) s[h][i] = 32 * h + 8 * (i >> 2) + (i & 3) > rel ? -INFINITY : s[h][i];
-    }
-    float most = s[0][0];
 #pragma unroll
     for (int h = 0; h < 2; h++)
 #pragma unroll
-      for (int i = 0; i < 16; i++) most = fmaxf(most, s[h][i]);
-    most *= p.c_scale;
-    if (__ballot(most > m + 8.f)) {                  // the reference moves only when a weight would pass 2^8
+      for (int i = 0; i < 16; i++) r.s[h][i] = 32 * h + 8 * (i >> 2) + (i & 3) > rel ? -INFINITY : r.s[h][i];
+  };
+  auto largest = [&](const Scores& r) {
+    float most = r.s[0][0];
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) most = fmaxf(most, r.s[h][i]);
+    return most * p.c_scale;
+  };
+  auto refer = [&](float most) {                     // the reference moves only when a weight would pass 2^8
+    if (__ballot(most > m + 8.f)) {
       const float mn = fmaxf(m, halves_max(most));
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       l *= keep;
@@ -201,52 +193,109 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int i = 0; i < 16; i++) o[d][i] *= keep;
       m = mn;
     }
+  };
+  struct Weights { uint32_t w[2][8]; };
+  auto weigh = [&](const Scores& r, Weights& w) {
     const float ref = m == -INFINITY ? 0.f : m;
-    uint32_t w[2][8];
+    float sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int h = 0; h < 2; h++)
 #pragma unroll
       for (int i = 0; i < 8; i++) {
-        const float a = __builtin_amdgcn_exp2f(fmaf(s[h][2 * i], p.c_scale, -ref)), c = __builtin_amdgcn_exp2f(fmaf(s[h][2 * i + 1], p.c_scale, -ref));
-        l += a; l += c;
-        w[h][i] = dense_pack<T>(a, c);
+        const float a = __builtin_amdgcn_exp2f(fmaf(r.s[h][2 * i], p.c_scale, -ref)), c = __builtin_amdgcn_exp2f(fmaf(r.s[h][2 * i + 1], p.c_scale, -ref));
+        sum[0] += a; sum[1] += c;
+        w.w[h][i] = dense_pack<T>(a, c);
       }
+    l += sum[0] + sum[1];
+  };
+  auto operand = [&](const Weights& w, int x) {      // of 16 keys
+    const int h = x >> 1, i = 4 * (x & 1);
+    return v4i{(int)w.w[h][i], (int)w.w[h][i + 1], (int)w.w[h][i + 2], (int)w.w[h][i + 3]};
+  };
+
+  // One block's weights under the next block's score products (where there is a next one), then its value products under the next
+  // block's maximum.  V0, K1: the stages they lie in; hidden: whether a query may not see all of the next block.
+  auto step = [&](const Scores& r, Scores& next, uint32_t V0, uint32_t K1, int kb_next, auto more, auto hidden) {
+    constexpr bool MORE = decltype(more)::value, HIDDEN = decltype(hidden)::value;
+    Weights w;
+    v4i v0[ND];
+    if (MORE) multiply(next, K1);
+    weigh(r, w);
+#pragma unroll
+    for (int d = 0; d < ND; d++) v0[d] = read_v(V0, d, 0);
+    if (MORE) {
+      // operands are asked for AHEAD products before they are needed (left to itself the compiler asks and waits for each), and a
+      // product is followed by the vector instructions that run beside it
+      constexpr int AHEAD = 4, PER = 64 / NS;
+      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * NS; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i < 2 * NS - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        else __builtin_amdgcn_sched_group_barrier(0x100, ND / 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, PER, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 32 / (2 * NS), 0);
+      }
+    }
     __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+      const v4i pw = operand(w, x);
+#pragma unroll
+      for (int d = 0; d < ND; d++) o[d] = T::mfma32(x == 0 ? v0[d] : read_v(V0, d, x), pw, o[d]);
+    }
+    float most = -INFINITY;
+    if (MORE) {
+      if (HIDDEN) hide(next, kb_next);
+      most = largest(next);
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * ND; i++) {
+      if (i < 3 * ND) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (MORE) __builtin_amdgcn_sched_group_barrier(0x002, ((HIDDEN ? 80 : 16) + 4 * ND - 1) / (4 * ND), 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (MORE) refer(most);
+  };
+  // A block whose values may be no numbers: those must not meet the weight 0 of a query that does not see them.  The products
+  // leave them out, and the queries that do see them get them added.
+  auto careful = [&](int kb) {
+    const uint32_t at = (kb & 1) * STAGE;
+    Scores r;
+    Weights w;
+    multiply(r, at);
+    hide(r, kb);
+    refer(largest(r));
+    weigh(r, w);
     uint32_t odd = 0;
 #pragma unroll
     for (int x = 0; x < 4; x++) {
-      const int h = x >> 1, i = 4 * (x & 1);
-      const v4i pw = {(int)w[h][i], (int)w[h][i + 1], (int)w[h][i + 2], (int)w[h][i + 3]};
+      const v4i pw = operand(w, x);
 #pragma unroll
       for (int d = 0; d < ND; d++) {
-        v4i a = x == 0 ? v0[d] : read_v(d, x);
-        if (MASKED) {                                // a value that is no number must not meet the weight 0 of a query that does not see it
+        v4i a = read_v(at, d, x);
 #pragma unroll
-          for (int y = 0; y < 4; y++) {
-            const uint32_t t = (((uint32_t)a[y] & T::kExponent) + T::kExponentUlp) & 0x80008000u;
-            odd |= t;
-            a[y] &= (int)~(t | (t - (t >> 15)));
-          }
+        for (int y = 0; y < 4; y++) {
+          const uint32_t t = (((uint32_t)a[y] & T::kExponent) + T::kExponentUlp) & 0x80008000u;
+          odd |= t;
+          a[y] &= (int)~(t | (t - (t >> 15)));
         }
         o[d] = T::mfma32(a, pw, o[d]);
       }
     }
-    if (!MASKED) {
-#pragma unroll
-      for (int i = 0; i < 3 * ND; i++) { __builtin_amdgcn_sched_group_barrier(0x100, 2, 0); __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); }
-      __builtin_amdgcn_sched_group_barrier(0x008, ND, 0);
-    }
-    if (MASKED && __ballot(odd != 0)) {              // such values, for the queries that do see them
+    if (__ballot(odd != 0)) {
+      const int rel = limit - kb * kKeys;
       for (int key = 0; key < kKeys; key++) {
-        const bool sees = key - 4 * half <= rel;
-        const uint32_t at = lds0 + (kb & 1) * STAGE + PLANE + key * ROW_BYTES;
+        const bool sees = key <= rel;
+        const uint32_t row_at = lds0 + at + PLANE + key * ROW_BYTES;
         const int sw = D == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2;
 #pragma unroll
         for (int d = 0; d < ND; d++)
 #pragma unroll
           for (int g = 0; g < 4; g++) {
             const int dim = 32 * d + 8 * g + 4 * half;
-            const v2i x = *(const __attribute__((address_space(3))) v2i*)(uintptr_t)(at + ((dim >> 3) ^ sw) * 16 + (dim & 7) * 2);
+            const v2i x = *(const __attribute__((address_space(3))) v2i*)(uintptr_t)(row_at + ((dim >> 3) ^ sw) * 16 + (dim & 7) * 2);
             const uint32_t t0 = (((uint32_t)x[0] & T::kExponent) + T::kExponentUlp) & 0x80008000u;
             const uint32_t t1 = (((uint32_t)x[1] & T::kExponent) + T::kExponentUlp) & 0x80008000u;
             if (sees && (t0 & 0x8000u)) o[d][4 * g] += dense_low<T>((uint32_t)x[0]);
@@ -258,32 +307,69 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   };
 
-  // Blocks that all of the wave's queries see whole, then the others: two loops, since one with both forms copies the
-  // accumulators in every block.
-  const int n_whole = max(0, min(wseen, wall)) / kKeys;
-  auto next = [&](int kb) {
-    lds_copy_wait_barrier<0>();                      // this block is there, and nobody reads the other stage any more
-    if (kb + 1 < n_blocks) stage(kb + 1, (kb + 1) & 1);
+  // Block kb + 1's keys and block kb's values are there, and nobody reads the stages any more that the next copies go to.
+  auto sync = [&](int kb) {
+    lds_copy_wait_barrier<0>();
+    if (kb + 2 < n_blocks) stage(kb + 2, kb & 1, true);
+    if (kb + 1 < n_blocks) stage(kb + 1, (kb + 1) & 1, false);
   };
-  auto turn = [&] {                                  // the operands' addresses to the other stage
-#pragma unroll
-    for (int s = 0; s < NS; s++) k_at[s] ^= STAGE;
-#pragma unroll
-    for (int d = 0; d < ND; d++) v_at[d] ^= STAGE;
-  };
-  if (n_blocks > 0) stage(0, 0);
+  const int n_mine = (max(wseen, 0) + kKeys - 1) / kKeys;
+  const int n_whole = max(0, min(wseen, wall)) / kKeys;            // blocks that all of the wave's queries see whole
+  if (n_blocks > 0) {
+    stage(0, 0, true);
+    if (n_blocks > 1) stage(1, 1, true);
+    stage(0, 0, false);
+  }
 #pragma unroll
   for (int s = 0; s < NS; s++) asm volatile("" : "+v"(q[s]));      // the queries are there: no wait for them in the loops, which would be one for the copies too
-  int kb = 0;
-  for (; kb < n_whole; kb++) {
-    next(kb);
-    attend(kb, std::false_type{});
-    turn();
-  }
-  for (; kb < n_blocks; kb++) {
-    next(kb);
-    if (kb * kKeys < wseen) attend(kb, std::true_type{});
-    turn();
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  if (n_blocks > 0) {
+    Scores r0, r1;
+    int kb = 0;
+    lds_copy_wait_barrier<0>();
+    if (n_mine > 0) {
+      multiply(r0, 0);
+      if (n_whole == 0) hide(r0, 0);
+      refer(largest(r0));
+    }
+    sync(0);                                         // (the third block's keys go where the first one's were)
+    if (n_mine > 0) {
+      for (; kb + 2 < n_whole; kb += 2) {
+        step(r0, r1, 0, STAGE, 0, yes, no);
+        sync(kb + 1);
+        step(r1, r0, STAGE, 0, 0, yes, no);
+        sync(kb + 2);
+      }
+      for (; kb + 1 < n_mine; kb++) {
+        step(r0, r1, (kb & 1) * STAGE, STAGE - (kb & 1) * STAGE, kb + 1, yes, yes);
+        r0 = r1;
+        sync(kb + 1);
+      }
+      step(r0, r1, (kb & 1) * STAGE, 0, 0, no, no);
+    }
+    for (; kb + 1 < n_blocks; kb++) sync(kb + 1);    // (waves whose queries see no more of the keys still copy)
+
+    // Something is no number: it may be a value that met a weight of 0.  All once more, carefully (results that should be no
+    // numbers come out the same).
+    bool fine = true;
+#pragma unroll
+    for (int d = 0; d < ND; d++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) fine = fine && __builtin_isfinite(o[d][i]);
+    if (__syncthreads_or(!fine)) {
+      m = -INFINITY; l = 0.f;
+#pragma unroll
+      for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[d][i] = 0.f;
+      for (kb = 0; kb < n_blocks; kb++) {
+        stage(kb, kb & 1, true);
+        stage(kb, kb & 1, false);
+        lds_copy_wait_barrier<0>();
+        if (kb < n_mine) careful(kb);
+      }
+    }
   }
   if (bad && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   l = halves_sum(l);
