@@ -34,48 +34,43 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int n = lane & 31, half = lane >> 5;
   const int kv = blockIdx.x % p.Hkv;
 
-  // this workgroup's sequence and tile: the last tiles, which see the most keys, first
-  auto bounds = [&](const int* cu, int b, int most, int& start) {
-    start = min(max(cu[b], 0), most);
-    return min(max(cu[b + 1], start), most) - start;
-  };
-  int b = -1, tile = 0;
+  // this workgroup's sequence and tile (a sequence's last tiles, which see the most keys, first), from one read of the lengths
+  int b = -1, tile = 0, q_start = 0, nq = 0, kv_start = 0, nk = 0;
   {
-    int total = 0;
-    for (int base = 0; base < p.B; base += 64) {
-      int start, k = 0;
-      if (base + lane < p.B) k = (bounds(p.cu_q, base + lane, p.n_q, start) * p.G + ROWS - 1) / ROWS;
-      total += wave_sum_int(k);
-    }
-    const int idx = total - 1 - (int)(blockIdx.x / p.Hkv);
-    if (idx < 0) return;
-    int before = 0;
-    for (int base = 0; base < p.B; base += 64) {
-      int start, k = 0;
-      if (base + lane < p.B) k = (bounds(p.cu_q, base + lane, p.n_q, start) * p.G + ROWS - 1) / ROWS;
-      const int end = before + wave_prefix_int(k);
+    const int idx = blockIdx.x / p.Hkv;
+    for (int base = 0, before = 0; base < p.B && b < 0; base += 64) {
+      const int i = base + lane;
+      int qs = 0, n_q = 0, ks = 0, n_k = 0;
+      if (i < p.B) {
+        const int q0 = p.cu_q[i], q1 = p.cu_q[i + 1];
+        if (PAGED) {
+          n_k = p.pages.seq_lens[i];
+        } else {
+          const int k0 = p.cu_kv[i], k1 = p.cu_kv[i + 1];
+          ks = min(max(k0, 0), p.n_kv);
+          n_k = min(max(k1, ks), p.n_kv) - ks;
+        }
+        qs = min(max(q0, 0), p.n_q);
+        n_q = min(max(q1, qs), p.n_q) - qs;
+      }
+      const int k = (n_q * p.G + ROWS - 1) / ROWS, end = before + wave_prefix_int(k);
       const unsigned long long m = __ballot(end > idx);
       if (m) {
-        const int l = __builtin_ctzll(m);
-        b = base + l;
-        tile = idx - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(k, l));
-        break;
+        const int at = __builtin_ctzll(m);
+        b = base + at;
+        tile = __builtin_amdgcn_readlane(end, at) - 1 - idx;
+        q_start = __builtin_amdgcn_readlane(qs, at); nq = __builtin_amdgcn_readlane(n_q, at);
+        kv_start = __builtin_amdgcn_readlane(ks, at); nk = __builtin_amdgcn_readlane(n_k, at);
       }
       before = __builtin_amdgcn_readlane(end, 63);
     }
+    if (b < 0) return;
+    if (PAGED) {
+      const int most = p.pages.max_pages * p.pages.page_rows;
+      if (nk > most && tile == 0 && kv == 0 && threadIdx.x == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+      nk = min(max(nk, 0), most);
+    }
   }
-  int q_start, kv_start = 0;
-  const int nq = bounds(p.cu_q, b, p.n_q, q_start);
-  int nk;
-  if (PAGED) {
-    const int len = p.pages.seq_lens[b], most = p.pages.max_pages * p.pages.page_rows;
-    nk = min(max(len, 0), most);
-    if (len > most && tile == 0 && kv == 0 && threadIdx.x == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
-  } else {
-    nk = bounds(p.cu_kv, b, p.n_kv, kv_start);
-  }
-  q_start = __builtin_amdgcn_readfirstlane(q_start); kv_start = __builtin_amdgcn_readfirstlane(kv_start);
-  nk = __builtin_amdgcn_readfirstlane(nk);
   const int NR = nq * p.G, row0 = tile * ROWS;
   const int ahead = nk - nq;                         // query token i sees the keys up to i + ahead
   const int last_row = min(row0 + ROWS, NR) - 1;
@@ -372,19 +367,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   if (bad && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+  // The output in whole lines: through LDS, a wave's rows in its own part of the stages, the 16-byte pieces of a row permuted.
+  // (Straight from the accumulators a row goes out in pieces of 8 bytes.)
   l = halves_sum(l);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (wrow + n < NR) {
-    uint16_t* op = p.out + (int64_t)(q_start + tok) * p.out_ld + head * D + 4 * half;
+  __syncthreads();                                   // nobody reads the stages any more
+  const uint32_t put = lds0 + wave * (32 * ROW_BYTES) + n * ROW_BYTES;
+  const int put_sw = D == 128 ? n & 15 : (n >> 1) & 7;
 #pragma unroll
-    for (int d = 0; d < ND; d++)
+  for (int d = 0; d < ND; d++)
 #pragma unroll
-      for (int g = 0; g < 4; g++) {
-        v2i r;
-        r[0] = (int)dense_pack<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
-        r[1] = (int)dense_pack<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
-        *(v2i*)(op + 32 * d + 8 * g) = r;
-      }
+    for (int g = 0; g < 4; g++) {
+      v2i r;
+      r[0] = (int)dense_pack<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
+      r[1] = (int)dense_pack<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
+      *(__attribute__((address_space(3))) v2i*)(uintptr_t)(put + ((4 * d + g) ^ put_sw) * 16 + half * 8) = r;
+    }
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; i++) {
+    const int r = i * RPI + my_row, out_row = wrow + r;
+    const int t = out_row / p.G, h = kv * p.G + out_row - t * p.G;
+    const v4i x = *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(lds0 + wave * (32 * ROW_BYTES) + r * ROW_BYTES +
+                                                                            (my_piece ^ (D == 128 ? r & 15 : (r >> 1) & 7)) * 16);
+    if (out_row < NR) *(v4i*)(p.out + (int64_t)(q_start + t) * p.out_ld + h * D + my_piece * 8) = x;
   }
 }
 
