@@ -94,8 +94,19 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // staging: a wave's share of a block's rows, the 16-byte pieces of a row permuted so that the reads below meet no bank twice
   const uint32_t lds0 = lds_address(lds);
   const int my_row = lane / PIECES, my_piece = lane % PIECES;
+  // Paged: a wave's rows of a block lie in one granule of 16.  Where they lie is looked up for 64 blocks at a time, a lane for each.
+  static_assert(16 % (kKeys / NW) == 0, "");
   bool bad = false;
-  const int* table = PAGED ? p.pages.block_table + (size_t)b * p.pages.max_pages : nullptr;
+  uint32_t at_low = 0, at_high = 0;
+  int looked_up = 0;                                 // the first of those blocks
+  auto look_up = [&](int kb) {
+    looked_up = kb;
+    const int granule = min(((kb + lane) * kKeys + wave * (kKeys / NW)) >> 4, (nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
+    int page = p.pages.block_table[(size_t)b * p.pages.max_pages + pg];
+    if (page < 0 || page >= p.pages.n_pages) { bad = true; page = 0; }
+    const uint64_t at = (((uint64_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * ROW_BYTES;
+    at_low = (uint32_t)at; at_high = (uint32_t)(at >> 32);
+  };
   auto stage = [&](int kb, int buf, bool keys) {
 #pragma unroll
     for (int i = 0; i < COPIES; i++) {
@@ -104,12 +115,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const uint8_t* from;
       uint32_t at;
       if (PAGED) {
-        const int granule = min((kb * kKeys + r0) >> 4, (nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
-        int page = __builtin_amdgcn_readfirstlane(table[pg]);
-        bad |= page < 0 || page >= p.pages.n_pages;
-        page = page < 0 || page >= p.pages.n_pages ? 0 : page;
-        const size_t base = (((size_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * ROW_BYTES;
-        from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) + base;
+        const int i = kb - looked_up;
+        from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) +
+               ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, i) << 32);
         at = (uint32_t)((r & 15) * ROW_BYTES);
       } else {
         const int64_t ld = keys ? p.k_ld : p.v_ld;
@@ -305,12 +313,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // Block kb + 1's keys and block kb's values are there, and nobody reads the stages any more that the next copies go to.
   auto sync = [&](int kb) {
     lds_copy_wait_barrier<0>();
+    if (PAGED && kb + 2 >= looked_up + 64) look_up(kb + 1);
     if (kb + 2 < n_blocks) stage(kb + 2, kb & 1, true);
     if (kb + 1 < n_blocks) stage(kb + 1, (kb + 1) & 1, false);
   };
   const int n_mine = (max(wseen, 0) + kKeys - 1) / kKeys;
   const int n_whole = max(0, min(wseen, wall)) / kKeys;            // blocks that all of the wave's queries see whole
   if (n_blocks > 0) {
+    if (PAGED) look_up(0);
     stage(0, 0, true);
     if (n_blocks > 1) stage(1, 1, true);
     stage(0, 0, false);
@@ -359,6 +369,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int i = 0; i < 16; i++) o[d][i] = 0.f;
       for (kb = 0; kb < n_blocks; kb++) {
+        if (PAGED && kb % 64 == 0) look_up(kb);
         stage(kb, kb & 1, true);
         stage(kb, kb & 1, false);
         lds_copy_wait_barrier<0>();
@@ -366,7 +377,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       }
     }
   }
-  if (bad && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+  if (__ballot(bad) && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   // The output in whole lines: through LDS, a wave's rows in its own part of the stages, the 16-byte pieces of a row permuted.
   // (Straight from the accumulators a row goes out in pieces of 8 bytes.)
   l = halves_sum(l);
