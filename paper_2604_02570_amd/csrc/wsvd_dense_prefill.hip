@@ -341,13 +341,19 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     sync(0);                                         // (the third block's keys go where the first one's were)
     if (n_mine > 0) {
       for (; kb + 2 < n_whole; kb += 2) {
+        __builtin_amdgcn_s_setprio(1);               // (the wave that multiplies goes before the one that copies or waits: 4 % at 8192 tokens)
         step(r0, r1, 0, STAGE, 0, yes, no);
+        __builtin_amdgcn_s_setprio(0);
         sync(kb + 1);
+        __builtin_amdgcn_s_setprio(1);
         step(r1, r0, STAGE, 0, 0, yes, no);
+        __builtin_amdgcn_s_setprio(0);
         sync(kb + 2);
       }
       for (; kb + 1 < n_mine; kb++) {
+        __builtin_amdgcn_s_setprio(1);
         step(r0, r1, (kb & 1) * STAGE, STAGE - (kb & 1) * STAGE, kb + 1, yes, yes);
+        __builtin_amdgcn_s_setprio(0);
         r0 = r1;
         sync(kb + 1);
       }
