@@ -107,6 +107,9 @@ inline __host__ __device__ int dense_units(int total, int most, int B, int targe
 constexpr int kDenseFold = 16;
 static_assert(kDenseWorkgroups <= kDenseFold * kDenseFold, "");
 
+// A prompt of few tiles shares their keys out among several workgroups a tile: as many as fill the chip's two a CU.
+constexpr int kDensePromptParts = 512, kDensePromptRows = 128;
+
 struct DenseAppendParams {
   const uint16_t *q, *k, *v;
   uint16_t *q_out, *k_out;
@@ -133,7 +136,8 @@ struct DensePromptParams {
   uint16_t* out;
   const int *cu_q, *cu_kv;
   DensePages pages;
-  int B, Hkv, G, causal, n_q, n_kv, tiles;
+  float* parts;                 // of tiles that several workgroups share: [tile][Hkv][split] of 128 x {maximum, sum}, 128 rows
+  int B, Hkv, G, causal, n_q, n_kv, splits;
   float c_scale;
   int* err_word;
 };

@@ -42,6 +42,12 @@ float scale_of(const wsvd_dense_desc* d) {
   const float s = d->sm_scale != 0.f ? d->sm_scale : 1.f / __builtin_sqrtf((float)d->d_head);
   return s * kLog2e;
 }
+wsvd_status check_workspace(const wsvd_ctx* ctx, const wsvd_dense_desc* desc) {
+  size_t need = 0;
+  const wsvd_status st = wsvd_dense_workspace_bytes(desc, &need);
+  if (st != WSVD_OK) return st;
+  return !ctx->ws || ctx->ws_bytes < need ? WSVD_E_WORKSPACE : WSVD_OK;
+}
 wsvd_status launched(hipError_t e) { return e == hipSuccess ? WSVD_OK : WSVD_E_HIP; }
 
 #define WSVD_TRY(expr) do { const wsvd_status st_ = (expr); if (st_ != WSVD_OK) return st_; } while (0)
@@ -54,7 +60,8 @@ wsvd_status wsvd_dense_workspace_bytes(const wsvd_dense_desc* desc, size_t* byte
   if (!bytes) return WSVD_E_NULL;
   WSVD_TRY(check_desc(desc));
   const size_t chunks = (size_t)dense_target(desc->n_kv_heads) + desc->batch;
-  *bytes = (size_t)kWsCounterInts * 4 + chunks * desc->n_q_heads * (desc->d_head + 2) * 8;
+  const size_t decode = chunks * desc->n_q_heads * (desc->d_head + 2) * 8, prompt = (size_t)kDensePromptParts * kDensePromptRows * (desc->d_head + 2) * 4;
+  *bytes = (size_t)kWsCounterInts * 4 + (decode > prompt ? decode : prompt);
   return WSVD_OK;
 }
 
@@ -97,9 +104,7 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   if (max_seq_len < 0) return WSVD_E_SHAPE;
   if (max_seq_len > (int64_t)cache->max_pages * cache->page_rows) return WSVD_E_CAPACITY;
   if ((int64_t)max_seq_len * desc->batch > ((int64_t)1 << 37)) return WSVD_E_SHAPE;      // (units of 128 rows are counted in 32 bits)
-  size_t need;
-  wsvd_dense_workspace_bytes(desc, &need);
-  if (!ctx->ws || ctx->ws_bytes < need) return WSVD_E_WORKSPACE;
+  WSVD_TRY(check_workspace(ctx, desc));
   DenseDecodeParams p = {};
   p.q = (const uint16_t*)q; p.q_ld = q_ld; p.out = (uint16_t*)out; p.pages = pages_of(cache);
   p.parts = (unsigned long long*)((int*)ctx->ws + kWsCounterInts);
@@ -133,6 +138,8 @@ wsvd_status wsvd_dense_prefill_attn(wsvd_ctx* ctx, const wsvd_dense_desc* desc, 
   p.q_ld = q_ld; p.k_ld = k_ld; p.v_ld = v_ld; p.out_ld = out_ld;
   p.cu_q = cu_q; p.cu_kv = cu_kv ? cu_kv : cu_q;
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads; p.causal = causal;
+  WSVD_TRY(check_workspace(ctx, desc));
+  p.parts = (float*)ctx->ws + kWsCounterInts;
   p.n_q = (int)n_q; p.n_kv = (int)n_kv; p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
   return launched(wsvd_launch_dense_prompt(p, desc->dtype, desc->d_head, false, (hipStream_t)hip_stream));
 }
@@ -153,6 +160,8 @@ wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* 
   p.q = (const uint16_t*)q; p.out = (uint16_t*)out; p.q_ld = q_ld; p.out_ld = out_ld;
   p.cu_q = cu_q; p.pages = pages_of(cache);
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads; p.causal = 1;
+  WSVD_TRY(check_workspace(ctx, desc));
+  p.parts = (float*)ctx->ws + kWsCounterInts;
   p.n_q = (int)n_q; p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
   return launched(wsvd_launch_dense_prompt(p, desc->dtype, desc->d_head, true, (hipStream_t)hip_stream));
 }

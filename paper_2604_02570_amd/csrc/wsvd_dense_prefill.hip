@@ -9,17 +9,77 @@
 // it, so P never leaves the registers and the transposed reads of V pick the keys in that order.  A query row is a (token,
 // head) pair, token-major, so the G heads of a kv head share every staged key block, and a tile covers few tokens: less of
 // the causal triangle is computed for nothing.
+#include <algorithm>
 #include <type_traits>
+#include "wsvd_append_split.h"
+#include "wsvd_attn_common.h"
 #include "wsvd_dense.h"
 
 namespace {
 
 constexpr int kKeys = 64;                            // keys of a staged block
+constexpr int kLeastBlocks = 6;                      // blocks that a workgroup of several for one tile has at least
 
 // lds_copy16 without the compiler's knowledge: it would let every later read of LDS wait for the copy (the next block's, while
 // this one is worked on).  The copies are waited for by lds_copy_wait_barrier alone.
 WSVD_DEV void copy16(uint32_t lds, const uint8_t* base, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+
+// A workgroup's sequence and tile (a sequence's last tiles, which see the most keys, first), from one read of the lengths, and what
+// that tile sees.
+struct PromptPlace {
+  int b, q_start, nq, kv_start, nk;
+  int row0;                                          // first of the tile's query rows
+  int ahead, seen;                                   // query token i sees the keys up to i + ahead; keys that the tile's last row sees
+  int n_blocks, splits;                              // blocks of them, and workgroups that share them
+};
+template <bool PAGED, int ROWS>
+WSVD_DEV bool prompt_place(const DensePromptParams& p, int idx, int lane, PromptPlace& at) {
+  const int most = PAGED ? p.pages.max_pages * p.pages.page_rows : p.n_kv;
+  for (int base = 0, before = 0; base < p.B; base += 64) {
+    const int i = base + lane;
+    int qs = 0, n_q = 0, ks = 0, n_k = 0;
+    if (i < p.B) {
+      const int q0 = p.cu_q[i], q1 = p.cu_q[i + 1];
+      if (PAGED) {
+        n_k = p.pages.seq_lens[i];
+      } else {
+        const int k0 = p.cu_kv[i], k1 = p.cu_kv[i + 1];
+        ks = min(max(k0, 0), most);
+        n_k = min(max(k1, ks), most) - ks;
+      }
+      qs = min(max(q0, 0), p.n_q);
+      n_q = min(max(q1, qs), p.n_q) - qs;
+    }
+    const int k = (n_q * p.G + ROWS - 1) / ROWS, end = before + wave_prefix_int(k);
+    const unsigned long long m = __ballot(end > idx);
+    before = __builtin_amdgcn_readlane(end, 63);
+    if (!m) continue;
+    const int l = __builtin_ctzll(m);
+    at.b = base + l;
+    at.row0 = (__builtin_amdgcn_readlane(end, l) - 1 - idx) * ROWS;
+    at.q_start = __builtin_amdgcn_readlane(qs, l); at.nq = __builtin_amdgcn_readlane(n_q, l);
+    at.kv_start = __builtin_amdgcn_readlane(ks, l); at.nk = __builtin_amdgcn_readlane(n_k, l);
+    if (PAGED) {
+      if (at.nk > most && threadIdx.x == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+      at.nk = min(max(at.nk, 0), most);
+    }
+    at.ahead = at.nk - at.nq;
+    at.seen = p.causal ? min(at.nk, (min(at.row0 + ROWS, at.nq * p.G) - 1) / p.G + at.ahead + 1) : at.nk;
+    at.n_blocks = at.seen > 0 ? (at.seen + kKeys - 1) / kKeys : 0;
+    at.splits = max(1, min(p.splits, at.n_blocks / kLeastBlocks));
+    return true;
+  }
+  return false;
+}
+WSVD_DEV float* prompt_part(const DensePromptParams& p, int idx, int kv, int split, int rows, int d) {
+  return p.parts + (((size_t)idx * p.Hkv + kv) * p.splits + split) * rows * (d + 2);
+}
+// Partial results lie where other launches hand over words {value, tag}, and stay there: none of them may look like a tag.
+WSVD_DEV float no_tag(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return __uint_as_float(u == kSplitTag || u == kLLTag ? u ^ 1u : u);
 }
 
 template <class T, int D, bool PAGED, int NW>
@@ -32,54 +92,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, half = lane >> 5;
-  const int kv = blockIdx.x % p.Hkv;
-
-  // this workgroup's sequence and tile (a sequence's last tiles, which see the most keys, first), from one read of the lengths
-  int b = -1, tile = 0, q_start = 0, nq = 0, kv_start = 0, nk = 0;
-  {
-    const int idx = blockIdx.x / p.Hkv;
-    for (int base = 0, before = 0; base < p.B && b < 0; base += 64) {
-      const int i = base + lane;
-      int qs = 0, n_q = 0, ks = 0, n_k = 0;
-      if (i < p.B) {
-        const int q0 = p.cu_q[i], q1 = p.cu_q[i + 1];
-        if (PAGED) {
-          n_k = p.pages.seq_lens[i];
-        } else {
-          const int k0 = p.cu_kv[i], k1 = p.cu_kv[i + 1];
-          ks = min(max(k0, 0), p.n_kv);
-          n_k = min(max(k1, ks), p.n_kv) - ks;
-        }
-        qs = min(max(q0, 0), p.n_q);
-        n_q = min(max(q1, qs), p.n_q) - qs;
-      }
-      const int k = (n_q * p.G + ROWS - 1) / ROWS, end = before + wave_prefix_int(k);
-      const unsigned long long m = __ballot(end > idx);
-      if (m) {
-        const int at = __builtin_ctzll(m);
-        b = base + at;
-        tile = __builtin_amdgcn_readlane(end, at) - 1 - idx;
-        q_start = __builtin_amdgcn_readlane(qs, at); nq = __builtin_amdgcn_readlane(n_q, at);
-        kv_start = __builtin_amdgcn_readlane(ks, at); nk = __builtin_amdgcn_readlane(n_k, at);
-      }
-      before = __builtin_amdgcn_readlane(end, 63);
-    }
-    if (b < 0) return;
-    if (PAGED) {
-      const int most = p.pages.max_pages * p.pages.page_rows;
-      if (nk > most && tile == 0 && kv == 0 && threadIdx.x == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
-      nk = min(max(nk, 0), most);
-    }
-  }
-  const int NR = nq * p.G, row0 = tile * ROWS;
-  const int ahead = nk - nq;                         // query token i sees the keys up to i + ahead
-  const int last_row = min(row0 + ROWS, NR) - 1;
-  const int seen = p.causal ? min(nk, last_row / p.G + ahead + 1) : nk;
-  const int n_blocks = seen > 0 ? (seen + kKeys - 1) / kKeys : 0;
+  const int kv = blockIdx.x % p.Hkv, split = blockIdx.x / p.Hkv % p.splits, idx = blockIdx.x / p.Hkv / p.splits;
+  PromptPlace at;
+  if (!prompt_place<PAGED, ROWS>(p, idx, lane, at) || split >= at.splits) return;
+  // A workgroup of several for a tile has a part of the tile's blocks: key0 on, everything below counts from there.
+  const int key0 = split * at.n_blocks / at.splits * kKeys, n_blocks = (split + 1) * at.n_blocks / at.splits - key0 / kKeys;
+  const int b = at.b, q_start = at.q_start, NR = at.nq * p.G, row0 = at.row0, ahead = at.ahead - key0;
+  const int nk = at.nk - key0, here = min(nk, n_blocks * kKeys);
   // a wave's 32 rows: the keys that its last one sees, and those that all of them see
   const int wrow = row0 + 32 * wave, wlast = min(wrow + 31, NR - 1);
-  const int wseen = wrow >= NR ? 0 : p.causal ? min(nk, wlast / p.G + ahead + 1) : nk;
-  const int wall = p.causal ? wrow / p.G + ahead + 1 : nk;
+  const int wseen = wrow >= NR ? 0 : p.causal ? min(here, wlast / p.G + ahead + 1) : here;
+  const int wall = p.causal ? wrow / p.G + ahead + 1 : here;
 
   // this lane's query: operand of the score product, and the last key it sees
   const int row = min(wrow + n, NR - 1), tok = row / p.G, head = kv * p.G + row - tok * p.G;
@@ -101,11 +124,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   int looked_up = 0;                                 // the first of those blocks
   auto look_up = [&](int kb) {
     looked_up = kb;
-    const int granule = min(((kb + lane) * kKeys + wave * (kKeys / NW)) >> 4, (nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
+    const int granule = min((key0 + (kb + lane) * kKeys + wave * (kKeys / NW)) >> 4, (at.nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
     int page = p.pages.block_table[(size_t)b * p.pages.max_pages + pg];
     if (page < 0 || page >= p.pages.n_pages) { bad = true; page = 0; }
-    const uint64_t at = (((uint64_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * ROW_BYTES;
-    at_low = (uint32_t)at; at_high = (uint32_t)(at >> 32);
+    const uint64_t bytes = (((uint64_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * ROW_BYTES;
+    at_low = (uint32_t)bytes; at_high = (uint32_t)(bytes >> 32);
   };
   auto stage = [&](int kb, int buf, bool keys) {
 #pragma unroll
@@ -113,18 +136,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const int r0 = (wave * COPIES + i) * RPI, r = r0 + my_row;
       const int sw = keys ? (D == 128 ? r & 15 : (r >> 1) & 7) : (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
       const uint8_t* from;
-      uint32_t at;
+      uint32_t off;
       if (PAGED) {
         const int i = kb - looked_up;
         from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) +
                ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, i) << 32);
-        at = (uint32_t)((r & 15) * ROW_BYTES);
+        off = (uint32_t)((r & 15) * ROW_BYTES);
       } else {
         const int64_t ld = keys ? p.k_ld : p.v_ld;
-        from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)kv_start + kb * kKeys) * ld + kv * D);
-        at = (uint32_t)min(r, nk - 1 - kb * kKeys) * (uint32_t)ld * 2u;
+        from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)at.kv_start + key0 + kb * kKeys) * ld + kv * D);
+        off = (uint32_t)min(r, nk - 1 - kb * kKeys) * (uint32_t)ld * 2u;
       }
-      copy16(lds0 + buf * STAGE + (keys ? 0 : PLANE) + r0 * ROW_BYTES, from, at + (my_piece ^ sw) * 16);
+      copy16(lds0 + buf * STAGE + (keys ? 0 : PLANE) + r0 * ROW_BYTES, from, off + (my_piece ^ sw) * 16);
     }
   };
 
@@ -384,6 +407,19 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   if (__ballot(bad) && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+  if (at.splits > 1) {                               // a part: as it is, for k_dense_prompt_join
+    float* const part = prompt_part(p, idx, kv, split, ROWS, D);
+    const int r = 32 * wave + n;
+    const float sum = no_tag(halves_sum(l));
+    if (half == 0) { part[2 * r] = no_tag(m); part[2 * r + 1] = sum; }
+#pragma unroll
+    for (int d = 0; d < ND; d++)
+#pragma unroll
+      for (int g = 0; g < 4; g++)
+        *(v4f*)(part + 2 * ROWS + r * D + 32 * d + 8 * g + 4 * half) =
+            v4f{no_tag(o[d][4 * g]), no_tag(o[d][4 * g + 1]), no_tag(o[d][4 * g + 2]), no_tag(o[d][4 * g + 3])};
+    return;
+  }
   // The output in whole lines: through LDS, a wave's rows in its own part of the stages, the 16-byte pieces of a row permuted.
   // (Straight from the accumulators a row goes out in pieces of 8 bytes.)
   l = halves_sum(l);
@@ -410,11 +446,64 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
+// The parts of the tiles that several workgroups share, joined in their order: 16 rows of a tile per workgroup, 8 or 4 dims of a
+// row per thread.
+template <class T, int D, bool PAGED, int ROWS>
+__global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) {
+  constexpr int N = D / 16;
+  const int lane = threadIdx.x & 63, kv = blockIdx.x % p.Hkv, idx = blockIdx.x / p.Hkv;
+  PromptPlace at;
+  if (!prompt_place<PAGED, ROWS>(p, idx, lane, at) || at.splits == 1) return;
+  const int r = blockIdx.y * 16 + threadIdx.x / 16, x = threadIdx.x % 16 * N, row = at.row0 + r;
+  if (row >= at.nq * p.G) return;
+  float M = -INFINITY, L = 0.f, O[N];
+#pragma unroll
+  for (int i = 0; i < N; i++) O[i] = 0.f;
+  const float* const parts = prompt_part(p, idx, kv, 0, ROWS, D);
+  for (int s0 = 0; s0 < at.splits; s0 += 4) {        // four in flight
+    float m[4], l[4], mn = M;
+    v4f o[4][N / 4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      const float* const part = parts + (size_t)min(s0 + k, at.splits - 1) * ROWS * (D + 2);
+      m[k] = part[2 * r]; l[k] = part[2 * r + 1];
+#pragma unroll
+      for (int i = 0; i < N / 4; i++) o[k][i] = *(const v4f*)(part + 2 * ROWS + r * D + x + 4 * i);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k++) mn = fmaxf(mn, m[k]);
+    const float keep = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mn);
+    L *= keep;                                       // (nothing seen: the sum and the row are 0, or NaN)
+#pragma unroll
+    for (int i = 0; i < N; i++) O[i] *= keep;
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+      if (s0 + k < at.splits) {
+        const float add = m[k] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[k] - mn);
+        L += l[k] * add;
+#pragma unroll
+        for (int i = 0; i < N; i++) O[i] += o[k][i / 4][i % 4] * add;
+      }
+    M = mn;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const int t = row / p.G;
+  uint32_t out[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; i++) out[i] = dense_pack<T>(O[2 * i] * inv, O[2 * i + 1] * inv);
+  __builtin_memcpy(__builtin_assume_aligned(p.out + (int64_t)(at.q_start + t) * p.out_ld + (kv * p.G + row - t * p.G) * D + x, N * 2), out, N * 2);
+}
+
 template <class T, int D, bool PAGED>
 hipError_t launch(DensePromptParams& p, hipStream_t s) {
-  constexpr int NW = 4;
-  p.tiles = (int)(((int64_t)p.n_q * p.G) / (32 * NW)) + p.B;       // at most: every sequence ends inside a tile
-  k_dense_prompt<T, D, PAGED, NW><<<dim3((unsigned)(p.tiles * p.Hkv)), 64 * NW, 0, s>>>(p);
+  constexpr int NW = 4, ROWS = 32 * NW;
+  const int64_t tiles = ((int64_t)p.n_q * p.G) / ROWS + p.B, wgs = tiles * p.Hkv;      // at most: every sequence ends inside a tile
+  // no sequence has more keys than there are, and no workgroup of several fewer than kLeastBlocks blocks of them
+  const int64_t keys = PAGED ? (int64_t)p.pages.max_pages * p.pages.page_rows : p.n_kv;
+  const int64_t most = std::min<int64_t>({32, kDensePromptParts / wgs, (keys + kKeys - 1) / kKeys / kLeastBlocks});
+  p.splits = (int)std::max<int64_t>(most, 1);
+  k_dense_prompt<T, D, PAGED, NW><<<dim3((unsigned)(wgs * p.splits)), 64 * NW, 0, s>>>(p);
+  if (p.splits > 1) k_dense_prompt_join<T, D, PAGED, ROWS><<<dim3((unsigned)wgs, ROWS / 16), 256, 0, s>>>(p);
   return hipGetLastError();
 }
 

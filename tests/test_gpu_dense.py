@@ -362,6 +362,49 @@ def test_chunk_bad_page_is_reported():
     L.close(W.E_SHAPE)
 
 
+# few tiles over many keys: several workgroups share a tile's keys, their parts are joined by a second launch
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(4, 1, 128, "bf16"), (4, 4, 64, "f16"), (7, 1, 128, "f16"), (16, 2, 64, "bf16")])
+def test_chunk_shared_by_workgroups(hq, hkv, d, dtype):
+    prompt_case(hq, hkv, d, dtype, [5, 0, 1, 70], [2600, 900, 3, 1201], page_rows=16)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(3, 1, 128, "bf16"), (2, 2, 64, "f16")])
+def test_prompt_shared_by_workgroups(causal, hq, hkv, d, dtype):
+    prompt_case(hq, hkv, d, dtype, [9, 40, 6], [1500, 20, 2049], causal=causal)
+    prompt_case(hq, hkv, d, dtype, [1100], causal=causal)
+
+
+def test_prompt_shared_by_workgroups_hidden_values():
+    # numbers that are none at the end of the keys, where only the last queries see them, and beyond what any query of a tile sees
+    def tweak(k, v):
+        v[1598, 3], v[1599, 64], v[1400, 7] = math.inf, math.nan, -math.inf
+        k[1597] = math.nan
+    prompt_case(2, 1, 128, "bf16", [6], [1600], tweak=tweak)
+    prompt_case(2, 1, 64, "f16", [300], [1600], tweak=lambda k, v: v[1597:, 5].fill_(math.inf))
+
+
+def test_workspace_serves_decode_and_prompts_in_turn():
+    """Partial results that a prompt leaves in the workspace lie where a decode call's workgroups hand theirs over."""
+    g = gen(31)
+    hq, hkv, d = 8, 1, 64
+    L = Layer(1, hq, hkv, d, "bf16")
+    pool = Pool(g, [4000], hkv, d, 16, "bf16")
+    cache = L.cache(pool)
+    k, v = pool.rows(0)
+    q = randn(g, "bf16", 20, hq * d)
+    qd, cu = q.cuda(), prefix([20]).cuda()
+    out, one = torch.empty(20, hq * d, dtype=torch.bfloat16, device="cuda"), torch.empty(1, hq, d, dtype=torch.bfloat16, device="cuda")
+    for _ in range(3):
+        W.wsvd_dense_prefill_attn_paged(L.ctx, L.desc, qd, hq * d, 20, cu, cache, out, hq * d)
+        W.wsvd_dense_decode_attn_paged(L.ctx, L.desc, qd[19:], hq * d, cache, 4000, one)
+        want, size = attend_fast(q.view(20, hq, d), k, v, torch.arange(3980, 4000), L.scale)
+        check(out.view(20, hq, d).cpu(), want, size, "bf16", True)
+        check(one.cpu(), want[19:], size[19:], "bf16", False)
+        out.zero_(), one.zero_()
+    L.close()
+
+
 # ------------------------------------------------------------------------------------------------ streams and graphs
 def test_decode_step_in_a_graph_on_another_stream():
     """Append and attention captured on a stream of their own; replays after the lengths and inputs have changed give what eager
