@@ -231,10 +231,14 @@ WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n,
 template <int D>
 struct DenseTile {
   v4i k[2][D / 32];                                  // 16 rows each, as they lie in memory
-  uint32_t v[8][D / 32];                             // row 4 quarter + i of either half, D / 16 dims
+  typedef int Piece __attribute__((ext_vector_type(D / 32)));
+  Piece v[8];                                        // row 4 quarter + i of either half, D / 16 dims
 };
+template <bool ONCE, class V>
+WSVD_DEV V load_row(const V* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
 
-template <class T, int D>
+// ONCE: the rows are asked for as data that is read once and need not stay in the caches.
+template <class T, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode(DenseDecodeParams p) {
   constexpr int NK = D / 32, NJ = D / 16, NW = kDenseWaves;
   extern __shared__ __attribute__((aligned(256))) float o_sh[];      // a granule pair's keys for each wave; at the end [NW][G][D]
@@ -280,10 +284,10 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
       const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, 2 * i + g) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, 2 * i + g) << 32;
       const uint16_t *kp = p.pages.k + base, *vp = p.pages.v + base;
 #pragma unroll
-      for (int j = 0; j < NK; j++) tile.k[g][j] = *(const v4i*)(kp + j * 512 + lane * 8);
+      for (int j = 0; j < NK; j++) tile.k[g][j] = load_row<ONCE>((const v4i*)(kp + j * 512 + lane * 8));
 #pragma unroll
       for (int i2 = 0; i2 < 4; i2++)
-        __builtin_memcpy(tile.v[4 * g + i2], __builtin_assume_aligned(vp + (4 * qd + i2) * D + c * NJ, D / 8), NJ * 2);
+        tile.v[4 * g + i2] = load_row<ONCE>((const typename DenseTile<D>::Piece*)(vp + (4 * qd + i2) * D + c * NJ));
     }
   };
   // A wave's keys go through LDS of its own: requested in whole lines (asked for as the product's operand, 16 rows of 64 bytes
@@ -324,7 +328,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
         const bool out = r0 + 16 * (i >> 2) + 4 * qd + (i & 3) >= end;
         s[i] = out ? -INFINITY : s[i];
 #pragma unroll
-        for (int j = 0; j < NK; j++) tile.v[i][j] = out ? 0u : tile.v[i][j];
+        for (int j = 0; j < NK; j++) tile.v[i][j] = out ? 0 : tile.v[i][j];
       }
     }
     float most = s[0];
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
       v4i a;
 #pragma unroll
       for (int i = 0; i < 4; i++)
-        a[i] = (int)__builtin_amdgcn_perm(tile.v[2 * i + 1][j >> 1], tile.v[2 * i][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
+        a[i] = (int)__builtin_amdgcn_perm((uint32_t)tile.v[2 * i + 1][j >> 1], (uint32_t)tile.v[2 * i][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
       o[j] = T::mfma16(a, hi, o[j]);
       o[j] = T::mfma16(a, lo, o[j]);
     }
@@ -437,16 +441,24 @@ hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
   else k_dense_append<T, D, 1><<<p.n_tokens, 256, 0, s>>>(p);
   return hipGetLastError();
 }
-template <class T, int D>
-hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
-  const int lds = kDenseWaves * D * 4 * (p.G > 16 ? p.G : 16);      // 16 rows of fp32 are as much as 32 keys
+template <class T, int D, bool ONCE>
+hipError_t launch_decode_form(const DenseDecodeParams& p, hipStream_t s) {
+  const int lds = kDenseWaves * D * 4 * 16;          // 32 keys a wave, and later 16 rows of fp32
   static LdsLimit limit;
   if (lds + kDenseWaves * 16 * 8 > 65536) {
-    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode<T, D>, kDenseWaves * 16 * D * 4);
+    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode<T, D, ONCE>, lds);
     if (e != hipSuccess) return e;
   }
-  k_dense_decode<T, D><<<(p.target + p.B) * p.Hkv, 64 * kDenseWaves, lds, s>>>(p);
+  k_dense_decode<T, D, ONCE><<<(p.target + p.B) * p.Hkv, 64 * kDenseWaves, lds, s>>>(p);
   return hipGetLastError();
+}
+template <class T, int D>
+hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
+  // Rows of 100 MB and more do not stay in the last-level cache (256 MB) until they are read again, and reading them as data that
+  // does is slower: 32 x 8192 rows of 4 heads (537 MB) 100 us against 90, 8 x 1000 of 32 (131 MB) 27.8 against 25.3; 74 MB over and
+  // over out of that cache 17.9 against 20.
+  const bool once = (int64_t)p.B * p.max_len * p.Hkv * D * 4 >= 100000000;
+  return once ? launch_decode_form<T, D, true>(p, s) : launch_decode_form<T, D, false>(p, s);
 }
 
 }  // namespace
