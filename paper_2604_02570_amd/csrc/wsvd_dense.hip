@@ -5,13 +5,20 @@
 
 namespace {
 
+// ONCE: data that is read or written once and need not stay in the caches
+template <bool ONCE, class V>
+WSVD_DEV V load_row(const V* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
+template <bool ONCE, class V>
+WSVD_DEV void store_row(V* p, V v) { if (ONCE) __builtin_nontemporal_store(v, p); else *p = v; }
+
 // ---------------------------------------------------------------- append
 // Rotation of the new tokens' queries and keys (dims i and i + d/2 turned by position * inv_freq[i]) and their keys and values
 // stored in the pages.  Bound: memory, every element read and written once; few tokens: two dependent loads.
 //   A wave finds its token's sequence, row and page, and its lanes the token's d / 2 angles, once for all heads: in 64 bits as
 // far as whole turns go (an fp32 product of a position of 1e5 would be off by 6e-3 radians), the sine and cosine of what is
 // left in 32.  Then the workgroup goes over the (token, head) pairs, 16 bytes of each half per thread.
-template <class T, int D, int TOK>
+// ONCE: nothing of it need stay in the caches.
+template <class T, int D, int TOK, bool ONCE>
 __global__ __launch_bounds__(256) void k_dense_append(DenseAppendParams p) {
   constexpr int HALF = D / 2, PER = D / 16;          // threads per (token, head)
   __shared__ float cs[TOK][2][HALF];
@@ -64,7 +71,7 @@ __global__ __launch_bounds__(256) void k_dense_append(DenseAppendParams p) {
     const uint16_t* src = kind == 0 ? p.q + t * p.q_ld : kind == 1 ? p.k + t * p.k_ld : p.v + t * p.v_ld;
     if (kind == 0 && !p.q_out) continue;
     src += hh * D + part * 8;
-    v4i a = *(const v4i*)src, b = *(const v4i*)(src + HALF);
+    v4i a = load_row<ONCE>((const v4i*)src), b = load_row<ONCE>((const v4i*)(src + HALF));
     if (p.inv_freq && kind < 2) {
       v4i ra, rb;
 #pragma unroll
@@ -79,16 +86,16 @@ __global__ __launch_bounds__(256) void k_dense_append(DenseAppendParams p) {
     }
     if (kind == 0) {
       uint16_t* dst = p.q_out + t * p.q_out_ld + hh * D + part * 8;
-      *(v4i*)dst = a; *(v4i*)(dst + HALF) = b;
+      store_row<ONCE>((v4i*)dst, a); store_row<ONCE>((v4i*)(dst + HALF), b);
       continue;
     }
     if (kind == 1 && p.k_out) {
       uint16_t* dst = p.k_out + t * p.k_out_ld + hh * D + part * 8;
-      *(v4i*)dst = a; *(v4i*)(dst + HALF) = b;
+      store_row<ONCE>((v4i*)dst, a); store_row<ONCE>((v4i*)(dst + HALF), b);
     }
     if (slot_sh[w] >= 0) {
       uint16_t* dst = (kind == 1 ? p.pages.k : p.pages.v) + (slot_sh[w] + (int64_t)hh * p.pages.page_rows) * D + part * 8;
-      *(v4i*)dst = a; *(v4i*)(dst + HALF) = b;
+      store_row<ONCE>((v4i*)dst, a); store_row<ONCE>((v4i*)(dst + HALF), b);
     }
   }
 }
@@ -234,8 +241,6 @@ struct DenseTile {
   typedef int Piece __attribute__((ext_vector_type(D / 32)));
   Piece v[8];                                        // row 4 quarter + i of either half, D / 16 dims
 };
-template <bool ONCE, class V>
-WSVD_DEV V load_row(const V* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
 
 // ONCE: the rows are asked for as data that is read once and need not stay in the caches.
 template <class T, int D, bool ONCE>
@@ -435,11 +440,22 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
   }
 }
 
+template <class T, int D, int TOK>
+hipError_t launch_append_form(const DenseAppendParams& p, hipStream_t s) {
+  const int wgs = (p.n_tokens + TOK - 1) / TOK;
+  // Calls that move 100 MB and more do not leave their rows in the last-level cache for whoever reads them next: 16 x ~1150 tokens of
+  // 32 heads (1.03 GB) 205 -> 179 us; 4 x 300 of 32 / 8 (17 MB) 8.0 -> 8.3 the other way.
+  if ((int64_t)p.n_tokens * (2 * p.Hq + 4 * p.Hkv) * D * 2 >= 100000000) k_dense_append<T, D, TOK, true><<<wgs, 256, 0, s>>>(p);
+  else k_dense_append<T, D, TOK, false><<<wgs, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
 template <class T, int D>
 hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
-  if (p.n_tokens >= 2048) k_dense_append<T, D, 4><<<(p.n_tokens + 3) / 4, 256, 0, s>>>(p);
-  else k_dense_append<T, D, 1><<<p.n_tokens, 256, 0, s>>>(p);
-  return hipGetLastError();
+  // Tokens of a workgroup: as few as give its 256 threads work, one where there are few (16 x ~1700 tokens of 16 / 2 heads of 64: 4
+  // tokens 50 us, 1 token 74; 16 x 2048 of 28 / 4 heads of 128: 124 and 104).
+  const int items = (p.Hq + 2 * p.Hkv) * (D / 16);
+  if (p.n_tokens < 2048 || items >= 256) return launch_append_form<T, D, 1>(p, s);
+  return items >= 128 ? launch_append_form<T, D, 2>(p, s) : launch_append_form<T, D, 4>(p, s);
 }
 template <class T, int D, bool ONCE>
 hipError_t launch_decode_form(const DenseDecodeParams& p, hipStream_t s) {
