@@ -1,6 +1,7 @@
 // Shared by the dense-layer kernels (uncompressed keys and values in a paged cache): parameters, 16-bit element types, and
 // the wave-wide searches that find a workgroup's sequence from lengths only the device knows.
 #pragma once
+#include "wsvd_dense_plan.h"
 #include "wsvd_dev.h"
 #include "wsvd_internal.h"
 
@@ -67,49 +68,6 @@ struct DensePages {
   int page_rows, max_pages, n_pages;
   uint32_t page_magic;          // dense_page_magic
 };
-// The page of a sequence's granule of 16 rows (granule / (page_rows / 16)) by a product: exact for granules below 2^23 and up to
-// 2^8 granules in a page, since granule * (magic * n - 2^32) < 2^31.  A page of one granule has a magic of 2^32, kept as 0.
-inline __host__ __device__ uint32_t dense_page_magic(int page_rows) {
-  const uint64_t n = (uint64_t)page_rows / 16;
-  return (uint32_t)((((uint64_t)1 << 32) + n - 1) / n);
-}
-inline __host__ __device__ int dense_page_index(int granule, uint32_t magic) {
-  return magic == 0 ? granule : (int)(((uint64_t)(uint32_t)granule * magic) >> 32);
-}
-
-// ---------------------------------------------------------------- how the decode attention divides its work
-// A CU holds one workgroup of kDenseWaves waves.  Sequences are cut into chunks of whole units (kDenseUnit rows), all of one
-// sequence about equal, none with more than dense_units: no more than `target` chunks per kv head in all, where there are fewer
-// sequences than that, and at most target + B in any case (u / units + 1 chunks for a sequence of u units, total / units <= target).
-constexpr int kDenseWaves = 8, kDenseUnit = 128, kDenseWorkgroups = 256;
-inline __host__ __device__ int dense_target(int Hkv) { return kDenseWorkgroups / Hkv > 1 ? kDenseWorkgroups / Hkv : 1; }
-inline __host__ __device__ int dense_units_of(int len) { return (int)(((unsigned)len + kDenseUnit - 1) / kDenseUnit); }
-inline __host__ __device__ int dense_chunks(int u, int units) { return u > units ? (u + units - 1) / units : 1; }
-// The most units of a chunk: all, where the longest sequence has no more than alone_units (one CU streams 74 GB/s, so that 330 KB
-// take as long as the hand-over that a cut costs); else at least min_units, and for up to 64 sequences the least at which there
-// are at most `target` chunks (a chunk too many is a second round of workgroups: 23 ragged sequences of up to 3001 rows, 8 kv
-// heads: 43.8 -> 36.5 us).  count(units): the chunks of all sequences.
-template <class Count>
-inline __host__ __device__ int dense_units(int total, int most, int B, int target, int alone_units, int min_units, Count count) {
-  if (most <= alone_units) return alone_units;
-  int units = (int)(((int64_t)total + target - 1) / target);
-  units = units > min_units ? units : min_units;
-  if (B > 64 || B > target || units >= most || count(units) <= target) return units;
-  int low = units, high = most;                      // at `most` there are B chunks
-  while (high - low > 1) {
-    const int mid = (low + high) / 2;
-    if (count(mid) <= target) high = mid; else low = mid;
-  }
-  return high;
-}
-// Partial results are folded by groups of kDenseFold chunks and then by groups of those: kDenseFold^2 chunks at most, which no
-// sequence exceeds (of total / target units or more a chunk, it has at most `target`).
-constexpr int kDenseFold = 16;
-static_assert(kDenseWorkgroups <= kDenseFold * kDenseFold, "");
-
-// A prompt of few tiles shares their keys out among several workgroups a tile: as many as fill the chip's two a CU.
-constexpr int kDensePromptParts = 512, kDensePromptRows = 128;
-
 struct DenseAppendParams {
   const uint16_t *q, *k, *v;
   uint16_t *q_out, *k_out;

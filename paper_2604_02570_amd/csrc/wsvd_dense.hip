@@ -278,9 +278,8 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
   auto look_up = [&](int t) {
     const int granule = min((first >> 4) + 2 * (t + NW * (lane >> 1)) + (lane & 1), last_granule);
     const int pg = dense_page_index(granule, p.pages.page_magic);
-    int page = table[pg];
-    if (page < 0 || page >= p.pages.n_pages) { bad = true; page = 0; }
-    const uint64_t at = (((uint64_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * D;
+    const int page = dense_page(table[pg], p.pages.n_pages, bad);
+    const uint64_t at = dense_pool_row(page, granule, pg, kv, p.Hkv, p.pages.page_rows) * D;
     at_low = (uint32_t)at; at_high = (uint32_t)(at >> 32);
   };
   auto load = [&](DenseTile<D>& tile, int i) {       // i: the tile's number among those looked up

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   PromptPlace at;
   if (!prompt_place<PAGED, ROWS>(p, idx, lane, at) || split >= at.splits) return;
   // A workgroup of several for a tile has a part of the tile's blocks: key0 on, everything below counts from there.
-  const int key0 = split * at.n_blocks / at.splits * kKeys, n_blocks = (split + 1) * at.n_blocks / at.splits - key0 / kKeys;
+  const int block0 = dense_share(split, at.n_blocks, at.splits), n_blocks = dense_share(split + 1, at.n_blocks, at.splits) - block0, key0 = block0 * kKeys;
   const int b = at.b, q_start = at.q_start, NR = at.nq * p.G, row0 = at.row0, ahead = at.ahead - key0;
   const int nk = at.nk - key0, here = min(nk, n_blocks * kKeys);
   // a wave's 32 rows: the keys that its last one sees, and those that all of them see
@@ -125,9 +125,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   auto look_up = [&](int kb) {
     looked_up = kb;
     const int granule = min((key0 + (kb + lane) * kKeys + wave * (kKeys / NW)) >> 4, (at.nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
-    int page = p.pages.block_table[(size_t)b * p.pages.max_pages + pg];
-    if (page < 0 || page >= p.pages.n_pages) { bad = true; page = 0; }
-    const uint64_t bytes = (((uint64_t)page * p.Hkv + kv) * p.pages.page_rows + (granule * 16 - pg * p.pages.page_rows)) * ROW_BYTES;
+    const int page = dense_page(p.pages.block_table[(size_t)b * p.pages.max_pages + pg], p.pages.n_pages, bad);
+    const uint64_t bytes = dense_pool_row(page, granule, pg, kv, p.Hkv, p.pages.page_rows) * ROW_BYTES;
     at_low = (uint32_t)bytes; at_high = (uint32_t)(bytes >> 32);
   };
   auto stage = [&](int kb, int buf, bool keys) {
