@@ -38,6 +38,10 @@ constexpr int kDenseWaves = 8, kDenseUnit = 128, kDenseWorkgroups = 256;
 WSVD_HD int dense_target(int Hkv) { return kDenseWorkgroups / Hkv > 1 ? kDenseWorkgroups / Hkv : 1; }
 WSVD_HD int dense_units_of(int len) { return (int)(((unsigned)len + kDenseUnit - 1) / kDenseUnit); }
 WSVD_HD int dense_chunks(int u, int units) { return u > units ? (u + units - 1) / units : 1; }
+// Partial results are folded by groups of kDenseFold chunks and then by groups of those: no sequence has more than kDenseFold^2.
+// (Groups of 16: 1 x 65001 rows of 2 heads 18.7 us, of 8: 15.5.  A group's end takes 7 chunks in 2 us, a second level costs 3: all
+// of 16 chunks by the last one's workgroup, 7 at a time, take 15.2 us where two levels take 12.7.)
+constexpr int kDenseFold = 8;
 // The most units of a chunk: all, where the longest sequence has no more than alone_units (one CU streams 74 GB/s, so that 330 KB
 // take as long as the hand-over that a cut costs); else at least min_units, and for up to 64 sequences the least at which there
 // are at most `target` chunks (a chunk too many is a second round of workgroups: 23 ragged sequences of up to 3001 rows, 8 kv
@@ -46,7 +50,9 @@ template <class Count>
 WSVD_HD int dense_units(int total, int most, int B, int target, int alone_units, int min_units, Count count) {
   if (most <= alone_units) return alone_units;
   int units = (int)(((int64_t)total + target - 1) / target);
+  const int least = (most + kDenseFold * kDenseFold - 1) / (kDenseFold * kDenseFold);
   units = units > min_units ? units : min_units;
+  units = units > least ? units : least;
   if (B > 64 || B > target || units >= most || count(units) <= target) return units;
   int low = units, high = most;                      // at `most` there are B chunks
   while (high - low > 1) {
@@ -55,11 +61,6 @@ WSVD_HD int dense_units(int total, int most, int B, int target, int alone_units,
   }
   return high;
 }
-// Partial results are folded by groups of kDenseFold chunks and then by groups of those: kDenseFold^2 chunks at most, which no
-// sequence exceeds (of total / target units or more a chunk, it has at most `target`).
-constexpr int kDenseFold = 16;
-static_assert(kDenseWorkgroups <= kDenseFold * kDenseFold, "");
-
 // A prompt of few tiles shares their keys out among several workgroups a tile: as many as fill the chip's two a CU.
 constexpr int kDensePromptParts = 512, kDensePromptRows = 128;
 
