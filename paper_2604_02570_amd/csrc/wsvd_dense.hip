@@ -309,6 +309,8 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
   for (int j = 0; j < NJ; j++) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
 
+  bool fine = true;                                  // see below
+  float part = 1.f;
   auto attend = [&](DenseTile<D>& tile, int t) {
     const int r0 = first + t * 32;
     float s[8];
@@ -350,12 +352,13 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) { w[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += w[i]; }
-    v4i hi, lo;                                      // weights as a pair of 16-bit numbers: what is lost is below fp32's own rounding of the sum
+    // weights as a pair of 16-bit numbers (what is lost is below fp32's own rounding of the sum), or as twice the same half
+    v4i hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const uint32_t h = dense_pack<T>(w[2 * i], w[2 * i + 1]);
+      const uint32_t h = dense_pack<T>(w[2 * i] * part, w[2 * i + 1] * part), rest = dense_pack<T>(w[2 * i] - dense_low<T>(h), w[2 * i + 1] - dense_high<T>(h));
       hi[i] = (int)h;
-      lo[i] = (int)dense_pack<T>(w[2 * i] - dense_low<T>(h), w[2 * i + 1] - dense_high<T>(h));
+      lo[i] = (int)(fine ? rest : h);
     }
 #pragma unroll
     for (int j = 0; j < NJ; j++) {
@@ -367,19 +370,37 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
       o[j] = T::mfma16(a, lo, o[j]);
     }
   };
-  for (int t = wave; t < n_tiles; t += 32 * NW) {    // 32 tiles of the wave
-    look_up(t);
-    const int n = min(32, (n_tiles - t + NW - 1) / NW);
-    DenseTile<D> t0, t1;
-    load(t0, 0);
-    int i = 0;
-    for (; i + 1 < n; i += 2) {
-      load(t1, i + 1);
-      attend(t0, t + NW * i);
-      load(t0, min(i + 2, 31));                      // (past the end: the last rows once more)
-      attend(t1, t + NW * (i + 1));
+  auto stream = [&] {
+    for (int t = wave; t < n_tiles; t += 32 * NW) {  // 32 tiles of the wave
+      look_up(t);
+      const int n = min(32, (n_tiles - t + NW - 1) / NW);
+      DenseTile<D> t0, t1;
+      load(t0, 0);
+      int i = 0;
+      for (; i + 1 < n; i += 2) {
+        load(t1, i + 1);
+        attend(t0, t + NW * i);
+        load(t0, min(i + 2, 31));                    // (past the end: the last rows once more)
+        attend(t1, t + NW * (i + 1));
+      }
+      if (i < n) attend(t0, t + NW * i);
     }
-    if (i < n) attend(t0, t + NW * i);
+  };
+  // A value that is infinite meets the low part of its weight too, which may be 0 or less and makes it no number: where something
+  // is none, once more with the weights in two equal halves.
+#pragma unroll 1
+  for (;;) {
+    stream();
+    float zero = 0.f;                                // NaN where a value is infinite or none
+#pragma unroll
+    for (int j = 0; j < NJ; j++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) zero = fmaf(o[j][i], 0.f, zero);
+    if (!fine || !__ballot(zero != 0.f && c < G)) break;           // (columns without a head may hold anything)
+    fine = false; part = 0.5f;
+    m = -INFINITY; l = 0.f;
+#pragma unroll
+    for (int j = 0; j < NJ; j++) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
   }
   if (__ballot(bad) && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   l = quarters_sum(l);

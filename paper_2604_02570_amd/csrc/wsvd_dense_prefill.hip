@@ -385,12 +385,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
     // Something is no number: it may be a value that met a weight of 0.  All once more, carefully (results that should be no
     // numbers come out the same).
-    bool fine = true;
+    float zero = 0.f;                                // NaN where a value is infinite or none
 #pragma unroll
     for (int d = 0; d < ND; d++)
 #pragma unroll
-      for (int i = 0; i < 16; i++) fine = fine && __builtin_isfinite(o[d][i]);
-    if (__syncthreads_or(!fine)) {
+      for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
+    if (__syncthreads_or(zero != 0.f)) {
       m = -INFINITY; l = 0.f;
 #pragma unroll
       for (int d = 0; d < ND; d++)

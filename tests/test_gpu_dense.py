@@ -244,6 +244,32 @@ def test_decode_infinite_scores():
     L.close()
 
 
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f16")])
+def test_decode_infinite_values(d, dtype):
+    """Infinite values that are seen come out infinite, NaN comes out NaN, and only in their own dims; one head and several chunks."""
+    g = gen(4)
+    L = Layer(2, 4, 2, d, dtype)
+    pool = Pool(g, [1300, 20], 2, d, 16, dtype)
+    k, v = pool.rows(0)
+    v[17, 0, 3], v[900, 1, 5], v[1299, 1, 7], v[40, 0, 9] = math.inf, -math.inf, math.nan, math.inf
+    pool.put(0, 0, k, v)
+    k1, v1 = pool.rows(1)
+    v1[19, 0, 0] = -math.inf
+    pool.put(1, 0, k1, v1)
+    q = randn(g, dtype, 2, 4 * d)
+    cache, out = L.cache(pool), torch.empty(2, 4, d, dtype=DTYPES[dtype], device="cuda")
+    W.wsvd_dense_decode_attn_paged(L.ctx, L.desc, q.cuda(), 4 * d, cache, 1300, out)
+    got = out.cpu()
+    for b, (kk, vv) in enumerate(((k, v), (k1, v1))):
+        want, size = attend(q[b:b + 1].view(1, 4, d), kk, vv, [kk.shape[0] - 1], L.scale)
+        fine = torch.isfinite(want)
+        assert not fine.all() and torch.equal(torch.isnan(want[0]), torch.isnan(got[b]))
+        infinite = torch.isinf(want[0])
+        assert torch.equal(want[0][infinite], got[b][infinite].to(F64))
+        check(torch.where(fine[0], got[b], 0), torch.where(fine[0], want[0], 0), torch.where(fine[0], size[0], 0), dtype, True)
+    L.close()
+
+
 def test_decode_bad_page_is_reported():
     g = gen(2)
     L = Layer(1, 4, 2, 64, "bf16")
