@@ -84,7 +84,7 @@ struct DenseDecodeParams {
   uint16_t* out;
   DensePages pages;
   unsigned long long* parts;    // words {value, tag} [chunk][Hkv][G][d + 2]: maximum, sum, row
-  int B, Hkv, G, max_len, target, alone_units, min_units;
+  int B, Hkv, G, max_len, waves, target, alone_units, min_units;
   float c_scale;                // sm_scale * log2(e)
   int* err_word;
 };

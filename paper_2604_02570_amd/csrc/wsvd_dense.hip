@@ -164,69 +164,77 @@ WSVD_DEV unsigned long long dense_word(const unsigned long long* at) { return __
 WSVD_DEV void dense_clear(unsigned long long* at) { __hip_atomic_store(at, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // What a workgroup holds of its chunk, or of its group's chunks: by output e = head * D + dim, as many as a thread has.
-template <int D>
+template <int D, int NW>
 struct DensePartial {
-  static constexpr int N = 16 * D / (64 * kDenseWaves);
+  static constexpr int N = 16 * D / (64 * NW);
   float M[N], L[N], U[N];
 };
 
 // Takes the partial results of n < kDenseFold chunks, `step` apart from `chunk` on, in front of its own.
-template <int D>
-WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n, int kv, DensePartial<D>& own, float* sh /* [2][kDenseFold][16] */) {
-  constexpr int NF = kDenseFold - 1;
+template <int D, int NW>
+WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n, int kv, DensePartial<D, NW>& own, float* sh /* [2][kDenseFold][16] */) {
+  constexpr int N = DensePartial<D, NW>::N, AT_ONCE = N < 4 ? N : 4, NF = kDenseFold - 1;
+  static_assert(NF * 16 <= 64 * NW, "a thread for every chunk's maxima");
   const int tid = threadIdx.x, G = p.G;
   unsigned long long* const part = dense_part(p, chunk, kv, D);
   const size_t stride = (size_t)step * p.Hkv * G * (D + 2);
   float *m_sh = sh, *l_sh = sh + kDenseFold * 16;
-  // All words of a thread are asked for at once, and again until all have come: its outputs' rows, and for n * G threads a chunk's
-  // maximum and sum.  (One output after the other: 8 us more for 60 chunks of 16 heads of 128.)
-  const bool has = tid < n * G;
+  // All words of a thread are asked for at once, and again until all have come: its outputs' rows (four outputs at a time), and for
+  // n * G threads a chunk's maximum and sum.  (One output after the other: 8 us more for 60 chunks of 16 heads of 128.)
+  bool has = tid < n * G, came = true;
   const int mk = has ? tid / G : 0, mg = has ? tid - mk * G : 0;
-  unsigned long long* const ml = part + mk * stride + mg * (D + 2);
   const unsigned long long none = split_word(0.f);
-  unsigned long long w[DensePartial<D>::N][NF], wm = none, wl = none;
-  bool came = false;
-  for (int budget = 1 << 14; budget && !came; budget--) {
-    if (has) { wm = dense_word(ml); wl = dense_word(ml + 1); }
 #pragma unroll
-    for (int i = 0; i < DensePartial<D>::N; i++) {
-      const uint32_t e = tid + i * 64 * kDenseWaves, off = e / D * (D + 2) + 2 + e % D;
+  for (int i0 = 0; i0 < N; i0 += AT_ONCE) {
+    if (i0 > 0 && i0 * 64 * NW >= G * D) break;
+    unsigned long long* const ml = part + mk * stride + mg * (D + 2);
+    unsigned long long w[AT_ONCE][NF], wm = none, wl = none;
+    bool all = false;
+    for (int budget = 1 << 14; budget && !all; budget--) {
+      if (i0 == 0 && has) { wm = dense_word(ml); wl = dense_word(ml + 1); }
 #pragma unroll
-      for (int k = 0; k < NF; k++) w[i][k] = k < n && (int)e < G * D ? dense_word(part + k * stride + off) : none;
+      for (int i = 0; i < AT_ONCE; i++) {
+        const uint32_t e = tid + (i0 + i) * 64 * NW, off = e / D * (D + 2) + 2 + e % D;
+#pragma unroll
+        for (int k = 0; k < NF; k++) w[i][k] = k < n && (int)e < G * D ? dense_word(part + k * stride + off) : none;
+      }
+      all = (uint32_t)(wm >> 32) == kSplitTag && (uint32_t)(wl >> 32) == kSplitTag;
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; i++)
+#pragma unroll
+        for (int k = 0; k < NF; k++) all = all && (uint32_t)(w[i][k] >> 32) == kSplitTag;
+      if (!all) __builtin_amdgcn_s_sleep(1);
     }
-    came = (uint32_t)(wm >> 32) == kSplitTag && (uint32_t)(wl >> 32) == kSplitTag;
+    came = came && all;
+    if (i0 == 0) {
+      if (has) {
+        m_sh[mk * 16 + mg] = __uint_as_float((uint32_t)wm);
+        l_sh[mk * 16 + mg] = __uint_as_float((uint32_t)wl);
+        dense_clear(ml);
+        dense_clear(ml + 1);
+      }
+      __syncthreads();
+    }
 #pragma unroll
-    for (int i = 0; i < DensePartial<D>::N; i++)
+    for (int i = 0; i < AT_ONCE; i++) {
+      const int e = tid + (i0 + i) * 64 * NW, g = e / D;
+      if (e < G * D) {
+        const uint32_t off = g * (D + 2) + 2 + e % D;
+        float M = own.M[i0 + i], L = 0.f, U = 0.f;
+        for (int k = 0; k < n; k++) M = fmaxf(M, m_sh[k * 16 + g]);
 #pragma unroll
-      for (int k = 0; k < NF; k++) came = came && (uint32_t)(w[i][k] >> 32) == kSplitTag;
-    if (!came) __builtin_amdgcn_s_sleep(1);
-  }
-  if (has) {
-    m_sh[mk * 16 + mg] = __uint_as_float((uint32_t)wm);
-    l_sh[mk * 16 + mg] = __uint_as_float((uint32_t)wl);
-    dense_clear(ml);
-    dense_clear(ml + 1);
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < DensePartial<D>::N; i++) {
-    const int e = tid + i * 64 * kDenseWaves, g = e / D;
-    if (e < G * D) {
-      const uint32_t off = g * (D + 2) + 2 + e % D;
-      float M = own.M[i], L = 0.f, U = 0.f;
-      for (int k = 0; k < n; k++) M = fmaxf(M, m_sh[k * 16 + g]);
-#pragma unroll
-      for (int k = 0; k < NF; k++)
-        if (k < n) {
-          const float m = m_sh[k * 16 + g], f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);  // (nothing seen: l and u are 0, or NaN)
-          L += l_sh[k * 16 + g] * f;
-          U += __uint_as_float((uint32_t)w[i][k]) * f;
-          dense_clear(part + k * stride + off);
-        }
-      const float f = own.M[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(own.M[i] - M);
-      own.L[i] = L + own.L[i] * f;
-      own.U[i] = U + own.U[i] * f;
-      own.M[i] = M;
+        for (int k = 0; k < NF; k++)
+          if (k < n) {
+            const float m = m_sh[k * 16 + g], f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);  // (nothing seen: l and u are 0, or NaN)
+            L += l_sh[k * 16 + g] * f;
+            U += __uint_as_float((uint32_t)w[i][k]) * f;
+            dense_clear(part + k * stride + off);
+          }
+        const float f = own.M[i0 + i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(own.M[i0 + i] - M);
+        own.L[i0 + i] = L + own.L[i0 + i] * f;
+        own.U[i0 + i] = U + own.U[i0 + i] * f;
+        own.M[i0 + i] = M;
+      }
     }
   }
   if (!came) atomicExch(p.err_word, (int)WSVD_E_HIP);              // never seen; keeps the wait finite
@@ -241,9 +249,9 @@ struct DenseTile {
 };
 
 // ONCE: the rows are asked for as data that is read once and need not stay in the caches.
-template <class T, int D, bool ONCE>
-__global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode(DenseDecodeParams p) {
-  constexpr int NK = D / 32, NJ = D / 16, NW = kDenseWaves;
+template <class T, int D, int NW, bool ONCE>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode(DenseDecodeParams p) {
+  constexpr int NK = D / 32, NJ = D / 16;
   extern __shared__ __attribute__((aligned(256))) float o_sh[];      // a granule pair's keys for each wave; at the end [NW][G][D]
   __shared__ float m_sh[NW][16], l_sh[NW][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -413,9 +421,9 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
       for (int i = 0; i < 4; i++) o_sh[(wave * G + c) * D + NJ * (4 * qd + i) + j] = o[j][i];
   }
   __syncthreads();
-  DensePartial<D> r;
+  DensePartial<D, NW> r;
 #pragma unroll
-  for (int i = 0; i < DensePartial<D>::N; i++) {
+  for (int i = 0; i < DensePartial<D, NW>::N; i++) {
     const int e = threadIdx.x + i * 64 * NW, g = e / D, x = e % D;
     r.M[i] = -INFINITY; r.L[i] = r.U[i] = 0.f;
     if (e < G * D) {
@@ -436,12 +444,12 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
     const int folds = !ends ? 0 : last && n_groups > 1 ? 2 : 1;
 #pragma unroll 1
     for (int i = 0; i < folds; i++)                  // the group's chunks, then the groups' results
-      dense_fold<D>(p, i == 0 ? c0 + group * kDenseFold : c0 + kDenseFold - 1, i == 0 ? 1 : kDenseFold,
+      dense_fold<D, NW>(p, i == 0 ? c0 + group * kDenseFold : c0 + kDenseFold - 1, i == 0 ? 1 : kDenseFold,
                     i == 0 ? at.chunk % kDenseFold : n_groups - 1, kv, r, o_sh);
     if (!last) {
       unsigned long long* const part = dense_part(p, idx, kv, D);
 #pragma unroll
-      for (int i = 0; i < DensePartial<D>::N; i++) {
+      for (int i = 0; i < DensePartial<D, NW>::N; i++) {
         const int e = threadIdx.x + i * 64 * NW, g = e / D, x = e % D;
         if (e < G * D) {
           dense_push(part + g * (D + 2) + 2 + x, r.U[i]);
@@ -452,7 +460,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) __attribute__((amdgpu_waves_per_e
     }
   }
 #pragma unroll
-  for (int i = 0; i < DensePartial<D>::N; i++) {
+  for (int i = 0; i < DensePartial<D, NW>::N; i++) {
     const int e = threadIdx.x + i * 64 * NW;
     if (e < G * D) p.out[((int64_t)at.b * p.Hkv * G + kv * G) * D + e] = (uint16_t)dense_pack<T>(r.L[i] == 0.f ? 0.f : r.U[i] / r.L[i], 0.f);
   }
@@ -475,16 +483,20 @@ hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
   if (p.n_tokens < 2048 || items >= 256) return launch_append_form<T, D, 1>(p, s);
   return items >= 128 ? launch_append_form<T, D, 2>(p, s) : launch_append_form<T, D, 4>(p, s);
 }
-template <class T, int D, bool ONCE>
+template <class T, int D, int NW, bool ONCE>
 hipError_t launch_decode_form(const DenseDecodeParams& p, hipStream_t s) {
-  const int lds = kDenseWaves * D * 4 * 16;          // 32 keys a wave, and later 16 rows of fp32
+  constexpr int LDS = NW * D * 4 * 16;               // 32 keys a wave, and later 16 rows of fp32
   static LdsLimit limit;
-  if (lds + kDenseWaves * 16 * 8 > 65536) {
-    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode<T, D, ONCE>, lds);
+  if (LDS + NW * 16 * 8 > 65536) {
+    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode<T, D, NW, ONCE>, LDS);
     if (e != hipSuccess) return e;
   }
-  k_dense_decode<T, D, ONCE><<<(p.target + p.B) * p.Hkv, 64 * kDenseWaves, lds, s>>>(p);
+  k_dense_decode<T, D, NW, ONCE><<<(p.target + p.B) * p.Hkv, 64 * NW, LDS, s>>>(p);
   return hipGetLastError();
+}
+template <class T, int D, bool ONCE>
+hipError_t launch_decode_waves(const DenseDecodeParams& p, hipStream_t s) {
+  return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE>(p, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE>(p, s) : launch_decode_form<T, D, 2, ONCE>(p, s);
 }
 template <class T, int D>
 hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
@@ -492,7 +504,7 @@ hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
   // does is slower: 32 x 8192 rows of 4 heads (537 MB) 100 us against 90, 8 x 1000 of 32 (131 MB) 27.8 against 25.3; 74 MB over and
   // over out of that cache 17.9 against 20.
   const bool once = (int64_t)p.B * p.max_len * p.Hkv * D * 4 >= 100000000;
-  return once ? launch_decode_form<T, D, true>(p, s) : launch_decode_form<T, D, false>(p, s);
+  return once ? launch_decode_waves<T, D, true>(p, s) : launch_decode_waves<T, D, false>(p, s);
 }
 
 }  // namespace

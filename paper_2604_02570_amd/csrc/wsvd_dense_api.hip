@@ -59,7 +59,7 @@ extern "C" {
 wsvd_status wsvd_dense_workspace_bytes(const wsvd_dense_desc* desc, size_t* bytes) {
   if (!bytes) return WSVD_E_NULL;
   WSVD_TRY(check_desc(desc));
-  const size_t chunks = (size_t)dense_target(desc->n_kv_heads) + desc->batch;
+  const size_t chunks = (size_t)dense_target(dense_waves(desc->batch, desc->n_kv_heads, 0), desc->n_kv_heads) + desc->batch;
   const size_t decode = chunks * desc->n_q_heads * (desc->d_head + 2) * 8, prompt = (size_t)kDensePromptParts * kDensePromptRows * (desc->d_head + 2) * 4;
   *bytes = (size_t)kWsCounterInts * 4 + (decode > prompt ? decode : prompt);
   return WSVD_OK;
@@ -109,7 +109,8 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   p.q = (const uint16_t*)q; p.q_ld = q_ld; p.out = (uint16_t*)out; p.pages = pages_of(cache);
   p.parts = (unsigned long long*)((int*)ctx->ws + kWsCounterInts);
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads;
-  p.max_len = max_seq_len; p.target = dense_target(p.Hkv);
+  p.max_len = max_seq_len; p.waves = dense_waves(p.B, p.Hkv, max_seq_len);
+  p.target = dense_target(p.waves, p.Hkv);
   // (in rows twice as many at half the row length; the min_chunk setting, where given, is taken for both)
   p.alone_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : 5 * 128 / desc->d_head;
   p.min_units = ctx->opt.min_chunk ? p.alone_units : 2 * 128 / desc->d_head;

@@ -83,7 +83,7 @@ WSVD_DEV float no_tag(float v) {
 }
 
 template <class T, int D, bool PAGED, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_prompt(DensePromptParams p) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3))) void k_dense_prompt(DensePromptParams p) {
   constexpr int ROWS = 32 * NW;                      // query rows of a workgroup
   constexpr int PIECES = D / 8, RPI = 64 / PIECES;   // 16-byte pieces of a row; rows that one copy of a wave brings
   constexpr int COPIES = kKeys / NW / RPI;

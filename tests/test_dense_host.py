@@ -120,7 +120,7 @@ def test_prompts_refuse(ctx):
 
 def test_workspace_holds_what_the_kernels_put_there():
     for batch, hq, hkv, d in ((1, 8, 8, 64), (1, 16, 1, 128), (32, 28, 4, 128), (4096, 32, 8, 128), (3, 1024, 1024, 64)):
-        target = max(1, 256 // hkv)
+        target = max(1, (1024 if batch * hkv >= 1024 else 512 if batch * hkv >= 512 else 256) // hkv)
         need = W.wsvd_dense_workspace_bytes(desc(batch=batch, n_q_heads=hq, n_kv_heads=hkv, d_head=d)) - 65536
         assert need >= (target + batch) * hq * (d + 2) * 8          # one word per value of every chunk
         assert need >= 512 * 128 * (d + 2) * 4                      # 512 parts of 128 rows
@@ -155,7 +155,8 @@ int main() {
   // chunks of the decode attention
   std::srand(7);
   for (int round = 0; round < 40000; round++) {
-    const int Hkv = 1 << (std::rand() % 11), target = dense_target(Hkv), B = 1 + std::rand() % (round % 3 ? 70 : 700);
+    const int Hkv = 1 << (std::rand() % 11), B = 1 + std::rand() % (round % 3 ? 70 : 700), target = dense_target(dense_waves(B, Hkv, round % 2 ? 1000 : 5000), Hkv);
+    CHECK(target <= dense_target(dense_waves(B, Hkv, 0), Hkv));          // the workspace's
     const int alone = 1 + std::rand() % 12, least = 1 + std::rand() % 6;
     std::vector<int> u(B);
     int total = 0, most = 0;

@@ -200,6 +200,13 @@ def test_decode_more_than_64_sequences():
     decode_case(4, 2, 64, "bf16", [(97 * i) % 401 for i in range(150)], 16, max_pages=32)
 
 
+@pytest.mark.parametrize("batch,hq,hkv,d", [(70, 8, 8, 64), (64, 16, 8, 128), (150, 8, 8, 64), (33, 64, 32, 128), (9, 128, 128, 64)])
+def test_decode_many_units(batch, hq, hkv, d):
+    """Two and four waves a workgroup (eight where a sequence is longer); one sequence is long enough to be cut all the same."""
+    decode_case(hq, hkv, d, "bf16", [(61 * i) % 150 for i in range(batch - 1)] + [1023], 64, max_pages=65)
+    decode_case(hq, hkv, d, "bf16", [(61 * i) % 50 for i in range(batch - 1)] + [4100], 64, max_pages=65)
+
+
 def test_decode_strides_and_scale():
     decode_case(6, 2, 128, "f16", [300, 40], 32, ld_extra=40, scale=0.25)
 
