@@ -495,7 +495,8 @@ typedef struct {
   float sm_scale;  /* softmax scale; 0 means 1/sqrt(d_head) */
 } wsvd_dense_desc;
 
-/* Scratch of wsvd_dense_decode_attn_paged (HOST output); a context's workspace may serve latent and dense layers in turn. */
+/* Scratch of the three dense attention calls (HOST output; tens of MB, most of it for prompts of few tiles, whose keys several
+ * workgroups share); without it they return WSVD_E_WORKSPACE.  A context's workspace may serve latent and dense layers in turn. */
 wsvd_status wsvd_dense_workspace_bytes(const wsvd_dense_desc *desc, size_t *bytes);
 
 /*
@@ -522,7 +523,7 @@ wsvd_status wsvd_dense_append_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, 
  * (as does a row whose scores are all -inf).  q [batch][q_ld], out [batch][n_q_heads][d_head] of dtype.  The rows of all
  * sequences are divided over the chip by the lengths found on the device and joined in a fixed order, so the result does
  * not depend on timing; max_seq_len is a HOST upper bound, at most max_pages * page_rows (a longer sequence records
- * WSVD_E_SHAPE and is attended over its first max_seq_len rows).
+ * WSVD_E_SHAPE and is attended over its first max_seq_len rows).  The min_chunk setting of the context applies.
  */
 wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld,
                                          const wsvd_paged_cache *cache, int32_t max_seq_len, void *out, void *hip_stream);

@@ -268,7 +268,9 @@ WSVD_DEV size_t a_packed_offset(int kv, int j, int e, int rank, int d_model) {
 // [0, kWsCounterInts*4): counters (zeroed by wsvd_set_workspace, self-resetting); then the attention's split words and the
 // append's pushed words (8-byte {value, tag} words, cleared by their consumer: zero between launches); then the fp32
 // partial sums of the sliced append kernels, which the decode step's projection launch uses for its slices too (followed
-// by its one pending word per sequence); no invariant there: written before read.
+// by its one pending word per sequence); no invariant there: written before read.  The dense layers' calls use the area behind the
+// counters as well: the decode attention for words of the same kind and tag, cleared by their consumer, the prompt attention for
+// plain partial results, none of which has the bits of a tag.
 // ints [0, batch) of [0, 8192): per sequence, workgroups that have read its length (one-launch decode steps) or have finished
 // (the store-and-attend launch), zero between launches; [8192, 12288): append tickets; [12288, 16000): fused-step row flags
 // (2*Hkv, hold the epoch of the last step); [16000]: fused-step finished-workgroup counter.

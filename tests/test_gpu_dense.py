@@ -154,13 +154,12 @@ def test_append_bad_rows_and_pages_store_nothing():
 
 
 # ------------------------------------------------------------------------------------------------ decode
-def decode_case(hq, hkv, d, dtype, lens, page_rows, *, max_len=None, scale=0.0, ld_extra=0, q_scale=1.0, max_pages=None, tweak=None, status=0):
+def decode_case(hq, hkv, d, dtype, lens, page_rows, *, max_len=None, scale=0.0, ld_extra=0, q_scale=1.0, max_pages=None, min_chunk=0, status=0):
     g = gen(11 + hq + d + sum(lens))
     L = Layer(len(lens), hq, hkv, d, dtype, scale)
+    W.wsvd_ctx_set_option(L.ctx, "min_chunk", min_chunk)
     pool = Pool(g, lens, hkv, d, page_rows, dtype, max_pages=max_pages)
     q = randn(g, dtype, len(lens), hq * d + ld_extra, scale=q_scale)
-    if tweak:
-        tweak(pool, q)
     cache = L.cache(pool)
     out = torch.full((len(lens), hq, d), math.nan, dtype=DTYPES[dtype], device="cuda")
     qd = q.cuda()
@@ -198,6 +197,13 @@ def test_decode_one_long_sequence(d, dtype):
 
 def test_decode_more_than_64_sequences():
     decode_case(4, 2, 64, "bf16", [(97 * i) % 401 for i in range(150)], 16, max_pages=32)
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(4, 4, 64, "bf16"), (16, 1, 128, "f16"), (7, 1, 128, "bf16")])
+def test_decode_small_chunks(hq, hkv, d, dtype):
+    """Chunks of 128 rows: one or two folds, groups that end in the middle, empty last chunks."""
+    decode_case(hq, hkv, d, dtype, [1, 129, 1024, 1025, 0, 2200, 7 * 128 + 1], 16, min_chunk=128)
+    decode_case(hq, hkv, d, dtype, [8300], 32, min_chunk=128)
 
 
 @pytest.mark.parametrize("batch,hq,hkv,d", [(70, 8, 8, 64), (64, 16, 8, 128), (150, 8, 8, 64), (33, 64, 32, 128), (9, 128, 128, 64)])
