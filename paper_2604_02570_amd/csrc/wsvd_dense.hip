@@ -395,13 +395,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       DenseTile<D> t0, t1;
       load(t0, 0);
       int i = 0;
-      for (; i + 1 < n; i += 2) {
+      for (; i + 2 < n; i += 2) {
         load(t1, i + 1);
         attend(t0, t + NW * i);
-        load(t0, min(i + 2, 31));                    // (past the end: the last rows once more)
+        load(t0, i + 2);
         attend(t1, t + NW * (i + 1));
       }
-      if (i < n) attend(t0, t + NW * i);
+      if (i + 1 < n) load(t1, i + 1);
+      attend(t0, t + NW * i);
+      if (i + 1 < n) attend(t1, t + NW * (i + 1));
     }
   };
   // A value that is infinite meets the low part of its weight too, which may be 0 or less and makes it no number: where something
