@@ -421,23 +421,22 @@ def wsvd_timeline_set_buffer(ctx, buf):
 
 
 # Dense layers.  A call on a few tokens is over on the GPU before the next one is marshalled, so these wrappers hand ctypes plain
-# addresses and integers (sizes have to be Python ints) and look nothing up twice: 3.1 us of host time for the append's 18
-# arguments, 4.0 the way of the wrappers above.
+# addresses, Python ints and the structures themselves, and look nothing up twice: 2.4 us of host time for the append's 18 arguments,
+# 4.0 the way of the wrappers above.
 def dense_desc(batch, n_q_heads, n_kv_heads, d_head, dtype, sm_scale=0.0) -> DenseDesc:
     return DenseDesc(batch, n_q_heads, n_kv_heads, d_head, DTYPES[dtype] if isinstance(dtype, str) else int(dtype), float(sm_scale))
 
 
-def _addr(t):
-    return t if t is None or isinstance(t, int) else t.data_ptr()
+def _addresses(*args):
+    """Tensors as their addresses, everything else (addresses given as ints among it) as it is."""
+    return [a.data_ptr() if hasattr(a, "data_ptr") else a for a in args]
 
 
 def _stream_addr(stream):
-    if isinstance(stream, int):
-        return stream
     if stream is None:
         import torch
         stream = torch.cuda.current_stream()
-    return stream.cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def wsvd_dense_workspace_bytes(desc):
@@ -448,29 +447,45 @@ def wsvd_dense_workspace_bytes(desc):
 
 def wsvd_dense_append_paged(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_tokens, cu_tokens, positions, inv_freq, q_out, q_out_ld, k_out, k_out_ld,
                             cache, stream=None):
-    status = (_lib or lib()).wsvd_dense_append_paged(ctx, byref(desc), _addr(q), q_ld, _addr(k), k_ld, _addr(v), v_ld, n_tokens,
-                                                     _addr(cu_tokens), _addr(positions), _addr(inv_freq), _addr(q_out), q_out_ld,
-                                                     _addr(k_out), k_out_ld, byref(cache), _stream_addr(stream))
+    call, on = (_lib or lib()).wsvd_dense_append_paged, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, desc, None if q is None else q.data_ptr(), q_ld, k.data_ptr(), k_ld, v.data_ptr(), v_ld, n_tokens,
+                      None if cu_tokens is None else cu_tokens.data_ptr(), None if positions is None else positions.data_ptr(),
+                      None if inv_freq is None else inv_freq.data_ptr(), None if q_out is None else q_out.data_ptr(), q_out_ld,
+                      None if k_out is None else k_out.data_ptr(), k_out_ld, cache, on)
+    except AttributeError:                                             # addresses in place of tensors
+        status = call(*_addresses(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_tokens, cu_tokens, positions, inv_freq, q_out, q_out_ld, k_out,
+                                  k_out_ld, cache, on))
     if status:
         raise WsvdError(status, "wsvd_dense_append_paged")
 
 
 def wsvd_dense_decode_attn_paged(ctx, desc, q, q_ld, cache, max_seq_len, out, stream=None):
-    status = (_lib or lib()).wsvd_dense_decode_attn_paged(ctx, byref(desc), _addr(q), q_ld, byref(cache), max_seq_len, _addr(out),
-                                                          _stream_addr(stream))
+    call, on = (_lib or lib()).wsvd_dense_decode_attn_paged, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, desc, q.data_ptr(), q_ld, cache, max_seq_len, out.data_ptr(), on)
+    except AttributeError:
+        status = call(*_addresses(ctx, desc, q, q_ld, cache, max_seq_len, out, on))
     if status:
         raise WsvdError(status, "wsvd_dense_decode_attn_paged")
 
 
 def wsvd_dense_prefill_attn(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_q, n_kv, cu_q, cu_kv, causal, out, out_ld, stream=None):
-    status = (_lib or lib()).wsvd_dense_prefill_attn(ctx, byref(desc), _addr(q), q_ld, _addr(k), k_ld, _addr(v), v_ld, n_q, n_kv,
-                                                     _addr(cu_q), _addr(cu_kv), causal, _addr(out), out_ld, _stream_addr(stream))
+    call, on = (_lib or lib()).wsvd_dense_prefill_attn, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, desc, q.data_ptr(), q_ld, k.data_ptr(), k_ld, v.data_ptr(), v_ld, n_q, n_kv, cu_q.data_ptr(),
+                      None if cu_kv is None else cu_kv.data_ptr(), causal, out.data_ptr(), out_ld, on)
+    except AttributeError:
+        status = call(*_addresses(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_q, n_kv, cu_q, cu_kv, causal, out, out_ld, on))
     if status:
         raise WsvdError(status, "wsvd_dense_prefill_attn")
 
 
 def wsvd_dense_prefill_attn_paged(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, stream=None):
-    status = (_lib or lib()).wsvd_dense_prefill_attn_paged(ctx, byref(desc), _addr(q), q_ld, n_q, _addr(cu_q), byref(cache), _addr(out),
-                                                           out_ld, _stream_addr(stream))
+    call, on = (_lib or lib()).wsvd_dense_prefill_attn_paged, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, desc, q.data_ptr(), q_ld, n_q, cu_q.data_ptr(), cache, out.data_ptr(), out_ld, on)
+    except AttributeError:
+        status = call(*_addresses(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, on))
     if status:
         raise WsvdError(status, "wsvd_dense_prefill_attn_paged")
