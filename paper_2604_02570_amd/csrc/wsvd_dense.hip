@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void k_dense_append(DenseAppendParams p) {
 // head and 4 of 16 rows; its 8 weights of 32 rows are, as they lie, its part of the second product's operand (the contraction over
 // rows may run in any order, V is taken in that one).  V's operand is made in registers: a lane loads 8 rows' same dims in whole
 // lines and pairs them up with one byte permute per two elements.
-// Bound: HBM.  32 x 8192 rows of 4 heads of 128 (537 MB): 89.5 us, 6.0 TB/s (a kernel that only reads them: 81 us); 640 rows of 32
+// Bound: HBM.  32 x 8192 rows of 4 heads of 128 (537 MB): 86.6 us, 6.2 TB/s (a kernel that only reads them: 81 us); 640 rows of 32
 // heads (10.5 MB): 7.7 us, of which 3.3 are a launch that finds no row, and the rest a CU's stream of 74 GB/s.
 // A workgroup's place: sequence, chunk of it, chunks it has, its length, the rows of a chunk; false for a workgroup that has none.
 struct DensePlace { int b, chunk, n_chunks, len, rows; };
