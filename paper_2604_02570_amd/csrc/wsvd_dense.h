@@ -95,7 +95,7 @@ struct DensePromptParams {
   const int *cu_q, *cu_kv;
   DensePages pages;
   float* parts;                 // of tiles that several workgroups share: [tile][Hkv][split] of 128 x {maximum, sum}, 128 rows
-  int B, Hkv, G, causal, n_q, n_kv, splits;
+  int B, Hkv, G, causal, n_q, n_kv, splits, pairs;
   float c_scale;
   int* err_word;
 };

@@ -12,12 +12,12 @@
 //
 // A workgroup is 4 waves of 32 query rows; two workgroups share a CU, so that one multiplies while the other starts, waits or ends.
 // Blocks of 64 keys go straight from memory to LDS, two stages deep.  A wave runs one block's softmax under the next block's score
-// products and the next block's maximum under this one's value products; what it costs is then
+// products and its own first value products, and the next block's maximum under the other value products; what it costs is then
 //   * matrix products: 1024 cycles per block and wave at d 128 (56 % of the time at 8192 tokens, all heads),
-//   * vector instructions: 123 and 32 exponentials, about as long,
+//   * vector instructions: about 120 and 32 exponentials, about as long, spread evenly over the products,
 //   * power: at full load the chip runs at 1.9 GHz instead of 2.4 (the same call on zeros takes 0.84 of the time).
-// 1 x 8192 tokens, 32 heads of 128: 1.17 PFLOP/s without a mask, 1.11 causal (products of 16384^2 matrices: 1.33); 16 x 2048 tokens:
-// 0.88, with 1.07 GB of queries, keys, values and outputs.  d 64: 0.93.
+// 1 x 8192 tokens, 32 heads of 128: 1.17 PFLOP/s without a mask, 1.08 causal (products of 16384^2 matrices: 1.37); 16 x 2048 tokens:
+// 0.91, with 1.07 GB of queries, keys, values and outputs.  d 64: 0.93.
 // Tried and not faster: 8 waves to a workgroup (0.86 where 4 have 0.90 at 16 x 2048); 64 rows a wave, one wave a SIMD (0.71: the
 // accumulators no longer fit the vector registers); the weights' sum by the matrix cores; the longest tiles of all sequences first
 // (16 x 2048: 0.57, keys and values no longer stay in the L2); lines of later blocks fetched to the L2 ahead.
@@ -40,14 +40,32 @@ WSVD_DEV void copy16(uint32_t lds, const uint8_t* base, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
-// A workgroup's sequence and tile (a sequence's last tiles, which see the most keys, first), from one read of the lengths, and what
-// that tile sees.
+// The same number, as one that the compiler knows nothing of: what is made of it is made where it is needed, and not kept in a register
+// over the loops between.
+WSVD_DEV int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+WSVD_DEV int anew_scalar(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
+// A workgroup's sequence and tile (a sequence's last tiles, which see the most keys, first), from one read of the lengths.  Where
+// workgroups take two tiles (p.pairs), the second is as far from the sequence's first as the first is from its last, so that all
+// pairs of a sequence cost the same; the tile in the middle of an odd number stays alone.
 struct PromptPlace {
   int b, q_start, nq, kv_start, nk;
-  int row0;                                          // first of the tile's query rows
-  int ahead, seen;                                   // query token i sees the keys up to i + ahead; keys that the tile's last row sees
-  int n_blocks, splits;                              // blocks of them, and workgroups that share them
+  int tile, second;                                  // second: -1 where there is none
+  int ahead;                                         // query token i sees the keys up to i + ahead
+  int splits;                                        // workgroups that share the tile's keys
 };
+// blocks of keys that a tile's last row sees
+template <int ROWS>
+WSVD_DEV int prompt_blocks(const DensePromptParams& p, const PromptPlace& at, int tile) {
+  const int seen = p.causal ? min(at.nk, (min((tile + 1) * ROWS, at.nq * p.G) - 1) / p.G + at.ahead + 1) : at.nk;
+  return seen > 0 ? (seen + kKeys - 1) / kKeys : 0;
+}
 template <bool PAGED, int ROWS>
 WSVD_DEV bool prompt_place(const DensePromptParams& p, int idx, int lane, PromptPlace& at) {
   const int most = PAGED ? p.pages.max_pages * p.pages.page_rows : p.n_kv;
@@ -66,13 +84,15 @@ WSVD_DEV bool prompt_place(const DensePromptParams& p, int idx, int lane, Prompt
       qs = min(max(q0, 0), p.n_q);
       n_q = min(max(q1, qs), p.n_q) - qs;
     }
-    const int k = (n_q * p.G + ROWS - 1) / ROWS, end = before + wave_prefix_int(k);
+    const int tiles = (n_q * p.G + ROWS - 1) / ROWS, k = p.pairs ? (tiles + 1) / 2 : tiles, end = before + wave_prefix_int(k);
     const unsigned long long m = __ballot(end > idx);
     before = __builtin_amdgcn_readlane(end, 63);
     if (!m) continue;
     const int l = __builtin_ctzll(m);
     at.b = base + l;
-    at.row0 = (__builtin_amdgcn_readlane(end, l) - 1 - idx) * ROWS;
+    const int from_end = idx - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(k, l));
+    at.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - from_end;
+    at.second = p.pairs && from_end < at.tile ? from_end : -1;
     at.q_start = __builtin_amdgcn_readlane(qs, l); at.nq = __builtin_amdgcn_readlane(n_q, l);
     at.kv_start = __builtin_amdgcn_readlane(ks, l); at.nk = __builtin_amdgcn_readlane(n_k, l);
     if (PAGED) {
@@ -80,9 +100,7 @@ WSVD_DEV bool prompt_place(const DensePromptParams& p, int idx, int lane, Prompt
       at.nk = min(max(at.nk, 0), most);
     }
     at.ahead = at.nk - at.nq;
-    at.seen = p.causal ? min(at.nk, (min(at.row0 + ROWS, at.nq * p.G) - 1) / p.G + at.ahead + 1) : at.nk;
-    at.n_blocks = at.seen > 0 ? (at.seen + kKeys - 1) / kKeys : 0;
-    at.splits = max(1, min(p.splits, at.n_blocks / kLeastBlocks));
+    at.splits = max(1, min(p.splits, prompt_blocks<ROWS>(p, at, at.tile) / kLeastBlocks));
     return true;
   }
   return false;
@@ -104,33 +122,33 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   constexpr int ROW_BYTES = 2 * D, PLANE = kKeys * ROW_BYTES, STAGE = 2 * PLANE;
   constexpr int ND = D / 32, NS = D / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
+  __shared__ int odd_sh[NW];                         // a wave's results that are no numbers
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, half = lane >> 5;
   const int kv = blockIdx.x % p.Hkv, split = blockIdx.x / p.Hkv % p.splits, idx = blockIdx.x / p.Hkv / p.splits;
   PromptPlace at;
   if (!prompt_place<PAGED, ROWS>(p, idx, lane, at) || split >= at.splits) return;
   // A workgroup of several for a tile has a part of the tile's blocks: key0 on, everything below counts from there.
-  const int block0 = dense_share(split, at.n_blocks, at.splits), n_blocks = dense_share(split + 1, at.n_blocks, at.splits) - block0, key0 = block0 * kKeys;
-  const int b = at.b, q_start = at.q_start, NR = at.nq * p.G, row0 = at.row0, ahead = at.ahead - key0;
-  const int nk = at.nk - key0, here = min(nk, n_blocks * kKeys);
-  // a wave's 32 rows: the keys that its last one sees, and those that all of them see
-  const int wrow = row0 + 32 * wave, wlast = min(wrow + 31, NR - 1);
-  const int wseen = wrow >= NR ? 0 : p.causal ? min(here, wlast / p.G + ahead + 1) : here;
-  const int wall = p.causal ? wrow / p.G + ahead + 1 : here;
-
-  // this lane's query: operand of the score product, and the last key it sees
-  const int row = min(wrow + n, NR - 1), tok = row / p.G, head = kv * p.G + row - tok * p.G;
-  const int limit = p.causal ? tok + ahead : nk - 1;
+  int tile = at.tile, n_blocks = prompt_blocks<ROWS>(p, at, tile);
+  const int block0 = dense_share(split, n_blocks, at.splits), key0 = block0 * kKeys;
+  n_blocks = dense_share(split + 1, n_blocks, at.splits) - block0;
+  const int b = at.b, q_start = at.q_start, NR = at.nq * p.G, ahead = at.ahead - key0, nk = at.nk - key0;
+  // this lane's query: operand of the score product
   v4i q[NS];
-  {
-    const uint16_t* qp = p.q + (int64_t)(q_start + tok) * p.q_ld + head * D + half * 8;
+  auto load_q = [&](int tile) {
+    const int i = anew(lane), row = min(tile * ROWS + 32 * wave + (i & 31), NR - 1), tok = row / p.G, head = kv * p.G + row - tok * p.G;
+    const uint16_t* qp = p.q + (int64_t)(q_start + tok) * p.q_ld + head * D + (i >> 5) * 8;
 #pragma unroll
     for (int s = 0; s < NS; s++) q[s] = *(const v4i*)(qp + s * 16);
-  }
+  };
+  load_q(tile);
 
   // staging: a wave's share of a block's rows, the 16-byte pieces of a row permuted so that the reads below meet no bank twice
   const uint32_t lds0 = lds_address(lds);
   const int my_row = lane / PIECES, my_piece = lane % PIECES;
+  static_assert(kKeys / NW == 16 && COPIES * RPI == 16, "");
+  const uint32_t k_stride = PAGED ? ROW_BYTES : (uint32_t)p.k_ld * 2u, v_stride = PAGED ? ROW_BYTES : (uint32_t)p.v_ld * 2u;
+  const uint32_t k_piece = (my_piece ^ (D == 128 ? my_row : my_row >> 1)) * 16, v_piece = (my_piece ^ (D == 128 ? my_row << 2 : (my_row & 2) << 1)) * 16;
   // Paged: a wave's rows of a block lie in one granule of 16.  Where they lie is looked up for 64 blocks at a time, a lane for each.
   static_assert(16 % (kKeys / NW) == 0, "");
   bool bad = false;
@@ -143,25 +161,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     const uint64_t bytes = dense_pool_row(page, granule, pg, kv, p.Hkv, p.pages.page_rows) * ROW_BYTES;
     at_low = (uint32_t)bytes; at_high = (uint32_t)(bytes >> 32);
   };
+  // (rows of a copy are a scalar's distance apart: what a lane adds is the same for every block)
   auto stage = [&](int kb, int buf, bool keys) {
-#pragma unroll
-    for (int i = 0; i < COPIES; i++) {
-      const int r0 = (wave * COPIES + i) * RPI, r = r0 + my_row;
-      const int sw = keys ? (D == 128 ? r & 15 : (r >> 1) & 7) : (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
-      const uint8_t* from;
-      uint32_t off;
-      if (PAGED) {
-        const int i = kb - looked_up;
-        from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) +
-               ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, i) << 32);
-        off = (uint32_t)((r & 15) * ROW_BYTES);
-      } else {
-        const int64_t ld = keys ? p.k_ld : p.v_ld;
-        from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)at.kv_start + key0 + kb * kKeys) * ld + kv * D);
-        off = (uint32_t)min(r, nk - 1 - kb * kKeys) * (uint32_t)ld * 2u;
-      }
-      copy16(lds0 + buf * STAGE + (keys ? 0 : PLANE) + r0 * ROW_BYTES, from, off + (my_piece ^ sw) * 16);
+    const uint32_t to = lds0 + buf * STAGE + (keys ? 0 : PLANE) + wave * (16 * ROW_BYTES);
+    const uint32_t stride = keys ? k_stride : v_stride;
+    if (!PAGED && (kb + 1) * kKeys > nk) {           // a block that ends before its last row: that one in the place of those behind it
+      const uint8_t* from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)at.kv_start + key0 + kb * kKeys) * (keys ? p.k_ld : p.v_ld) + kv * D);
+      const int row = wave * 16 + anew(my_row);
+#pragma unroll 1
+      for (int i = 0; i < COPIES; i++)               // (rarely: small rather than fast)
+        copy16(to + i * 1024, from, (uint32_t)min(row + i * RPI, nk - 1 - kb * kKeys) * stride + (keys ? k_piece ^ (i << 6) : v_piece));
+      return;
     }
+    const uint8_t* from;
+    if (PAGED) {
+      const int i = kb - looked_up;
+      from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) +
+             ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, i) << 32);
+    } else {
+      from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)at.kv_start + key0 + kb * kKeys + wave * 16) * (keys ? p.k_ld : p.v_ld) + kv * D);
+    }
+#pragma unroll
+    for (int i = 0; i < COPIES; i++)
+      copy16(to + i * 1024, from + (uint64_t)(i * RPI) * stride, my_row * stride + (keys ? k_piece ^ (i << 6) : v_piece));
   };
 
   // addresses of the operands in a stage
@@ -189,12 +211,16 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   };
 
   struct Scores { v16f s[2]; };
-  float m = -INFINITY, l = 0.f;
+  int limit = 0;                                     // the last key that this lane's query sees
+  float m, l[2];                                     // maximum; sums of every other weight
   v16f o[ND];
+  auto clear = [&] {
+    m = -INFINITY; l[0] = l[1] = 0.f;
 #pragma unroll
-  for (int d = 0; d < ND; d++)
+    for (int d = 0; d < ND; d++)
 #pragma unroll
-    for (int i = 0; i < 16; i++) o[d][i] = 0.f;
+      for (int i = 0; i < 16; i++) o[d][i] = 0.f;
+  };
 
   auto multiply = [&](Scores& r, uint32_t stage) {   // a block's scores
 #pragma unroll
@@ -206,12 +232,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
 #pragma unroll
       for (int h = 0; h < 2; h++) r.s[h] = T::mfma32(read_k(stage, h, x), q[x], r.s[h]);
   };
-  auto hide = [&](Scores& r, int kb) {               // keys that this lane's query does not see
-    const int rel = limit - kb * kKeys - 4 * half;
+  // keys that this lane's query does not see
+  auto last_seen = [&](int kb) { return limit - kb * kKeys - 4 * half; };
+  auto hide = [&](Scores& r, int at, int rel) { r.s[at >> 4][at & 15] = 32 * (at >> 4) + 8 * ((at & 15) >> 2) + (at & 3) > rel ? -INFINITY : r.s[at >> 4][at & 15]; };
+  auto hide_all = [&](Scores& r, int kb) {
+    const int rel = last_seen(kb);
 #pragma unroll
-    for (int h = 0; h < 2; h++)
-#pragma unroll
-      for (int i = 0; i < 16; i++) r.s[h][i] = 32 * h + 8 * (i >> 2) + (i & 3) > rel ? -INFINITY : r.s[h][i];
+    for (int i = 0; i < 32; i++) hide(r, i, rel);
   };
   auto largest = [&](const Scores& r) {
     float most = r.s[0][0];
@@ -225,7 +252,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     if (__ballot(most > m + 8.f)) {
       const float mn = fmaxf(m, halves_max(most));
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      l *= keep;
+      l[0] *= keep; l[1] *= keep;
 #pragma unroll
       for (int d = 0; d < ND; d++)
 #pragma unroll
@@ -233,69 +260,77 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
       m = mn;
     }
   };
-  struct Weights { uint32_t w[2][8]; };
-  auto weigh = [&](const Scores& r, Weights& w) {
+  struct Weights { uint32_t w[4][4]; };             // a quarter of the keys: 16, 4 words of which are this lane's
+  auto weigh = [&](const Scores& r, Weights& w, int j) {           // two weights, one of 16 words
     const float ref = m == -INFINITY ? 0.f : m;
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int h = 0; h < 2; h++)
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        const float a = __builtin_amdgcn_exp2f(fmaf(r.s[h][2 * i], p.c_scale, -ref)), c = __builtin_amdgcn_exp2f(fmaf(r.s[h][2 * i + 1], p.c_scale, -ref));
-        sum[0] += a; sum[1] += c;
-        w.w[h][i] = dense_pack<T>(a, c);
-      }
-    l += sum[0] + sum[1];
+    const int at = 2 * (j & 7);
+    const float a = __builtin_amdgcn_exp2f(fmaf(r.s[j >> 3][at], p.c_scale, -ref)), c = __builtin_amdgcn_exp2f(fmaf(r.s[j >> 3][at + 1], p.c_scale, -ref));
+    l[0] += a; l[1] += c;
+    w.w[j >> 2][j & 3] = dense_pack<T>(a, c);
   };
-  auto operand = [&](const Weights& w, int x) {      // of 16 keys
-    const int h = x >> 1, i = 4 * (x & 1);
-    return v4i{(int)w.w[h][i], (int)w.w[h][i + 1], (int)w.w[h][i + 2], (int)w.w[h][i + 3]};
-  };
+  auto operand = [&](const Weights& w, int x) { return v4i{(int)w.w[x][0], (int)w.w[x][1], (int)w.w[x][2], (int)w.w[x][3]}; };
 
   // One block's weights under the next block's score products (where there is a next one), then its value products under the next
   // block's maximum.  V0, K1: the stages they lie in; hidden: whether a query may not see all of the next block.
   auto step = [&](const Scores& r, Scores& next, uint32_t V0, uint32_t K1, int kb_next, auto more, auto hidden) {
     constexpr bool MORE = decltype(more)::value, HIDDEN = decltype(hidden)::value;
     Weights w;
-    v4i v0[ND];
-    if (MORE) multiply(next, K1);
-    weigh(r, w);
-#pragma unroll
-    for (int d = 0; d < ND; d++) v0[d] = read_v(V0, d, 0);
+    v4i v[2][ND];
+    // Everything in the order in which it is to run: operands are asked for AHEAD products before they are needed, and a product is
+    // followed by the vector instructions that run beside it (the compiler, left to itself, asks and waits for each operand).  The
+    // weights of EARLY quarters of the keys come beside the next block's score products, those of the others beside the value products of
+    // the first quarters, the next block's maxima beside the last (all weights beside the scores: 3 x 333 tokens behind 1501 rows
+    // 51.6 us, two quarters 48.2, three 48.5; 16 x 2048 tokens 647, 632, 631).  AHEAD 4 at d_head 64 takes registers that three waves a
+    // SIMD do not have (2048 tokens behind 8000, 16 / 2 heads: 150 us, 134 with 2).
+    constexpr int AHEAD = D == 128 ? 4 : 2, NP = 2 * NS, EARLY = 2, FREE = 4 - EARLY;
     if (MORE) {
-      // operands are asked for AHEAD products before they are needed (left to itself the compiler asks and waits for each), and a
-      // product is followed by the vector instructions that run beside it
-      constexpr int AHEAD = 4, PER = 64 / NS;
-      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+      v4i k[AHEAD];
 #pragma unroll
-      for (int i = 0; i < 2 * NS; i++) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if (i < 2 * NS - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        else __builtin_amdgcn_sched_group_barrier(0x100, ND / 2, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, PER, 0);
-        __builtin_amdgcn_sched_group_barrier(0x400, 32 / (2 * NS), 0);
+      for (int i = 0; i < AHEAD; i++) k[i] = read_k(K1, i & 1, i >> 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NP; i++) {
+        next.s[i & 1] = T::mfma32(k[i % AHEAD], q[i >> 1], i < 2 ? v16f{} : next.s[i & 1]);
+        if (i + AHEAD < NP) k[i % AHEAD] = read_k(K1, i & 1, (i + AHEAD) >> 1);
+        else {
+#pragma unroll
+          for (int d = (i + AHEAD - NP) * ND / AHEAD; d < (i + AHEAD - NP + 1) * ND / AHEAD; d++) v[0][d] = read_v(V0, d, 0);
+        }
+#pragma unroll
+        for (int j = i * 4 * EARLY / NP; j < (i + 1) * 4 * EARLY / NP; j++) weigh(r, w, j);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    } else {
+#pragma unroll
+      for (int d = 0; d < ND; d++) v[0][d] = read_v(V0, d, 0);
+#pragma unroll
+      for (int j = 0; j < 4 * EARLY; j++) weigh(r, w, j);
     }
-    __builtin_amdgcn_sched_barrier(0);
+    const int rel = HIDDEN ? last_seen(kb_next) : 0;
+    float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int x = 0; x < 4; x++) {
       const v4i pw = operand(w, x);
 #pragma unroll
-      for (int d = 0; d < ND; d++) o[d] = T::mfma32(x == 0 ? v0[d] : read_v(V0, d, x), pw, o[d]);
-    }
-    float most = -INFINITY;
-    if (MORE) {
-      if (HIDDEN) hide(next, kb_next);
-      most = largest(next);
-    }
+      for (int d = 0; d < ND; d++) {
+        o[d] = T::mfma32(v[x & 1][d], pw, o[d]);
+        if (x < 3) v[(x + 1) & 1][d] = read_v(V0, d, x + 1);
+        if (x < FREE) {
 #pragma unroll
-    for (int i = 0; i < 4 * ND; i++) {
-      if (i < 3 * ND) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if (MORE) __builtin_amdgcn_sched_group_barrier(0x002, ((HIDDEN ? 80 : 16) + 4 * ND - 1) / (4 * ND), 0);
+          for (int j = d * 4 / ND; j < (d + 1) * 4 / ND; j++) weigh(r, w, 4 * (x + EARLY) + j);
+        } else if (MORE) {
+          constexpr int N = 32 / ((4 - FREE) * ND);
+#pragma unroll
+          for (int i = 0; i < N; i++) {
+            const int at = ((x - FREE) * ND + d) * N + i;
+            if (HIDDEN) hide(next, at, rel);
+            most[i & 1] = fmaxf(most[i & 1], next.s[at >> 4][at & 15]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (MORE) refer(most);
+    if (MORE) refer(fmaxf(most[0], most[1]) * p.c_scale);
   };
   // A block whose values may be no numbers: those must not meet the weight 0 of a query that does not see them.  The products
   // leave them out, and the queries that do see them get them added.
@@ -304,9 +339,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     Scores r;
     Weights w;
     multiply(r, at);
-    hide(r, kb);
+    hide_all(r, kb);
     refer(largest(r));
-    weigh(r, w);
+    for (int j = 0; j < 16; j++) weigh(r, w, j);
     uint32_t odd = 0;
 #pragma unroll
     for (int x = 0; x < 4; x++) {
@@ -324,7 +359,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
       }
     }
     if (__ballot(odd != 0)) {
-      const int rel = limit - kb * kKeys;
+      const int rel = limit - kb * kKeys, half = anew(lane) >> 5;
       for (int key = 0; key < kKeys; key++) {
         const bool sees = key <= rel;
         const uint32_t row_at = lds0 + at + PLANE + key * ROW_BYTES;
@@ -346,117 +381,152 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     }
   };
 
-  // Block kb + 1's keys and block kb's values are there, and nobody reads the stages any more that the next copies go to.
+  // Block kb + 1's keys and block kb's values are there, and nobody reads the stages any more that the next copies go to.  Behind
+  // the last block come the first keys of the workgroup's second tile.
+  int next_blocks = at.second >= 0 ? prompt_blocks<ROWS>(p, at, at.second) : 0;
   auto sync = [&](int kb) {
     lds_copy_wait_barrier<0>();
     if (PAGED && kb + 2 >= looked_up + 64) look_up(kb + 1);
     if (kb + 2 < n_blocks) stage(kb + 2, kb & 1, true);
     if (kb + 1 < n_blocks) stage(kb + 1, (kb + 1) & 1, false);
+    else if (next_blocks > 0) {
+      if (PAGED && looked_up != 0) look_up(anew_scalar(0));
+      stage(anew_scalar(0), 0, true);
+      if (next_blocks > 1) stage(anew_scalar(1), 1, true);
+    }
   };
-  const int n_mine = (max(wseen, 0) + kKeys - 1) / kKeys;
-  const int n_whole = max(0, min(wseen, wall)) / kKeys;            // blocks that all of the wave's queries see whole
+  auto queries_there = [&] {                         // no wait for them in the loops, which would be one for the copies too
+#pragma unroll
+    for (int s = 0; s < NS; s++) asm volatile("" : "+v"(q[s]));
+  };
   if (n_blocks > 0) {
     if (PAGED) look_up(0);
     stage(0, 0, true);
     if (n_blocks > 1) stage(1, 1, true);
     stage(0, 0, false);
   }
-#pragma unroll
-  for (int s = 0; s < NS; s++) asm volatile("" : "+v"(q[s]));      // the queries are there: no wait for them in the loops, which would be one for the copies too
+  queries_there();
+  if (n_blocks > 0) lds_copy_wait_barrier<0>();
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
-  if (n_blocks > 0) {
-    Scores r0, r1;
-    int kb = 0;
-    lds_copy_wait_barrier<0>();
-    if (n_mine > 0) {
-      multiply(r0, 0);
-      if (n_whole == 0) hide(r0, 0);
-      refer(largest(r0));
-    }
-    sync(0);                                         // (the third block's keys go where the first one's were)
-    if (n_mine > 0) {
-      for (; kb + 2 < n_whole; kb += 2) {
-        __builtin_amdgcn_s_setprio(1);               // (the wave that multiplies goes before the one that copies or waits: 4 % at 8192 tokens)
-        step(r0, r1, 0, STAGE, 0, yes, no);
-        __builtin_amdgcn_s_setprio(0);
-        sync(kb + 1);
-        __builtin_amdgcn_s_setprio(1);
-        step(r1, r0, STAGE, 0, 0, yes, no);
-        __builtin_amdgcn_s_setprio(0);
-        sync(kb + 2);
+#pragma unroll 1
+  for (;;) {
+    // a wave's 32 rows: the keys that its last one sees, and those that all of them see
+    const int row0 = tile * ROWS, wrow = row0 + 32 * wave, wlast = min(wrow + 31, NR - 1), here = min(nk, n_blocks * kKeys);
+    const int wseen = wrow >= NR ? 0 : p.causal ? min(here, wlast / p.G + ahead + 1) : here;
+    const int wall = p.causal ? wrow / p.G + ahead + 1 : here;
+    const int n_mine = (max(wseen, 0) + kKeys - 1) / kKeys;
+    const int n_whole = max(0, min(wseen, wall)) / kKeys;            // blocks that all of the wave's queries see whole
+    limit = p.causal ? min(wrow + n, NR - 1) / p.G + ahead : nk - 1;
+    clear();
+    if (n_blocks > 0) {
+      Scores r0, r1;
+      int kb = 0;
+      if (n_mine > 0) {
+        multiply(r0, 0);
+        if (n_whole == 0) hide_all(r0, 0);
+        refer(largest(r0));
       }
-      for (; kb + 1 < n_mine; kb++) {
-        __builtin_amdgcn_s_setprio(1);
-        step(r0, r1, (kb & 1) * STAGE, STAGE - (kb & 1) * STAGE, kb + 1, yes, yes);
-        __builtin_amdgcn_s_setprio(0);
-        r0 = r1;
-        sync(kb + 1);
+      sync(0);                                       // (the third block's keys go where the first one's were)
+      if (n_mine > 0) {
+        for (; kb + 2 < n_whole; kb += 2) {
+          __builtin_amdgcn_s_setprio(1);             // (the wave that multiplies goes before the one that copies or waits: 4 % at 8192 tokens)
+          step(r0, r1, 0, STAGE, 0, yes, no);
+          __builtin_amdgcn_s_setprio(0);
+          sync(kb + 1);
+          __builtin_amdgcn_s_setprio(1);
+          step(r1, r0, STAGE, 0, 0, yes, no);
+          __builtin_amdgcn_s_setprio(0);
+          sync(kb + 2);
+        }
+        for (; kb + 1 < n_mine; kb++) {
+          __builtin_amdgcn_s_setprio(1);
+          step(r0, r1, (kb & 1) * STAGE, STAGE - (kb & 1) * STAGE, kb + 1, yes, yes);
+          __builtin_amdgcn_s_setprio(0);
+          r0 = r1;
+          sync(kb + 1);
+        }
       }
-      step(r0, r1, (kb & 1) * STAGE, 0, 0, no, no);
-    }
-    for (; kb + 1 < n_blocks; kb++) sync(kb + 1);    // (waves whose queries see no more of the keys still copy)
+      if (next_blocks > 0) load_q(at.second);        // (the last scores are there)
+      if (n_mine > 0) step(r0, r1, (kb & 1) * STAGE, 0, 0, no, no);
+      for (; kb + 1 < n_blocks; kb++) sync(kb + 1);  // (waves whose queries see no more of the keys still copy)
 
-    // Something is no number: it may be a value that met a weight of 0.  All once more, carefully (results that should be no
-    // numbers come out the same).
-    float zero = 0.f;                                // NaN where a value is infinite or none
-#pragma unroll
-    for (int d = 0; d < ND; d++)
-#pragma unroll
-      for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
-    if (__syncthreads_or(zero != 0.f)) {
-      m = -INFINITY; l = 0.f;
+      // Something is no number: it may be a value that met a weight of 0.  All once more, carefully (results that should be no
+      // numbers come out the same).
+      float zero = 0.f;                              // NaN where a value is infinite or none
 #pragma unroll
       for (int d = 0; d < ND; d++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) o[d][i] = 0.f;
-      for (kb = 0; kb < n_blocks; kb++) {
-        if (PAGED && kb % 64 == 0) look_up(kb);
-        stage(kb, kb & 1, true);
-        stage(kb, kb & 1, false);
-        lds_copy_wait_barrier<0>();
-        if (kb < n_mine) careful(kb);
+        for (int i = 0; i < 16; i++) zero = fmaf(o[d][i], 0.f, zero);
+      odd_sh[wave] = __ballot(zero != 0.f) != 0;
+      queries_there();
+      lds_copy_wait_barrier<0>();                    // (the second tile's keys are there, and nobody reads this one's any more)
+      bool odd = false;
+#pragma unroll
+      for (int w = 0; w < NW; w++) odd = odd || odd_sh[w] != 0;
+      if (odd) {
+        clear();
+        if (next_blocks > 0) { load_q(tile); queries_there(); }
+        for (kb = 0; kb < n_blocks; kb++) {
+          if (PAGED && kb % 64 == 0) look_up(anew_scalar(kb));
+          stage(kb, kb & 1, true);
+          stage(kb, kb & 1, false);
+          lds_copy_wait_barrier<0>();
+          if (kb < n_mine) careful(kb);
+        }
+        if (next_blocks > 0) {
+          load_q(at.second);
+          queries_there();
+          if (PAGED) look_up(anew_scalar(0));
+          __syncthreads();
+          stage(anew_scalar(0), 0, true);
+          if (next_blocks > 1) stage(anew_scalar(1), 1, true);
+          lds_copy_wait_barrier<0>();
+        }
       }
     }
+    if (next_blocks > 0) stage(anew_scalar(0), 0, false);
+    if (at.splits > 1) {                             // a part: as it is, for k_dense_prompt_join
+      float* const part = prompt_part(p, idx, kv, split, ROWS, D);
+      const int i0 = anew(lane), half = i0 >> 5, r = 32 * wave + (i0 & 31);
+      const float sum = no_tag(halves_sum(l[0] + l[1]));
+      if (half == 0) { part[2 * r] = no_tag(m); part[2 * r + 1] = sum; }
+#pragma unroll
+      for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+          *(v4f*)(part + 2 * ROWS + r * D + 32 * d + 8 * g + 4 * half) =
+              v4f{no_tag(o[d][4 * g]), no_tag(o[d][4 * g + 1]), no_tag(o[d][4 * g + 2]), no_tag(o[d][4 * g + 3])};
+      break;
+    }
+    // The output from the accumulators, 16 bytes a lane: the halves of a wave have 4 of 8 dims each, and swap so that the first half
+    // stores the even pieces and the second the odd ones.
+    const float sum = halves_sum(l[0] + l[1]), inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int i0 = anew(lane), row = wrow + (i0 & 31);
+    if (row < NR) {
+      const int tok = row / p.G;
+      uint16_t* const to = p.out + (int64_t)(q_start + tok) * p.out_ld + (kv * p.G + row - tok * p.G) * D + (i0 >> 5) * 8;
+#pragma unroll
+      for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+          v4i x;
+#pragma unroll
+          for (int i = 0; i < 2; i++) {
+            const uint32_t even = dense_pack<T>(o[d][4 * g + 2 * i] * inv, o[d][4 * g + 2 * i + 1] * inv);
+            const uint32_t odd = dense_pack<T>(o[d][4 * g + 4 + 2 * i] * inv, o[d][4 * g + 4 + 2 * i + 1] * inv);
+            const auto r = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
+            x[i] = (int)r[0]; x[2 + i] = (int)r[1];
+          }
+          *(v4i*)(to + 32 * d + 8 * g) = x;
+        }
+    }
+    if (next_blocks == 0 && (at.second < 0 || tile == at.second)) break;
+    tile = at.second;
+    n_blocks = next_blocks;
+    next_blocks = 0;
   }
   if (__ballot(bad) && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
-  if (at.splits > 1) {                               // a part: as it is, for k_dense_prompt_join
-    float* const part = prompt_part(p, idx, kv, split, ROWS, D);
-    const int r = 32 * wave + n;
-    const float sum = no_tag(halves_sum(l));
-    if (half == 0) { part[2 * r] = no_tag(m); part[2 * r + 1] = sum; }
-#pragma unroll
-    for (int d = 0; d < ND; d++)
-#pragma unroll
-      for (int g = 0; g < 4; g++)
-        *(v4f*)(part + 2 * ROWS + r * D + 32 * d + 8 * g + 4 * half) =
-            v4f{no_tag(o[d][4 * g]), no_tag(o[d][4 * g + 1]), no_tag(o[d][4 * g + 2]), no_tag(o[d][4 * g + 3])};
-    return;
-  }
-  // The output in whole lines: through LDS, a wave's rows in its own part of the stages, the 16-byte pieces of a row permuted.
-  // (Straight from the accumulators a row goes out in pieces of 8 bytes.)
-  l = halves_sum(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  __syncthreads();                                   // nobody reads the stages any more
-  const uint32_t put = lds0 + wave * (32 * ROW_BYTES) + n * ROW_BYTES;
-  const int put_sw = D == 128 ? n & 15 : (n >> 1) & 7;
-#pragma unroll
-  for (int d = 0; d < ND; d++)
-#pragma unroll
-    for (int g = 0; g < 4; g++) {
-      v2i r;
-      r[0] = (int)dense_pack<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
-      r[1] = (int)dense_pack<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
-      *(__attribute__((address_space(3))) v2i*)(uintptr_t)(put + ((4 * d + g) ^ put_sw) * 16 + half * 8) = r;
-    }
-#pragma unroll
-  for (int i = 0; i < 32 / RPI; i++) {
-    const int r = i * RPI + my_row, out_row = wrow + r;
-    const int t = out_row / p.G, h = kv * p.G + out_row - t * p.G;
-    const v4i x = *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(lds0 + wave * (32 * ROW_BYTES) + r * ROW_BYTES +
-                                                                            (my_piece ^ (D == 128 ? r & 15 : (r >> 1) & 7)) * 16);
-    if (out_row < NR) *(v4i*)(p.out + (int64_t)(q_start + t) * p.out_ld + h * D + my_piece * 8) = x;
-  }
 }
 
 // The parts of the tiles that several workgroups share, joined in their order: 16 rows of a tile per workgroup, 8 or 4 dims of a
@@ -467,7 +537,7 @@ __global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) 
   const int lane = threadIdx.x & 63, kv = blockIdx.x % p.Hkv, idx = blockIdx.x / p.Hkv;
   PromptPlace at;
   if (!prompt_place<PAGED, ROWS>(p, idx, lane, at) || at.splits == 1) return;
-  const int r = blockIdx.y * 16 + threadIdx.x / 16, x = threadIdx.x % 16 * N, row = at.row0 + r;
+  const int r = blockIdx.y * 16 + threadIdx.x / 16, x = threadIdx.x % 16 * N, row = at.tile * ROWS + r;
   if (row >= at.nq * p.G) return;
   float M = -INFINITY, L = 0.f, O[N];
 #pragma unroll
@@ -510,11 +580,19 @@ __global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) 
 template <class T, int D, bool PAGED>
 hipError_t launch(DensePromptParams& p, hipStream_t s) {
   constexpr int NW = 4, ROWS = 32 * NW;
-  const int64_t tiles = ((int64_t)p.n_q * p.G) / ROWS + p.B, wgs = tiles * p.Hkv;      // at most: every sequence ends inside a tile
+  int64_t tiles = ((int64_t)p.n_q * p.G) / ROWS + p.B;           // at most: every sequence ends inside a tile
+  // Two tiles a workgroup where there are many and they differ: the second one's first keys and queries are asked for under the first
+  // one's last products, so that every other tile starts without a wait (16 x 2048 tokens, 32 heads of 128: 650 -> 632 us, 64 x 300, 32 / 8
+  // heads: 129 -> 121, 4 x 4096 of 16 / 2 heads of 64: 166 -> 158; over 13 causal calls of 2048 to 5920 tiles 0.93 to 1.04 of the time, 0.98
+  // on average).  With fewer tiles the last round of workgroups costs more (1283 ragged tiles: 73 -> 81 us), and without a mask all
+  // tiles cost the same already.
+  p.pairs = p.causal && tiles * p.Hkv >= 2048;
+  if (p.pairs) tiles = (tiles + p.B) / 2;
+  const int64_t wgs = tiles * p.Hkv;
   // no sequence has more keys than there are, and no workgroup of several fewer than kLeastBlocks blocks of them
   const int64_t keys = PAGED ? (int64_t)p.pages.max_pages * p.pages.page_rows : p.n_kv;
   const int64_t most = std::min<int64_t>({32, kDensePromptParts / wgs, (keys + kKeys - 1) / kKeys / kLeastBlocks});
-  p.splits = (int)std::max<int64_t>(most, 1);
+  p.splits = p.pairs ? 1 : (int)std::max<int64_t>(most, 1);
   k_dense_prompt<T, D, PAGED, NW><<<dim3((unsigned)(wgs * p.splits)), 64 * NW, 0, s>>>(p);
   if (p.splits > 1) k_dense_prompt_join<T, D, PAGED, ROWS><<<dim3((unsigned)wgs, ROWS / 16), 256, 0, s>>>(p);
   return hipGetLastError();

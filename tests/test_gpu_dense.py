@@ -482,3 +482,41 @@ def test_decode_step_in_a_graph_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(out, replayed) and torch.isfinite(replayed).all(), i
     L.close()
+
+
+# ------------------------------------------------------------------------------------------------ two tiles a workgroup
+def spread(lengths, batch):
+    """The lengths among sequences of none: so many that workgroups take two tiles each."""
+    out = [0] * batch
+    for i, n in enumerate(lengths):
+        out[(i * 997 + 3) % batch] = n
+    return out
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(4, 4, 128, "bf16"), (7, 1, 128, "f16"), (4, 2, 64, "bf16"), (16, 1, 64, "f16")])
+def test_prompt_two_tiles_a_workgroup(hq, hkv, d, dtype):
+    # even and odd numbers of tiles, last ones of few rows, one tile alone
+    prompt_case(hq, hkv, d, dtype, spread([700, 129, 128, 1, 257, 384, 33, 511], 2100 // hkv), spare=3)
+
+
+def test_prompt_two_tiles_a_workgroup_keys_of_another_number():
+    # more keys than queries; fewer, so that the second tile sees nothing, or the first only part of its keys; none
+    nq, nk = [300, 300, 300, 300, 140, 520], [800, 130, 300, 0, 10, 391]
+    prompt_case(3, 1, 128, "bf16", spread(nq, 2100), spread(nk, 2100))
+    prompt_case(2, 2, 64, "f16", spread(nq, 1100), spread(nk, 1100))
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,page_rows", [(2, 1, 128, "bf16", 16), (1, 1, 64, "f16", 112), (5, 1, 128, "f16", 128)])
+def test_chunk_two_tiles_a_workgroup(hq, hkv, d, dtype, page_rows):
+    # more than 64 blocks of keys: where they lie is looked up again for the second tile
+    prompt_case(hq, hkv, d, dtype, spread([260, 300, 129, 2], 2100), spread([4700, 300, 4300, 70], 2100), page_rows=page_rows)
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(1, 1, 128, "bf16"), (2, 1, 64, "f16")])
+def test_prompt_two_tiles_a_workgroup_hidden_values(hq, hkv, d, dtype):
+    # numbers that are none late in the sequence (the first tile of a pair sees them, the second does not), early, and in between
+    def tweak(k, v):
+        v[350, 3], v[399, 60], v[130, 5], v[2, 7] = math.inf, math.nan, -math.inf, math.inf
+        k[380] = math.nan
+    prompt_case(hq, hkv, d, dtype, spread([400], 2100), tweak=tweak)
+    prompt_case(hq, hkv, d, dtype, spread([300], 2100), tweak=lambda k, v: v[297:, 5].fill_(math.inf))
