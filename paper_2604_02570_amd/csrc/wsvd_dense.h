@@ -85,6 +85,7 @@ struct DenseDecodeParams {
   DensePages pages;
   unsigned long long* parts;    // words {value, tag} [chunk][Hkv][G][d + 2]: maximum, sum, row
   int B, Hkv, G, max_len, waves, target, alone_units, min_units;
+  int alone;                    // no sequence is cut
   float c_scale;                // sm_scale * log2(e)
   int* err_word;
 };

@@ -114,6 +114,7 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   // (in rows twice as many at half the row length; the min_chunk setting, where given, is taken for both)
   p.alone_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : 5 * 128 / desc->d_head;
   p.min_units = ctx->opt.min_chunk ? p.alone_units : 2 * 128 / desc->d_head;
+  p.alone = dense_units_of(max_seq_len) <= p.alone_units;
   p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
   return launched(wsvd_launch_dense_decode(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
 }
