@@ -362,7 +362,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     float most = s[0];
 #pragma unroll
     for (int i = 1; i < 8; i++) most = fmaxf(most, s[i]);
-    if (__ballot(most > m + 8.f)) {                  // the reference moves only when a weight would pass 2^8
+    if (__ballot(most > m + T::kMove)) {             // (see the element types)
       const float mn = fmaxf(m, quarters_max(most));
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       l *= keep;
@@ -372,11 +372,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int i = 0; i < 4; i++) o[j][i] *= keep;
       m = mn;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = m == -INFINITY ? 0.f : m - T::kRaise;
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) { w[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += w[i]; }
-    // weights as a pair of 16-bit numbers (what is lost is below fp32's own rounding of the sum), or as twice the same half
+    // weights as a pair of 16-bit numbers (bf16: off by at most 2^-17 of the weight; f16: by 2^-23 of it or 2^-36 of the reference's), or as
+    // twice the same half
     v4i hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; i++) {

@@ -1,0 +1,97 @@
+"""Dense-layer attention on the GPU where single numbers decide: weights far below the largest, infinite values and scores, what other
+calls left in the workspace; against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+import paper_2604_02570_amd as W
+from dense_ref import DTYPES, F64, Pool, attend_fast, check, prefix, randn
+from test_gpu_dense import Layer, gen
+
+pytestmark = pytest.mark.gpu
+LN2 = math.log(2.0)                             # as the softmax scale: scores count in powers of two
+
+
+def run_decode(dtype, q, keys, values, *, scale=0.0, min_chunk=0, page_rows=16, L=None):
+    """q [B, Hq, d]; keys, values: a tensor [rows, Hkv, d] for every sequence."""
+    B, hq, d = q.shape
+    own = L is None
+    L = L or Layer(B, hq, keys[0].shape[1], d, dtype, scale)
+    W.wsvd_ctx_set_option(L.ctx, "min_chunk", min_chunk)
+    lens = [k.shape[0] for k in keys]
+    pool = Pool(gen(17), lens, keys[0].shape[1], d, page_rows, dtype, fill_rows=False)
+    for b, (k, v) in enumerate(zip(keys, values)):
+        pool.put(b, 0, k, v)
+    out = torch.full((B, hq, d), 7.0, dtype=DTYPES[dtype], device="cuda")
+    W.wsvd_dense_decode_attn_paged(L.ctx, L.desc, q.cuda(), hq * d, L.cache(pool), max(lens), out)
+    got = out.cpu()
+    if own:
+        L.close()
+    return got
+
+
+def run_prompt(dtype, q, k, v, nq, nk, *, scale=0.0, causal=True, page_rows=0, batch=0):
+    """q [tokens, Hq, d], k, v [rows, Hkv, d], packed; batch: sequences of nothing behind them up to this number."""
+    nq, nk = [list(n) + [0] * (batch - len(n)) for n in (nq, nk)]
+    T, hq, d = q.shape
+    hkv = k.shape[1]
+    L = Layer(len(nq), hq, hkv, d, dtype, scale)
+    out = torch.full((T, hq * d), 7.0, dtype=DTYPES[dtype], device="cuda")
+    if page_rows:
+        pool, at = Pool(gen(18), nk, hkv, d, page_rows, dtype, fill_rows=False), prefix(nk).tolist()
+        for b in range(len(nk)):
+            pool.put(b, 0, k[at[b]:at[b + 1]], v[at[b]:at[b + 1]])
+        W.wsvd_dense_prefill_attn_paged(L.ctx, L.desc, q.cuda(), hq * d, T, prefix(nq).cuda(), L.cache(pool), out, hq * d)
+    else:
+        W.wsvd_dense_prefill_attn(L.ctx, L.desc, q.cuda(), hq * d, k.cuda(), hkv * d, v.cuda(), hkv * d, T, k.shape[0], prefix(nq).cuda(),
+                                  prefix(nk).cuda(), causal, out, hq * d)
+    got = out.cpu().view(T, hq, d)
+    L.close()
+    return got
+
+
+def same_kind(got, want):
+    """Infinite where the formula is infinite, NaN where it is NaN; returns where it is a number."""
+    assert torch.equal(torch.isnan(want), torch.isnan(got))
+    infinite = torch.isinf(want)
+    assert torch.equal(want[infinite], got[infinite].to(F64))
+    return torch.isfinite(want)
+
+
+# ------------------------------------------------------------------------------------------------ weights far below the largest
+def sink(dtype, rows, hq, hkv, d, gap, at, dims=None):
+    """A key `gap` powers of two above the others, whose scores spread a little, and whose value is 0: the output is what the small
+    weights make it.  Queries of 1 in their first dim."""
+    g = gen(rows + d)
+    q = torch.zeros(1, hq, d, dtype=DTYPES[dtype])
+    q[..., 0] = 1.0
+    k, v = torch.zeros(rows, hkv, d, dtype=DTYPES[dtype]), 1.0 + randn(g, dtype, rows, hkv, d, scale=0.25)
+    k[..., 0] = randn(g, dtype, rows, hkv, scale=0.5)
+    k[at, :, 0], v[at] = gap, 0.0
+    return q, k, v
+
+
+def check_small_weights(got, want, size, dtype, rounded, rows, v):
+    """As everywhere; and where the type's small numbers run out, a weight is off by at most 2^-36 of the largest."""
+    lost = rows * 2.0 ** -36 * v.to(F64).abs().max()
+    check(got, want, size + (lost * 2.0 ** 12 if dtype == "f16" else 0.0), dtype, rounded)
+
+
+@pytest.mark.parametrize("rows,min_chunk", [(640, 0), (1100, 128), (65001, 0)])
+@pytest.mark.parametrize("gap", [18.0, 25.5, 27.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_decode_weights_far_below_the_largest(dtype, gap, rows, min_chunk):
+    for at in (0, rows // 2, rows - 1) if rows < 2000 else (0,):
+        q, k, v = sink(dtype, rows, 4, 1, 64, gap, at)
+        got = run_decode(dtype, q, [k], [v], scale=LN2, min_chunk=min_chunk)
+        want, size = attend_fast(q, k, v, [rows - 1], LN2)
+        check_small_weights(got, want, size, dtype, False, rows, v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_decode_peaked_scores_over_many_rows(dtype):
+    g = gen(77)
+    q, k, v = randn(g, dtype, 1, 8, 128, scale=4.0), randn(g, dtype, 20011, 2, 128), randn(g, dtype, 20011, 2, 128)
+    want, size = attend_fast(q, k, v, [20010], 128 ** -0.5)
+    check_small_weights(run_decode(dtype, q, [k], [v]), want, size, dtype, False, 20011, v)
