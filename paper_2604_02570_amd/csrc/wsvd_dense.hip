@@ -362,7 +362,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     float most = s[0];
 #pragma unroll
     for (int i = 1; i < 8; i++) most = fmaxf(most, s[i]);
-    if (__ballot(most > m + T::kMove)) {             // (see the element types)
+    if (__ballot(most - m > T::kMove)) {             // (see the element types; the difference is exact where m + kMove is not)
       const float mn = fmaxf(m, quarters_max(most));
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       l *= keep;
