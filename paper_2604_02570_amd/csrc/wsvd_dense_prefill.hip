@@ -246,11 +246,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     for (int h = 0; h < 2; h++)
 #pragma unroll
       for (int i = 0; i < 16; i++) most = fmaxf(most, r.s[h][i]);
-    return most * p.c_scale;
+    return most;
   };
-  auto refer = [&](float most) {                     // the reference moves only when a weight would pass 2^8
-    if (__ballot(most > m + 8.f)) {
-      const float mn = fmaxf(m, halves_max(most));
+  auto refer = [&](float most) {                     // (see the element types; the difference is formed as the weights' are, without rounding)
+    if (__ballot(fmaf(most, p.c_scale, -m) > T::kMove)) {
+      const float mn = fmaxf(m, halves_max(most) * p.c_scale);
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       l[0] *= keep; l[1] *= keep;
 #pragma unroll
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   };
   struct Weights { uint32_t w[4][4]; };             // a quarter of the keys: 16, 4 words of which are this lane's
   auto weigh = [&](const Scores& r, Weights& w, int j) {           // two weights, one of 16 words
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = m == -INFINITY ? 0.f : m - T::kRaise;
     const int at = 2 * (j & 7);
     const float a = __builtin_amdgcn_exp2f(fmaf(r.s[j >> 3][at], p.c_scale, -ref)), c = __builtin_amdgcn_exp2f(fmaf(r.s[j >> 3][at + 1], p.c_scale, -ref));
     l[0] += a; l[1] += c;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (MORE) refer(fmaxf(most[0], most[1]) * p.c_scale);
+    if (MORE) refer(fmaxf(most[0], most[1]));
   };
   // A block whose values may be no numbers: those must not meet the weight 0 of a query that does not see them.  The products
   // leave them out, and the queries that do see them get them added.

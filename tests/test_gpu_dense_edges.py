@@ -116,3 +116,33 @@ def test_decode_large_scores(dtype, most, rows, min_chunk):
     q, k, v = large_scores(dtype, 1, rows, 64, most)
     got = run_decode(dtype, q, [k], [v], scale=LN2, min_chunk=min_chunk)
     assert ((got.to(F64) - 1).abs() <= torch.finfo(DTYPES[dtype]).eps).all()
+
+
+@pytest.mark.parametrize("queries,rows,page_rows", [(300, 700, 0), (5, 2600, 0), (300, 700, 16), (5, 2600, 112)])
+@pytest.mark.parametrize("gap", [18.0, 25.5, 27.0])
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "f16"), (128, "bf16")])
+def test_prompt_weights_far_below_the_largest(d, dtype, gap, queries, rows, page_rows):
+    """Tiles of one workgroup, and of several."""
+    for at in (0, rows - queries - 3):
+        q, k, v = sink(dtype, rows, 2, 1, d, gap, at)
+        q = q.expand(queries, 2, d).contiguous()
+        got = run_prompt(dtype, q, k, v, [queries], [rows], scale=LN2, page_rows=page_rows)
+        want, size = attend_fast(q, k, v, torch.arange(rows - queries, rows), LN2)
+        check_small_weights(got, want, size, dtype, True, rows, v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_prompt_peaked_scores_of_both_types(dtype):
+    g = gen(78)
+    q, k, v = randn(g, dtype, 900, 4, 128, scale=4.0), randn(g, dtype, 900, 1, 128), randn(g, dtype, 900, 1, 128)
+    want, size = attend_fast(q, k, v, torch.arange(900), 128 ** -0.5)
+    check_small_weights(run_prompt(dtype, q, k, v, [900], [900]), want, size, dtype, True, 900, v)
+
+
+@pytest.mark.parametrize("queries,rows,page_rows", [(200, 700, 0), (5, 2600, 0), (200, 700, 16)])
+@pytest.mark.parametrize("most", [2.0 ** 15, 2.0 ** 21, 2.0 ** 24, 2.0 ** 26])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_prompt_large_scores(dtype, most, queries, rows, page_rows):
+    q, k, v = large_scores(dtype, queries, rows, 128, most)
+    got = run_prompt(dtype, q, k, v, [queries], [rows], scale=LN2, page_rows=page_rows)
+    assert ((got.to(F64) - 1).abs() <= torch.finfo(DTYPES[dtype]).eps).all()
