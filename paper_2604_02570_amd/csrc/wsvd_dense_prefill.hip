@@ -502,6 +502,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     // The output from the accumulators, 16 bytes a lane: the halves of a wave have 4 of 8 dims each, and swap so that the first half
     // stores the even pieces and the second the odd ones.
     const float sum = halves_sum(l[0] + l[1]), inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (__ballot(sum == 0.f)) {                      // zeros, whatever the values are that scores of -inf met
+#pragma unroll
+      for (int d = 0; d < ND; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[d][i] = sum == 0.f ? 0.f : o[d][i];
+    }
     const int i0 = anew(lane), row = wrow + (i0 & 31);
     if (row < NR) {
       const int tok = row / p.G;
@@ -573,7 +579,7 @@ __global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) 
   const int t = row / p.G;
   uint32_t out[N / 2];
 #pragma unroll
-  for (int i = 0; i < N / 2; i++) out[i] = dense_pack<T>(O[2 * i] * inv, O[2 * i + 1] * inv);
+  for (int i = 0; i < N / 2; i++) out[i] = L == 0.f ? 0 : dense_pack<T>(O[2 * i] * inv, O[2 * i + 1] * inv);
   __builtin_memcpy(__builtin_assume_aligned(p.out + (int64_t)(at.q_start + t) * p.out_ld + (kv * p.G + row - t * p.G) * D + x, N * 2), out, N * 2);
 }
 

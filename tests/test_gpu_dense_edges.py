@@ -146,3 +146,22 @@ def test_prompt_large_scores(dtype, most, queries, rows, page_rows):
     q, k, v = large_scores(dtype, queries, rows, 128, most)
     got = run_prompt(dtype, q, k, v, [queries], [rows], scale=LN2, page_rows=page_rows)
     assert ((got.to(F64) - 1).abs() <= torch.finfo(DTYPES[dtype]).eps).all()
+
+
+# ------------------------------------------------------------------------------------------------ infinite scores and values
+@pytest.mark.parametrize("queries,rows,page_rows,batch", [(70, 70, 0, 0), (70, 90, 16, 0), (6, 1600, 0, 0), (6, 1600, 16, 0), (300, 300, 0, 2100)])
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16")])
+def test_prompt_nothing_but_scores_of_minus_infinity_gives_zeros(d, dtype, queries, rows, page_rows, batch):
+    """Whatever the values hold: tiles of one workgroup, of several, two tiles a workgroup."""
+    g = gen(5)
+    q, k, v = randn(g, dtype, queries, 2, d).abs(), torch.full((rows, 1, d), -math.inf, dtype=DTYPES[dtype]), randn(g, dtype, rows, 1, d)
+    v[3, 0, 1], v[3, 0, 2], v[rows // 2, 0, 5], v[rows - queries, 0, d - 1] = math.inf, math.nan, -math.inf, math.nan
+    assert (run_prompt(dtype, q, k, v, [queries], [rows], page_rows=page_rows, batch=batch) == 0).all()
+
+
+@pytest.mark.parametrize("min_chunk", [0, 128])
+def test_decode_nothing_but_scores_of_minus_infinity_gives_zeros(min_chunk):
+    g = gen(6)
+    q, k, v = randn(g, "bf16", 1, 2, 64).abs(), torch.full((700, 1, 64), -math.inf, dtype=torch.bfloat16), randn(g, "bf16", 700, 1, 64)
+    v[3, 0, 1], v[300, 0, 2], v[699, 0, 5] = math.inf, math.nan, -math.inf
+    assert (run_decode("bf16", q, [k], [v], min_chunk=min_chunk) == 0).all()
