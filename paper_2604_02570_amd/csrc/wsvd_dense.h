@@ -7,17 +7,17 @@
 
 // ---------------------------------------------------------------- element types
 // BF16 and F16 operands of the matrix cores, 8 per lane and 4 dwords.  kExponent: the exponent bits of both halves of a dword.
-//   The softmax's weights are operands too, 2^(score - reference + kRaise), and the reference moves when a score passes it by more than
-// kMove.  A bf16 weight can be as small as an fp32 one.  An f16 one has all its bits down to 2^-14 and is gone below 2^-25, where the sum of
-// the weights, in fp32, still counts it (65001 rows 26 powers of two below one whose value is 0: output 9 % off).  So the largest f16
-// weights are 2^11 to 2^15.9 (65504 is 2^16 less half a step): full relative precision 25 powers of two below the reference, and no
-// weight off by more than 2^-36 of the reference's.  (Moved at 4.9: scores of a later block rarely pass the first one's by more; 2048 tokens
-// behind 6144, f16: 217.7 us, with 4 219.5, with 8 and a start of 2^7 218.3.)
+//   The softmax's weights are operands too, 2^(score - reference).  The reference is set kRaise below the largest score so far, and set anew when
+// a weight would pass 2^kTop.  A bf16 weight can be as small as an fp32 one.  An f16 one has all its bits down to 2^-14 and is gone below
+// 2^-25, where the sum of the weights, in fp32, still counts it (65001 rows 26 powers of two below one whose value is 0: output 9 % off).
+// So the largest f16 weights are 2^11 to 2^15.9 (65504 is 2^16 less half a step): full relative precision 25 powers of two below the largest
+// score, and no weight off by more than 2^-36 of the largest.  (Anew at 4.9 more: scores of a later block rarely pass the first one's by more;
+// 2048 tokens behind 6144, f16: 217.7 us, at 4 more 219.5, 2^7 to 2^15 218.3.)
 struct DenseBf16 {
   using Elem = __bf16;
   using V8 = v8bf16;
   static constexpr uint32_t kExponent = 0x7F807F80u, kExponentUlp = 0x00800080u;
-  static constexpr float kMove = 8.f, kRaise = 0.f;
+  static constexpr float kRaise = 0.f, kTop = 8.f;
   static WSVD_DEV v4f mfma16(v4i a, v4i b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0); }
   static WSVD_DEV v16f mfma32(v4i a, v4i b, v16f c) { return mfma_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c); }
 };
@@ -25,7 +25,7 @@ struct DenseF16 {
   using Elem = _Float16;
   using V8 = v8f16;
   static constexpr uint32_t kExponent = 0x7C007C00u, kExponentUlp = 0x04000400u;
-  static constexpr float kMove = 4.9f, kRaise = 11.f;
+  static constexpr float kRaise = 11.f, kTop = 15.9f;
   static WSVD_DEV v4f mfma16(v4i a, v4i b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0); }
   static WSVD_DEV v16f mfma32(v4i a, v4i b, v16f c) { return mfma_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c); }
 };

@@ -336,6 +336,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   bool fine = true;                                  // see below
   float part = 1.f;
   auto attend = [&](DenseTile<D>& tile, int t) {
+#pragma clang fp contract(off)                       // (a score is the same number against the limit and in its weight)
     const int r0 = first + t * 32;
     float s[8];
 #pragma unroll
@@ -362,8 +363,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     float most = s[0];
 #pragma unroll
     for (int i = 1; i < 8; i++) most = fmaxf(most, s[i]);
-    if (__ballot(most - m > T::kMove)) {             // (see the element types; the difference is exact where m + kMove is not)
-      const float mn = fmaxf(m, quarters_max(most));
+    if (__ballot(most - m > T::kTop)) {              // (see the element types)
+      const float top = quarters_max(most), low = top - T::kRaise;
+      const float mn = fmaxf(m, top - low > T::kTop ? top : low);    // (steps of 16, between scores of 2^27 and 2^28)
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       l *= keep;
 #pragma unroll
@@ -372,7 +374,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int i = 0; i < 4; i++) o[j][i] *= keep;
       m = mn;
     }
-    const float ref = m == -INFINITY ? 0.f : m - T::kRaise;
+    const float ref = m == -INFINITY ? 0.f : m;
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) { w[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += w[i]; }

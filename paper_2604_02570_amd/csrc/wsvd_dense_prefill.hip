@@ -249,8 +249,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     return most;
   };
   auto refer = [&](float most) {                     // (see the element types; the difference is formed as the weights' are, without rounding)
-    if (__ballot(fmaf(most, p.c_scale, -m) > T::kMove)) {
-      const float mn = fmaxf(m, halves_max(most) * p.c_scale);
+    if (__ballot(fmaf(most, p.c_scale, -m) > T::kTop)) {
+      const float top = halves_max(most), low = fmaf(top, p.c_scale, -T::kRaise);
+      const float mn = fmaxf(m, fmaf(top, p.c_scale, -low) > T::kTop ? top * p.c_scale : low);     // (steps of 16, between scores of 2^27 and 2^28)
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       l[0] *= keep; l[1] *= keep;
 #pragma unroll
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   };
   struct Weights { uint32_t w[4][4]; };             // a quarter of the keys: 16, 4 words of which are this lane's
   auto weigh = [&](const Scores& r, Weights& w, int j) {           // two weights, one of 16 words
-    const float ref = m == -INFINITY ? 0.f : m - T::kRaise;
+    const float ref = m == -INFINITY ? 0.f : m;
     const int at = 2 * (j & 7);
     const float a = __builtin_amdgcn_exp2f(fmaf(r.s[j >> 3][at], p.c_scale, -ref)), c = __builtin_amdgcn_exp2f(fmaf(r.s[j >> 3][at + 1], p.c_scale, -ref));
     l[0] += a; l[1] += c;

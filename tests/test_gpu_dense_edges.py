@@ -97,23 +97,25 @@ def test_decode_peaked_scores_over_many_rows(dtype):
     check_small_weights(run_decode(dtype, q, [k], [v]), want, size, dtype, False, 20011, v)
 
 
-def large_scores(dtype, queries, rows, d, most):
-    """Values of 1 and scores up to `most` powers of two that keep growing by the steps in which 32 bits hold them, then jump about."""
+def large_scores(dtype, queries, rows, d, most, growth):
+    """Values of 1 and scores of `most` powers of two and more, in the steps of which 32 bits hold them: they grow by 0.5 every `growth` rows,
+    then jump about."""
     g = gen(rows)
     q = torch.zeros(queries, 2, d, dtype=DTYPES[dtype])
     q[..., 0], q[..., 1] = 2.0 ** math.floor(math.log2(most) / 2), 1.0
     k = torch.zeros(rows, 1, d, dtype=DTYPES[dtype])
-    k[..., 0], k[..., 1] = most / q[0, 0, 0].item(), torch.arange(rows)[:, None] % 300 * 0.5
+    k[..., 0], k[..., 1] = most / q[0, 0, 0].item(), torch.arange(rows)[:, None] // growth * 0.5
     k[rows // 2:, 0, 1] = (torch.randint(0, 60, (rows - rows // 2,), generator=g) * 0.5).to(DTYPES[dtype])
     return q, k, torch.ones(rows, 1, d, dtype=DTYPES[dtype])
 
 
 @pytest.mark.parametrize("rows,min_chunk", [(900, 0), (1500, 128)])
-@pytest.mark.parametrize("most", [2.0 ** 15, 2.0 ** 21, 2.0 ** 24, 2.0 ** 26, 2.0 ** 27, 2.0 ** 30])
+@pytest.mark.parametrize("growth", [1, 8, 60])
+@pytest.mark.parametrize("most", [2.0 ** 15, 2.0 ** 21, 2.0 ** 24, 2.0 ** 25, 2.0 ** 26, 2.0 ** 27, 2.0 ** 28, 2.0 ** 30])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-def test_decode_large_scores(dtype, most, rows, min_chunk):
+def test_decode_large_scores(dtype, most, growth, rows, min_chunk):
     """Weights stay inside the type whatever the scores' own steps are: a mean of ones is 1, up to the weights' rounding."""
-    q, k, v = large_scores(dtype, 1, rows, 64, most)
+    q, k, v = large_scores(dtype, 1, rows, 64, most, growth)
     got = run_decode(dtype, q, [k], [v], scale=LN2, min_chunk=min_chunk)
     assert ((got.to(F64) - 1).abs() <= torch.finfo(DTYPES[dtype]).eps).all()
 
@@ -140,10 +142,11 @@ def test_prompt_peaked_scores_of_both_types(dtype):
 
 
 @pytest.mark.parametrize("queries,rows,page_rows", [(200, 700, 0), (5, 2600, 0), (200, 700, 16)])
-@pytest.mark.parametrize("most", [2.0 ** 15, 2.0 ** 21, 2.0 ** 24, 2.0 ** 26])
+@pytest.mark.parametrize("growth", [1, 8, 60])
+@pytest.mark.parametrize("most", [2.0 ** 15, 2.0 ** 21, 2.0 ** 24, 2.0 ** 25, 2.0 ** 26, 2.0 ** 27])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-def test_prompt_large_scores(dtype, most, queries, rows, page_rows):
-    q, k, v = large_scores(dtype, queries, rows, 128, most)
+def test_prompt_large_scores(dtype, most, growth, queries, rows, page_rows):
+    q, k, v = large_scores(dtype, queries, rows, 128, most, growth)
     got = run_prompt(dtype, q, k, v, [queries], [rows], scale=LN2, page_rows=page_rows)
     assert ((got.to(F64) - 1).abs() <= torch.finfo(DTYPES[dtype]).eps).all()
 
