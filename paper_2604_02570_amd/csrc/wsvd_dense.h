@@ -41,6 +41,14 @@ template <class T>
 WSVD_DEV float dense_low(uint32_t x) { return (float)__builtin_bit_cast(typename T::Elem, (uint16_t)x); }
 template <class T>
 WSVD_DEV float dense_high(uint32_t x) { return (float)__builtin_bit_cast(typename T::Elem, (uint16_t)(x >> 16)); }
+// Ones in the halves of a dword that are infinite or no number.
+template <class T>
+WSVD_DEV uint32_t dense_odd(uint32_t x) {
+  const uint32_t t = ((x & T::kExponent) + T::kExponentUlp) & 0x80008000u;
+  return t | (t - (t >> 15));
+}
+// A partial result under another reference: one that is infinite stays so where the factor is too small for 32 bits.
+WSVD_DEV float dense_scaled(float u, float k) { return __builtin_isinf(u) ? u : u * k; }
 
 // ---------------------------------------------------------------- wave-wide integer helpers
 // Inclusive prefix sum over the wave: within rows of 16 lanes by shifts, then the last lanes' sums onto the rows behind.

@@ -1,5 +1,6 @@
 // Dense layers next to latent ones: rotary embedding with the append to a paged cache of plain keys and values, and the
 // attention of one new token per sequence over it.
+#include <type_traits>
 #include "wsvd_attn_common.h"
 #include "wsvd_dense.h"
 
@@ -243,12 +244,12 @@ WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n,
           if (k < n) {
             const float m = m_sh[k * 16 + g], f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);  // (nothing seen: l and u are 0, or NaN)
             L += l_sh[k * 16 + g] * f;
-            U += __uint_as_float((uint32_t)w[i][k]) * f;
+            U += dense_scaled(__uint_as_float((uint32_t)w[i][k]), f);
             dense_clear(part + k * stride + off);
           }
         const float f = own.M[i0 + i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(own.M[i0 + i] - M);
         own.L[i0 + i] = L + own.L[i0 + i] * f;
-        own.U[i0 + i] = U + own.U[i0 + i] * f;
+        own.U[i0 + i] = U + dense_scaled(own.U[i0 + i], f);
         own.M[i0 + i] = M;
       }
     }
@@ -333,10 +334,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
   for (int j = 0; j < NJ; j++) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
 
-  bool fine = true;                                  // see below
-  float part = 1.f;
-  auto attend = [&](DenseTile<D>& tile, int t) {
+  bool odd = false;                                  // careful: infinite values and NaN alone, or all but those (see below)
+  auto attend = [&](DenseTile<D>& tile, int t, auto careful) {
 #pragma clang fp contract(off)                       // (a score is the same number against the limit and in its weight)
+    constexpr bool CAREFUL = decltype(careful)::value;
     const int r0 = first + t * 32;
     float s[8];
 #pragma unroll
@@ -371,21 +372,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
       for (int j = 0; j < NJ; j++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) o[j][i] *= keep;
+        for (int i = 0; i < 4; i++) o[j][i] = CAREFUL ? dense_scaled(o[j][i], keep) : o[j][i] * keep;
       m = mn;
+    }
+    if (CAREFUL) {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < NK; j++) tile.v[i][j] &= (int)(odd ? dense_odd<T>((uint32_t)tile.v[i][j]) : ~dense_odd<T>((uint32_t)tile.v[i][j]));
     }
     const float ref = m == -INFINITY ? 0.f : m;
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) { w[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += w[i]; }
-    // weights as a pair of 16-bit numbers (bf16: off by at most 2^-17 of the weight; f16: by 2^-23 of it or 2^-36 of the reference's), or as
-    // twice the same half
+    if (CAREFUL && odd) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) w[i] = s[i] == -INFINITY ? 0.f : 1.f;
+    }
+    // weights as a pair of 16-bit numbers (bf16: off by at most 2^-17 of the weight; f16: by 2^-23 of it or 2^-36 of the reference's)
     v4i hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const uint32_t h = dense_pack<T>(w[2 * i] * part, w[2 * i + 1] * part), rest = dense_pack<T>(w[2 * i] - dense_low<T>(h), w[2 * i + 1] - dense_high<T>(h));
+      const uint32_t h = dense_pack<T>(w[2 * i], w[2 * i + 1]), rest = dense_pack<T>(w[2 * i] - dense_low<T>(h), w[2 * i + 1] - dense_high<T>(h));
       hi[i] = (int)h;
-      lo[i] = (int)(fine ? rest : h);
+      lo[i] = (int)(CAREFUL && odd ? h : rest);
     }
 #pragma unroll
     for (int j = 0; j < NJ; j++) {
@@ -397,39 +407,47 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       o[j] = T::mfma16(a, lo, o[j]);
     }
   };
-  auto stream = [&] {
-    for (int t = wave; t < n_tiles; t += 32 * NW) {  // 32 tiles of the wave
-      look_up(t);
-      const int n = min(32, (n_tiles - t + NW - 1) / NW);
-      DenseTile<D> t0, t1;
-      load(t0, 0);
-      int i = 0;
-      for (; i + 2 < n; i += 2) {
-        load(t1, i + 1);
-        attend(t0, t + NW * i);
-        load(t0, i + 2);
-        attend(t1, t + NW * (i + 1));
-      }
-      if (i + 1 < n) load(t1, i + 1);
-      attend(t0, t + NW * i);
-      if (i + 1 < n) attend(t1, t + NW * (i + 1));
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  for (int t = wave; t < n_tiles; t += 32 * NW) {    // 32 tiles of the wave
+    look_up(t);
+    const int n = min(32, (n_tiles - t + NW - 1) / NW);
+    DenseTile<D> t0, t1;
+    load(t0, 0);
+    int i = 0;
+    for (; i + 2 < n; i += 2) {
+      load(t1, i + 1);
+      attend(t0, t + NW * i, no);
+      load(t0, i + 2);
+      attend(t1, t + NW * (i + 1), no);
     }
-  };
-  // A value that is infinite meets the low part of its weight too, which may be 0 or less and makes it no number: where something
-  // is none, once more with the weights in two equal halves.
-#pragma unroll 1
-  for (;;) {
-    stream();
-    float zero = 0.f;                                // NaN where a value is infinite or none
+    if (i + 1 < n) load(t1, i + 1);
+    attend(t0, t + NW * i, no);
+    if (i + 1 < n) attend(t1, t + NW * (i + 1), no);
+  }
+  // A value that is infinite meets the low part of its weight too, which may be 0 or less and makes it no number, and a weight that the
+  // type or 32 bits round to 0.  Where something is none, all once more, a tile at a time: first such values alone, with 1 for every
+  // weight (any weight leaves infinite what is infinite) but 0 under a score of -inf, then the others, as exactly as ever.
+  float zero = 0.f;                                  // NaN where a value is infinite or none
 #pragma unroll
-    for (int j = 0; j < NJ; j++)
+  for (int j = 0; j < NJ; j++)
 #pragma unroll
-      for (int i = 0; i < 4; i++) zero = fmaf(o[j][i], 0.f, zero);
-    if (!fine || !__ballot(zero != 0.f && c < G)) break;           // (columns without a head may hold anything)
-    fine = false; part = 0.5f;
-    m = -INFINITY; l = 0.f;
+    for (int i = 0; i < 4; i++) zero = fmaf(o[j][i], 0.f, zero);
+  if (__ballot(zero != 0.f && c < G)) {              // (columns without a head may hold anything)
 #pragma unroll
     for (int j = 0; j < NJ; j++) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
+    odd = true;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; pass++, odd = false) {
+      m = -INFINITY; l = 0.f;
+#pragma unroll 1
+      for (int t = wave; t < n_tiles; t += NW) {
+        DenseTile<D> tile;
+        look_up(t);
+        load(tile, 0);
+        attend(tile, t, yes);
+      }
+    }
   }
   if (__ballot(bad) && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   l = quarters_sum(l);
@@ -457,7 +475,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int w = 0; w < NW; w++) {
         const float k = m_sh[w][g] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_sh[w][g] - r.M[i]);
         r.L[i] += l_sh[w][g] * k;
-        r.U[i] += o_sh[(w * G + g) * D + ((x + 4 * g) & (D - 1))] * k;
+        r.U[i] += dense_scaled(o_sh[(w * G + g) * D + ((x + 4 * g) & (D - 1))], k);
       }
     }
   }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2604_02570_amd as W
-from dense_ref import DTYPES, F64, Pool, attend_fast, check, prefix, randn
+from dense_ref import DTYPES, F64, Pool, attend, attend_fast, check, prefix, randn
 from test_gpu_dense import Layer, gen
 
 pytestmark = pytest.mark.gpu
@@ -168,3 +168,53 @@ def test_decode_nothing_but_scores_of_minus_infinity_gives_zeros(min_chunk):
     q, k, v = randn(g, "bf16", 1, 2, 64).abs(), torch.full((700, 1, 64), -math.inf, dtype=torch.bfloat16), randn(g, "bf16", 700, 1, 64)
     v[3, 0, 1], v[300, 0, 2], v[699, 0, 5] = math.inf, math.nan, -math.inf
     assert (run_decode("bf16", q, [k], [v], min_chunk=min_chunk) == 0).all()
+
+
+def infinite_values(dtype, rows, d, gap, top, odd):
+    """One key `gap` powers of two above the others, and values that are no numbers at a key of a small weight."""
+    g = gen(rows + d)
+    q = torch.zeros(1, 4, d, dtype=DTYPES[dtype])
+    q[..., 0] = 1.0
+    k, v = torch.zeros(rows, 2, d, dtype=DTYPES[dtype]), randn(g, dtype, rows, 2, d)
+    k[..., 0] = randn(g, dtype, rows, 2, scale=0.5)
+    k[top, :, 0] = gap
+    v[odd, 0, 3], v[odd, 0, 6], v[odd, 1, 4], v[odd, 1, 5] = math.inf, -math.inf, -math.inf, math.nan
+    return q, k, v
+
+
+@pytest.mark.parametrize("rows,min_chunk", [(33, 0), (600, 0), (1500, 128)])
+@pytest.mark.parametrize("gap", [40.0, 200.0])
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16"), (128, "f16")])
+def test_decode_infinite_values_of_small_weights(d, dtype, gap, rows, min_chunk):
+    """A weight too small for the type, or for 32 bits, is not 0: infinite values come out infinite, whichever key comes first and
+    whichever workgroup has it."""
+    for top, odd in ((0, rows - 1), (rows - 1, 0), (rows // 2, 7), (1, 2)):
+        q, k, v = infinite_values(dtype, rows, d, gap, top, odd)
+        want, size = attend(q, k, v, [rows - 1], LN2)
+        got = run_decode(dtype, q, [k], [v], scale=LN2, min_chunk=min_chunk)
+        fine = same_kind(got, want)
+        assert torch.isinf(want).sum() == 2 * 3 and torch.isnan(want).sum() == 2
+        check(torch.where(fine, got, 0), torch.where(fine, want, 0), torch.where(fine, size, 0), dtype, False)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16")])
+def test_decode_numbers_beside_infinite_values(d, dtype):
+    """What is a number comes out as exactly as without infinite values beside it."""
+    g = gen(8)
+    for rows in (2, 5, 40):
+        q, k, v = randn(g, dtype, 1, 16, d), randn(g, dtype, rows, 2, d), randn(g, dtype, rows, 2, d)
+        v[1, 0, 3], v[0, 1, 9], v[1, 1, 9] = math.inf, math.inf, -math.inf
+        want, size = attend(q, k, v, [rows - 1], d ** -0.5)
+        got = run_decode(dtype, q, [k], [v])
+        fine = same_kind(got, want)
+        check(torch.where(fine, got, 0), torch.where(fine, want, 0), torch.where(fine, size, 0), dtype, False)
+
+
+def test_decode_infinite_value_under_a_score_of_minus_infinity():
+    """0 times infinity, as the formula has it."""
+    g = gen(9)
+    q, k, v = randn(g, "bf16", 1, 2, 64).abs(), randn(g, "bf16", 40, 1, 64), randn(g, "bf16", 40, 1, 64)
+    k[11], v[11, 0, 5] = -math.inf, math.inf
+    want, _ = attend(q, k, v, [39], 0.125)
+    assert torch.isnan(want[..., 5]).all()
+    same_kind(run_decode("bf16", q, [k], [v]), want)
