@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
       for (int i = 0; i < 16; i++) most = fmaxf(most, r.s[h][i]);
     return most;
   };
-  auto refer = [&](float most) {                     // (see the element types; the difference is formed as the weights' are, without rounding)
+  auto refer = [&](float most, auto careful) {       // (see the element types; the difference is formed as the weights' are, without rounding)
     if (__ballot(fmaf(most, p.c_scale, -m) > T::kTop)) {
       const float top = halves_max(most), low = fmaf(top, p.c_scale, -T::kRaise);
       const float mn = fmaxf(m, fmaf(top, p.c_scale, -low) > T::kTop ? top * p.c_scale : low);     // (steps of 16, between scores of 2^27 and 2^28)
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
 #pragma unroll
       for (int d = 0; d < ND; d++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) o[d][i] *= keep;
+        for (int i = 0; i < 16; i++) o[d][i] = decltype(careful)::value ? dense_scaled(o[d][i], keep) : o[d][i] * keep;
       m = mn;
     }
   };
@@ -331,17 +331,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (MORE) refer(fmaxf(most[0], most[1]));
+    if (MORE) refer(fmaxf(most[0], most[1]), std::false_type{});
   };
-  // A block whose values may be no numbers: those must not meet the weight 0 of a query that does not see them.  The products
-  // leave them out, and the queries that do see them get them added.
+  // A block whose values may be no numbers: those must not meet the weight 0 of a query that does not see them, or one that is only
+  // rounded to 0.  The products leave them out, and the queries that do see them get them added (NaN where the score is -inf).
   auto careful = [&](int kb) {
     const uint32_t at = (kb & 1) * STAGE;
     Scores r;
     Weights w;
     multiply(r, at);
     hide_all(r, kb);
-    refer(largest(r));
+    refer(largest(r), std::true_type{});
     for (int j = 0; j < 16; j++) weigh(r, w, j);
     uint32_t odd = 0;
 #pragma unroll
@@ -352,17 +352,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
         v4i a = read_v(at, d, x);
 #pragma unroll
         for (int y = 0; y < 4; y++) {
-          const uint32_t t = (((uint32_t)a[y] & T::kExponent) + T::kExponentUlp) & 0x80008000u;
+          const uint32_t t = dense_odd<T>((uint32_t)a[y]);
           odd |= t;
-          a[y] &= (int)~(t | (t - (t >> 15)));
+          a[y] &= (int)~t;
         }
         o[d] = T::mfma32(a, pw, o[d]);
       }
     }
     if (__ballot(odd != 0)) {
       const int rel = limit - kb * kKeys, half = anew(lane) >> 5;
+      uint32_t none = 0;                             // of this lane's keys, those with a score of -inf
+#pragma unroll 1
+      for (int h = 1; h >= 0; h--) {                 // (scored again: nothing of them is kept over the products)
+        v16f x = {};
+#pragma unroll
+        for (int s = 0; s < NS; s++) x = T::mfma32(read_k(anew_scalar(at), anew_scalar(h), s), q[s], x);
+#pragma unroll
+        for (int i = 15; i >= 0; i--) none = 2 * none + (x[i] == -INFINITY);
+      }
+      const uint32_t other = (uint32_t)__shfl_xor((int)none, 32);
+#pragma unroll 1
       for (int key = 0; key < kKeys; key++) {
         const bool sees = key <= rel;
+        const uint32_t theirs = (key >> 2 & 1) == half ? none : other;
+        const float weight = (float)(~theirs >> (16 * (key >> 5) + 4 * (key >> 3 & 3) + (key & 3)) & 1u);
         const uint32_t row_at = lds0 + at + PLANE + key * ROW_BYTES;
         const int sw = D == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2;
 #pragma unroll
@@ -371,12 +384,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
           for (int g = 0; g < 4; g++) {
             const int dim = 32 * d + 8 * g + 4 * half;
             const v2i x = *(const __attribute__((address_space(3))) v2i*)(uintptr_t)(row_at + ((dim >> 3) ^ sw) * 16 + (dim & 7) * 2);
-            const uint32_t t0 = (((uint32_t)x[0] & T::kExponent) + T::kExponentUlp) & 0x80008000u;
-            const uint32_t t1 = (((uint32_t)x[1] & T::kExponent) + T::kExponentUlp) & 0x80008000u;
-            if (sees && (t0 & 0x8000u)) o[d][4 * g] += dense_low<T>((uint32_t)x[0]);
-            if (sees && (t0 >> 31)) o[d][4 * g + 1] += dense_high<T>((uint32_t)x[0]);
-            if (sees && (t1 & 0x8000u)) o[d][4 * g + 2] += dense_low<T>((uint32_t)x[1]);
-            if (sees && (t1 >> 31)) o[d][4 * g + 3] += dense_high<T>((uint32_t)x[1]);
+            const uint32_t t0 = dense_odd<T>((uint32_t)x[0]), t1 = dense_odd<T>((uint32_t)x[1]);
+            if (sees && (t0 & 0x8000u)) o[d][4 * g] = fmaf(dense_low<T>((uint32_t)x[0]), weight, o[d][4 * g]);
+            if (sees && (t0 >> 31)) o[d][4 * g + 1] = fmaf(dense_high<T>((uint32_t)x[0]), weight, o[d][4 * g + 1]);
+            if (sees && (t1 & 0x8000u)) o[d][4 * g + 2] = fmaf(dense_low<T>((uint32_t)x[1]), weight, o[d][4 * g + 2]);
+            if (sees && (t1 >> 31)) o[d][4 * g + 3] = fmaf(dense_high<T>((uint32_t)x[1]), weight, o[d][4 * g + 3]);
           }
       }
     }
@@ -387,7 +399,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   int next_blocks = at.second >= 0 ? prompt_blocks<ROWS>(p, at, at.second) : 0;
   auto sync = [&](int kb) {
     lds_copy_wait_barrier<0>();
-    if (PAGED && kb + 2 >= looked_up + 64) look_up(kb + 1);
+    if (PAGED && kb + 2 >= looked_up + 64) look_up(anew_scalar(kb + 1));
     if (kb + 2 < n_blocks) stage(kb + 2, kb & 1, true);
     if (kb + 1 < n_blocks) stage(kb + 1, (kb + 1) & 1, false);
     else if (next_blocks > 0) {
@@ -426,7 +438,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
       if (n_mine > 0) {
         multiply(r0, 0);
         if (n_whole == 0) hide_all(r0, 0);
-        refer(largest(r0));
+        refer(largest(r0), no);
       }
       sync(0);                                       // (the third block's keys go where the first one's were)
       if (n_mine > 0) {
@@ -565,14 +577,14 @@ __global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) 
     const float keep = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mn);
     L *= keep;                                       // (nothing seen: the sum and the row are 0, or NaN)
 #pragma unroll
-    for (int i = 0; i < N; i++) O[i] *= keep;
+    for (int i = 0; i < N; i++) O[i] = dense_scaled(O[i], keep);
 #pragma unroll
     for (int k = 0; k < 4; k++)
       if (s0 + k < at.splits) {
         const float add = m[k] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[k] - mn);
         L += l[k] * add;
 #pragma unroll
-        for (int i = 0; i < N; i++) O[i] += o[k][i / 4][i % 4] * add;
+        for (int i = 0; i < N; i++) O[i] += dense_scaled(o[k][i / 4][i % 4], add);
       }
     M = mn;
   }

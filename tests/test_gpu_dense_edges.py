@@ -218,3 +218,29 @@ def test_decode_infinite_value_under_a_score_of_minus_infinity():
     want, _ = attend(q, k, v, [39], 0.125)
     assert torch.isnan(want[..., 5]).all()
     same_kind(run_decode("bf16", q, [k], [v]), want)
+
+
+@pytest.mark.parametrize("queries,rows,page_rows,batch", [(40, 200, 0, 0), (40, 200, 16, 0), (5, 1600, 0, 0), (300, 400, 0, 2100)])
+@pytest.mark.parametrize("gap", [40.0, 200.0])
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16")])
+def test_prompt_infinite_values_of_small_weights(d, dtype, gap, queries, rows, page_rows, batch):
+    for top, odd in ((0, rows - queries), (rows - queries, 0), (rows - queries - 1, 1)):
+        q, k, v = infinite_values(dtype, rows, d, gap, top, odd)
+        q = q.expand(queries, 4, d).contiguous()
+        want, size = attend(q, k, v, torch.arange(rows - queries, rows), LN2)
+        got = run_prompt(dtype, q, k, v, [queries], [rows], scale=LN2, page_rows=page_rows, batch=batch)
+        fine = same_kind(got, want)
+        assert torch.isinf(want).any() and torch.isnan(want).any()
+        check(torch.where(fine, got, 0), torch.where(fine, want, 0), torch.where(fine, size, 0), dtype, True)
+
+
+@pytest.mark.parametrize("queries,rows", [(30, 70), (5, 1600)])
+def test_prompt_infinite_value_under_a_score_of_minus_infinity(queries, rows):
+    """0 times infinity, as the formula has it, for the queries that see the key, at every place of a block."""
+    g = gen(10)
+    q, k, v = randn(g, "bf16", queries, 2, 64).abs(), randn(g, "bf16", rows, 1, 64), randn(g, "bf16", rows, 1, 64)
+    for i, key in enumerate((0, 3, 5, 14, 22, 31, 32, 45, 63, rows - 2)):
+        k[key], v[key, 0, 5 + i], v[key, 0, 40] = -math.inf, -math.inf if i % 2 else math.inf, math.inf
+        v[key + 1, 0, 30 + i] = math.inf
+    want, _ = attend(q, k, v, torch.arange(rows - queries, rows), 0.125)
+    same_kind(run_prompt("bf16", q, k, v, [queries], [rows]), want)
