@@ -9,7 +9,7 @@
 enum { kNoDefer = 0, kDeferSlices = 1, kDeferShares = 2, kPushShares = 3, kPushSlices = 4 };
 constexpr bool defer_pushes(int defer) { return defer == kPushShares || defer == kPushSlices; }
 constexpr bool defer_slices(int defer) { return defer == kDeferSlices || defer == kPushSlices; }
-constexpr uint32_t kLLTag = 0x4C4C5701u;      // marks a pushed word as written by the running launch's helper
+constexpr uint32_t kLLTag = 0x7FA54C57u;      // marks a pushed word as written by the running launch's helper (a signalling NaN, as kSplitTag)
 WSVD_DEV unsigned long long ll_word(float v) { return ((unsigned long long)kLLTag << 32) | (unsigned long long)__float_as_uint(v); }
 template <int DEFER>
 WSVD_DEV void append_defer_out(const AppendParams& p, size_t i, float v) {

@@ -237,7 +237,9 @@ WSVD_DEV void compute_qtilde(const AttnParams& p, const void* bk_lds, const floa
 // area is all zeros between launches.
 // Returns false in the workgroups that only delivered a partial (they are done); true in the one that now holds the
 // whole sequence's (m, l, u) in Msh, Lsh, Ush, visible to all of its threads.
-constexpr uint32_t kSplitTag = 0x53504C54u;
+// The tag is a signalling NaN: no sum or product that another launch leaves in the workspace has its bits (arithmetic makes quiet ones, and
+// one that came through from a 16-bit number has its low bits 0).
+constexpr uint32_t kSplitTag = 0x7FA5504Du;
 WSVD_DEV unsigned long long split_word(float v) { return ((unsigned long long)kSplitTag << 32) | (unsigned long long)__float_as_uint(v); }
 
 template <int R, int NT = 0>

@@ -23,7 +23,6 @@
 // (16 x 2048: 0.57, keys and values no longer stay in the L2); lines of later blocks fetched to the L2 ahead.
 #include <algorithm>
 #include <type_traits>
-#include "wsvd_append_split.h"
 #include "wsvd_attn_common.h"
 #include "wsvd_dense.h"
 
@@ -107,11 +106,6 @@ WSVD_DEV bool prompt_place(const DensePromptParams& p, int idx, int lane, Prompt
 }
 WSVD_DEV float* prompt_part(const DensePromptParams& p, int idx, int kv, int split, int rows, int d) {
   return p.parts + (((size_t)idx * p.Hkv + kv) * p.splits + split) * rows * (d + 2);
-}
-// Partial results lie where other launches hand over words {value, tag}, and stay there: none of them may look like a tag.
-WSVD_DEV float no_tag(float v) {
-  const uint32_t u = __float_as_uint(v);
-  return __uint_as_float(u == kSplitTag || u == kLLTag ? u ^ 1u : u);
 }
 
 template <class T, int D, bool PAGED, int NW>
@@ -502,14 +496,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     if (at.splits > 1) {                             // a part: as it is, for k_dense_prompt_join
       float* const part = prompt_part(p, idx, kv, split, ROWS, D);
       const int i0 = anew(lane), half = i0 >> 5, r = 32 * wave + (i0 & 31);
-      const float sum = no_tag(halves_sum(l[0] + l[1]));
-      if (half == 0) { part[2 * r] = no_tag(m); part[2 * r + 1] = sum; }
+      const float sum = halves_sum(l[0] + l[1]);
+      if (half == 0) { part[2 * r] = m; part[2 * r + 1] = sum; }
 #pragma unroll
       for (int d = 0; d < ND; d++)
 #pragma unroll
         for (int g = 0; g < 4; g++)
           *(v4f*)(part + 2 * ROWS + r * D + 32 * d + 8 * g + 4 * half) =
-              v4f{no_tag(o[d][4 * g]), no_tag(o[d][4 * g + 1]), no_tag(o[d][4 * g + 2]), no_tag(o[d][4 * g + 3])};
+              v4f{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
       break;
     }
     // The output from the accumulators, 16 bytes a lane: the halves of a wave have 4 of 8 dims each, and swap so that the first half

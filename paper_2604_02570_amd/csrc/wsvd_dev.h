@@ -270,7 +270,8 @@ WSVD_DEV size_t a_packed_offset(int kv, int j, int e, int rank, int d_model) {
 // partial sums of the sliced append kernels, which the decode step's projection launch uses for its slices too (followed
 // by its one pending word per sequence); no invariant there: written before read.  The dense layers' calls use the area behind the
 // counters as well: the decode attention for words of the same kind and tag, cleared by their consumer, the prompt attention for
-// plain partial results, none of which has the bits of a tag.
+// plain partial results.  Tags are signalling NaNs, which no fp32 sum, maximum or product is: whoever waits for words takes nothing
+// for one that other calls, of this layer or another, have left there.
 // ints [0, batch) of [0, 8192): per sequence, workgroups that have read its length (one-launch decode steps) or have finished
 // (the store-and-attend launch), zero between launches; [8192, 12288): append tickets; [12288, 16000): fused-step row flags
 // (2*Hkv, hold the epoch of the last step); [16000]: fused-step finished-workgroup counter.

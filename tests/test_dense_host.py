@@ -194,3 +194,16 @@ def test_pages_and_work_division(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-I", CSRC, str(source), "-o", str(program)], check=True)
     r = subprocess.run([str(program)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+def test_tags_of_words_are_no_sum():
+    """Plain fp32 sums of other calls lie where a call waits for tagged words: a tag is a signalling NaN, which arithmetic never makes,
+    with low bits set, which a NaN that came from 16 bits has not."""
+    import re
+    tags = []
+    for name, constant in (("wsvd_attn_common.h", "kSplitTag"), ("wsvd_append_split.h", "kLLTag")):
+        with open(os.path.join(CSRC, name)) as f:
+            tags.append(int(re.search(r"constexpr uint32_t %s = (0x[0-9A-Fa-f]+)u" % constant, f.read()).group(1), 16))
+    assert len(set(tags)) == 2
+    for tag in tags:
+        assert tag >> 23 & 0xFF == 0xFF and not tag >> 22 & 1 and tag & 0x1FFF

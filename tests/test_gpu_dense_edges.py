@@ -244,3 +244,86 @@ def test_prompt_infinite_value_under_a_score_of_minus_infinity(queries, rows):
         v[key + 1, 0, 30 + i] = math.inf
     want, _ = attend(q, k, v, torch.arange(rows - queries, rows), 0.125)
     same_kind(run_prompt("bf16", q, k, v, [queries], [rows]), want)
+
+
+# ------------------------------------------------------------------------------------------------ what is left in the workspace
+def left_behind(L, pattern):
+    """The area behind the counters as another layer's plain 32-bit sums may leave it."""
+    words = L.ws.view(torch.int32)
+    words[16384:] = pattern
+
+
+# 32-bit numbers of every kind that a sum can be
+@pytest.mark.parametrize("pattern", [0x53504C54, 0x4C4C5701, 0x3F800000, -0x40000000, 0x7F800000, 0x7FC00000, -1 << 22, 1])
+def test_decode_over_what_sums_leave_in_the_workspace(pattern):
+    g = gen(41)
+    hq, hkv, d, rows = 4, 2, 64, 3000
+    q, k, v = randn(g, "bf16", 1, hq, d), randn(g, "bf16", rows, hkv, d), randn(g, "bf16", rows, hkv, d)
+    want, size = attend_fast(q, k, v, [rows - 1], d ** -0.5)
+    L = Layer(1, hq, hkv, d, "bf16")
+    left_behind(L, pattern)
+    for _ in range(2):
+        check(run_decode("bf16", q, [k], [v], L=L), want, size, "bf16", False)
+    L.close()
+
+
+@pytest.mark.parametrize("name,over", [("c3_small", dict(context=1500, batch=2)), ("c4_small", dict()), ("c2_small", dict(context=900)), ("c1", dict())])
+def test_one_workspace_serves_latent_and_dense_layers_in_turn(name, over):
+    """Latent appends, split attention and decode steps between dense prompts whose tiles are shared and dense decode calls that are cut, on
+    one context: the latent calls as on a context of their own, bit for bit, the dense ones against the formula."""
+    import wsvd_inputs as WI
+    from cases import build_case
+    from harness import as_dtype_dev, q_to_device
+    from test_gpu_parity import layer_for
+    c = build_case(name, extra_cap=128, **over)
+    sp = c.sp
+    alone, shared = layer_for(c), layer_for(c)
+    g = gen(51)
+    hq, hkv, d, rows, tokens = 4, 1, 128, 2600, 9
+    k, v, q = randn(g, "bf16", rows, hkv, d), randn(g, "bf16", rows, hkv, d), randn(g, "bf16", tokens, hq, d)
+    want, size = attend_fast(q, k, v, torch.arange(rows - tokens, rows), d ** -0.5)
+    desc = W.dense_desc(1, hq, hkv, d, "bf16")
+    shared.ws = torch.empty(max(W.wsvd_dense_workspace_bytes(desc), shared.ws.numel()), dtype=torch.uint8, device="cuda")
+    W.wsvd_set_workspace(shared.ctx, shared.ws)
+    pool = Pool(gen(17), [rows], hkv, d, 16, "bf16", fill_rows=False)
+    pool.put(0, 0, k, v)
+    kd, vd, lens, table, qd, cu = pool.k.cuda(), pool.v.cuda(), torch.tensor([rows], dtype=torch.int32).cuda(), pool.table.cuda(), q.cuda(), prefix([tokens]).cuda()
+    cache = W.make_paged_cache(kd, vd, None, None, lens, table, 16, pool.max_pages, pool.n_pages)
+    many, one = (torch.empty(n, hq, d, dtype=torch.bfloat16, device="cuda") for n in (tokens, 1))
+    x = as_dtype_dev(WI.bf16_exact(c.x_new[0]) if sp.factor_dtype == "bf16" else c.x_new[0], sp.factor_dtype)
+    ql, qs, _ = q_to_device(c.q32[0], sp.q_dtype)
+    B = [as_dtype_dev(b, sp.factor_dtype) for b in (c.BK, c.BV)]
+    A = {}
+    for L in (alone, shared):
+        L.upload(c.cache)
+        A[L] = [L.pack_A(a, sp.factor_dtype) for a in (c.AK, c.AV)]
+
+    def dense():
+        many.zero_(), one.zero_()
+        W.wsvd_dense_prefill_attn_paged(shared.ctx, desc, qd, hq * d, tokens, cu, cache, many, hq * d)
+        W.wsvd_dense_decode_attn_paged(shared.ctx, desc, qd[tokens - 1:], hq * d, cache, rows, one)
+        W.wsvd_dense_prefill_attn_paged(shared.ctx, desc, qd, hq * d, tokens, cu, cache, many, hq * d)
+        check(many.cpu(), want, size, "bf16", True)
+        check(one.cpu(), want[tokens - 1:], size[tokens - 1:], "bf16", False)
+
+    longest = int(c.lens.max())
+    for i in range(4):
+        outs = []
+        for L in (alone, shared):
+            W.wsvd_ctx_set_option(L.ctx, "step_launches", 0 if i % 2 else 2)
+            if L is shared:
+                dense()
+            assert L.append(x, None, *A[L]) == 0
+            if L is shared:
+                dense()
+            o = [L.attend(ql, qs, *B, longest + 2 * i + 1)]
+            if L is shared:
+                dense()
+            got, st = L.step(x, *A[L], ql, qs, *B, longest + 2 * i + 2)
+            assert st == 0, W.status_str(st)
+            outs.append(o + [got])
+        for a, b in zip(*outs):
+            assert (a == b).all(), i
+        for a, b in ((alone.k_codes, shared.k_codes), (alone.v_codes, shared.v_codes)):
+            assert torch.equal(a, b)
+    alone.close(), shared.close()
