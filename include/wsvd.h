@@ -488,6 +488,8 @@ wsvd_status wsvd_linear_w4a8_split(wsvd_ctx *ctx, const int8_t *x, const void *x
  *           nothing there, an attention reads page 0 in its place.
  *   Packed sequences   cu_*[batch + 1] (DEVICE): tokens of sequence b are [cu[b], cu[b + 1]), any number of them, also none.
  *           Packed tokens from cu[batch] on belong to nobody: nothing is written for them.
+ *   Sizes   A call is a launch of fewer than 2^32 threads, which batch * n_kv_heads up to 2^22 and n_q * n_q_heads up to 2^30 always
+ *           are; an attention that would need more is refused (WSVD_E_SHAPE).
  */
 typedef struct {
   int32_t batch, n_q_heads, n_kv_heads, d_head;

@@ -519,11 +519,8 @@ hipError_t launch_append_form(const DenseAppendParams& p, hipStream_t s) {
 }
 template <class T, int D>
 hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
-  // Tokens of a workgroup: as few as give its 256 threads work, one where there are few (16 x ~1700 tokens of 16 / 2 heads of 64: 4
-  // tokens 50 us, 1 token 74; 16 x 2048 of 28 / 4 heads of 128: 124 and 104).
-  const int items = (p.Hq + 2 * p.Hkv) * (D / 16);
-  if (p.n_tokens < 2048 || items >= 256) return launch_append_form<T, D, 1>(p, s);
-  return items >= 128 ? launch_append_form<T, D, 2>(p, s) : launch_append_form<T, D, 4>(p, s);
+  const int tokens = dense_append_tokens(p.n_tokens, (p.Hq + 2 * p.Hkv) * (D / 16));
+  return tokens == 1 ? launch_append_form<T, D, 1>(p, s) : tokens == 2 ? launch_append_form<T, D, 2>(p, s) : launch_append_form<T, D, 4>(p, s);
 }
 template <class T, int D, int NW, bool ONCE>
 hipError_t launch_decode_form(const DenseDecodeParams& p, hipStream_t s) {
@@ -533,7 +530,7 @@ hipError_t launch_decode_form(const DenseDecodeParams& p, hipStream_t s) {
     const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode<T, D, NW, ONCE>, LDS);
     if (e != hipSuccess) return e;
   }
-  k_dense_decode<T, D, NW, ONCE><<<(p.alone ? p.B : p.target + p.B) * p.Hkv, 64 * NW, LDS, s>>>(p);
+  k_dense_decode<T, D, NW, ONCE><<<(unsigned)dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0), 64 * NW, LDS, s>>>(p);
   return hipGetLastError();
 }
 template <class T, int D, bool ONCE>

@@ -104,10 +104,8 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   if (max_seq_len < 0) return WSVD_E_SHAPE;
   if (max_seq_len > (int64_t)cache->max_pages * cache->page_rows) return WSVD_E_CAPACITY;
   if ((int64_t)max_seq_len * desc->batch > ((int64_t)1 << 37)) return WSVD_E_SHAPE;      // (units of 128 rows are counted in 32 bits)
-  WSVD_TRY(check_workspace(ctx, desc));
   DenseDecodeParams p = {};
   p.q = (const uint16_t*)q; p.q_ld = q_ld; p.out = (uint16_t*)out; p.pages = pages_of(cache);
-  p.parts = (unsigned long long*)((int*)ctx->ws + kWsCounterInts);
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads;
   p.max_len = max_seq_len; p.waves = dense_waves(p.B, p.Hkv, max_seq_len);
   p.target = dense_target(p.waves, p.Hkv);
@@ -115,6 +113,9 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   p.alone_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : 5 * 128 / desc->d_head;
   p.min_units = ctx->opt.min_chunk ? p.alone_units : 2 * 128 / desc->d_head;
   p.alone = dense_units_of(max_seq_len) <= p.alone_units;
+  if (!dense_launchable(dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0), 64 * p.waves)) return WSVD_E_SHAPE;
+  WSVD_TRY(check_workspace(ctx, desc));
+  p.parts = (unsigned long long*)((int*)ctx->ws + kWsCounterInts);
   p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
   return launched(wsvd_launch_dense_decode(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
 }
@@ -140,6 +141,7 @@ wsvd_status wsvd_dense_prefill_attn(wsvd_ctx* ctx, const wsvd_dense_desc* desc, 
   p.q_ld = q_ld; p.k_ld = k_ld; p.v_ld = v_ld; p.out_ld = out_ld;
   p.cu_q = cu_q; p.cu_kv = cu_kv ? cu_kv : cu_q;
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads; p.causal = causal;
+  if (!dense_launchable(dense_prompt_grid(n_q, p.B, p.Hkv, p.G, causal != 0).workgroups, 256)) return WSVD_E_SHAPE;
   WSVD_TRY(check_workspace(ctx, desc));
   p.parts = (float*)ctx->ws + kWsCounterInts;
   p.n_q = (int)n_q; p.n_kv = (int)n_kv; p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
@@ -162,6 +164,7 @@ wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* 
   p.q = (const uint16_t*)q; p.out = (uint16_t*)out; p.q_ld = q_ld; p.out_ld = out_ld;
   p.cu_q = cu_q; p.pages = pages_of(cache);
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads; p.causal = 1;
+  if (!dense_launchable(dense_prompt_grid(n_q, p.B, p.Hkv, p.G, true).workgroups, 256)) return WSVD_E_SHAPE;
   WSVD_TRY(check_workspace(ctx, desc));
   p.parts = (float*)ctx->ws + kWsCounterInts;
   p.n_q = (int)n_q; p.c_scale = scale_of(desc); p.err_word = ctx->err_word;

@@ -74,5 +74,28 @@ WSVD_HD int dense_units(int total, int most, int B, int target, int alone_units,
 // A prompt of few tiles shares their keys out among several workgroups a tile: as many as fill the chip's two a CU.
 constexpr int kDensePromptParts = 512, kDensePromptRows = 128;
 
+// ---------------------------------------------------------------- launches
+// A launch has fewer than 2^32 threads.
+WSVD_HD bool dense_launchable(int64_t workgroups, int threads) { return workgroups < ((int64_t)1 << 32) / threads; }
+// Tokens of an append workgroup, `items` = 16-byte pairs of a token: as few as give its 256 threads work, one where there are few (16 x ~1700
+// tokens of 16 / 2 heads of 64: 4 tokens 50 us, 1 token 74; 16 x 2048 of 28 / 4 heads of 128: 124 and 104), and two where that many workgroups
+// of one are no launch.
+WSVD_HD int dense_append_tokens(int64_t n_tokens, int items) {
+  if (n_tokens < 2048 || (items >= 256 && dense_launchable(n_tokens, 256))) return 1;
+  return items >= 128 ? 2 : 4;
+}
+WSVD_HD int64_t dense_decode_workgroups(int B, int Hkv, int target, bool alone) { return (alone ? (int64_t)B : (int64_t)target + B) * Hkv; }
+// The prompt attention's, at most: every sequence ends inside a tile.  Two tiles a workgroup where there are many and they differ: the second
+// one's first keys and queries are asked for under the first one's last products, so that every other tile starts without a wait (16 x 2048
+// tokens, 32 heads of 128: 650 -> 632 us, 64 x 300, 32 / 8 heads: 129 -> 121, 4 x 4096 of 16 / 2 heads of 64: 166 -> 158; over 13 causal
+// calls of 2048 to 5920 tiles 0.93 to 1.04 of the time, 0.98 on average).  With fewer tiles the last round of workgroups costs more (1283
+// ragged tiles: 73 -> 81 us), and without a mask all tiles cost the same already.
+struct DensePromptGrid { int64_t workgroups; bool pairs; };
+WSVD_HD DensePromptGrid dense_prompt_grid(int64_t n_q, int B, int Hkv, int G, bool causal) {
+  const int64_t tiles = n_q * G / kDensePromptRows + B;
+  const bool pairs = causal && tiles * Hkv >= 2048;
+  return {(pairs ? (tiles + B) / 2 : tiles) * Hkv, pairs};
+}
+
 // A workgroup's share of a tile's n blocks, one of `splits`: [dense_share(split), dense_share(split + 1)).
 WSVD_HD int dense_share(int split, int n, int splits) { return (int)((int64_t)split * n / splits); }

@@ -593,15 +593,10 @@ __global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) 
 template <class T, int D, bool PAGED>
 hipError_t launch(DensePromptParams& p, hipStream_t s) {
   constexpr int NW = 4, ROWS = 32 * NW;
-  int64_t tiles = ((int64_t)p.n_q * p.G) / ROWS + p.B;           // at most: every sequence ends inside a tile
-  // Two tiles a workgroup where there are many and they differ: the second one's first keys and queries are asked for under the first
-  // one's last products, so that every other tile starts without a wait (16 x 2048 tokens, 32 heads of 128: 650 -> 632 us, 64 x 300, 32 / 8
-  // heads: 129 -> 121, 4 x 4096 of 16 / 2 heads of 64: 166 -> 158; over 13 causal calls of 2048 to 5920 tiles 0.93 to 1.04 of the time, 0.98
-  // on average).  With fewer tiles the last round of workgroups costs more (1283 ragged tiles: 73 -> 81 us), and without a mask all
-  // tiles cost the same already.
-  p.pairs = p.causal && tiles * p.Hkv >= 2048;
-  if (p.pairs) tiles = (tiles + p.B) / 2;
-  const int64_t wgs = tiles * p.Hkv;
+  static_assert(ROWS == kDensePromptRows, "");
+  const DensePromptGrid grid = dense_prompt_grid(p.n_q, p.B, p.Hkv, p.G, p.causal != 0);
+  const int64_t wgs = grid.workgroups;
+  p.pairs = grid.pairs;
   // no sequence has more keys than there are, and no workgroup of several fewer than kLeastBlocks blocks of them
   const int64_t keys = PAGED ? (int64_t)p.pages.max_pages * p.pages.page_rows : p.n_kv;
   const int64_t most = std::min<int64_t>({32, kDensePromptParts / wgs, (keys + kKeys - 1) / kKeys / kLeastBlocks});

@@ -207,3 +207,74 @@ def test_tags_of_words_are_no_sum():
     assert len(set(tags)) == 2
     for tag in tags:
         assert tag >> 23 & 0xFF == 0xFF and not tag >> 22 & 1 and tag & 0x1FFF
+
+
+def test_calls_of_more_threads_than_a_launch_has_are_refused(ctx):
+    """2^32 threads: WSVD_E_SHAPE, not an error of the launch (and what fits gets as far as the workspace)."""
+    many, longer = dict(batch=65536, n_q_heads=128, n_kv_heads=128, d_head=64), dict(max_pages=200)
+    refuses(W.E_SHAPE, decode, ctx, desc(**many), cache(**longer), q_ld=8192, most=2000)
+    refuses(W.E_WORKSPACE, decode, ctx, desc(**many), cache(**longer), q_ld=8192, most=64)
+    refuses(W.E_WORKSPACE, decode, ctx, desc(**{**many, "n_q_heads": 64, "n_kv_heads": 64}), cache(**longer), q_ld=8192, most=2000)
+    refuses(W.E_SHAPE, decode, ctx, desc(**{**many, "n_q_heads": 1024, "n_kv_heads": 1024}), cache(), q_ld=65536, most=64)
+    wide = dict(n_q_heads=1024, n_kv_heads=64, d_head=64)
+    for f, kw in ((prompt, dict(k_ld=4096, v_ld=4096, n_kv=1 << 24)), (prompt, dict(k_ld=4096, v_ld=4096, n_kv=1 << 24, causal=0)), (chunk, {})):
+        refuses(W.E_SHAPE, f, ctx, desc(**wide), q_ld=65536, out_ld=65536, n_q=1 << 24, **kw)
+        refuses(W.E_WORKSPACE, f, ctx, desc(**wide), q_ld=65536, out_ld=65536, n_q=1 << 20, **{**kw, **({"n_kv": 1 << 20} if kw else {})})
+
+
+LAUNCHES = r"""
+#include "wsvd_dense_plan.h"
+#include <cstdio>
+#include <initializer_list>
+#define CHECK(x) do { if (!(x)) { std::printf("line %d: %s\n", __LINE__, #x); return 1; } } while (0)
+int main() {
+  CHECK(dense_launchable((1 << 24) - 1, 256) && !dense_launchable(1 << 24, 256) && dense_launchable((1 << 23) - 1, 512));
+  // appends of every size are a launch, and every token is in it
+  for (int64_t n = 1; n <= 1 << 24; n = n < 5000 ? n + 1 : n + n / 3 < 1 << 24 ? n + n / 3 : n < 1 << 24 ? 1 << 24 : n + 1)
+    for (int items : {12, 64, 127, 128, 255, 256, 400, 5000}) {
+      const int t = dense_append_tokens(n, items);
+      CHECK((t == 1 || t == 2 || t == 4) && dense_launchable((n + t - 1) / t, 256));
+      CHECK(n >= (1 << 24) || t == (n < 2048 || items >= 256 ? 1 : items >= 128 ? 2 : 4));
+    }
+  // what the interface promises to take
+  for (int Hkv = 1; Hkv <= 1024; Hkv *= 2)
+    for (int B = 1; B <= 65536 && (int64_t)B * Hkv <= 1 << 22; B = 2 * B + (B & 2)) {
+      for (int len : {0, 1024, 1025, 1 << 27}) {
+        const int waves = dense_waves(B, Hkv, len);
+        for (bool alone : {false, true}) CHECK(dense_launchable(dense_decode_workgroups(B, Hkv, dense_target(waves, Hkv), alone), 64 * waves));
+      }
+      for (int G = 1; G <= 16; G++)
+        if (G * Hkv <= 1024)
+          for (bool causal : {false, true}) {
+            const int64_t most = ((int64_t)1 << 30) / (G * Hkv), n = most < 1 << 24 ? most : 1 << 24;
+            CHECK(dense_launchable(dense_prompt_grid(n, B, Hkv, G, causal).workgroups, 256));
+          }
+    }
+  // enough workgroups for every division of the tokens among the sequences: two tiles a workgroup, or one
+  for (int B : {1, 2, 7, 300})
+    for (int G : {1, 3, 7, 16})
+      for (int Hkv : {1, 8})
+        for (int seed = 1; seed < 400; seed++) {
+          int64_t n = 0, one = 0, two = 0;
+          unsigned x = (unsigned)seed * 2654435761u;
+          for (int b = 0; b < B; b++) {
+            x = x * 1664525u + 1013904223u;
+            const int64_t len = (x >> 8) % (seed % 3 ? 40 : 3000), tiles = (len * G + 127) / 128;
+            n += len; one += tiles; two += (tiles + 1) / 2;
+          }
+          for (bool causal : {false, true}) {
+            const DensePromptGrid g = dense_prompt_grid(n, B, Hkv, G, causal);
+            CHECK(g.workgroups >= (g.pairs ? two : one) * Hkv);
+          }
+        }
+  return 0;
+}
+"""
+
+
+def test_launches_hold_their_work(tmp_path):
+    source, program = tmp_path / "launches.cpp", tmp_path / "launches"
+    source.write_text(LAUNCHES)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-I", CSRC, str(source), "-o", str(program)], check=True)
+    r = subprocess.run([str(program)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
