@@ -478,7 +478,8 @@ wsvd_status wsvd_linear_w4a8_split(wsvd_ctx *ctx, const int8_t *x, const void *x
  *   dtype   BF16 or F16: queries, keys, values and outputs.  Scores, softmax statistics and sums are fp32.
  *   Heads   n_q_heads / n_kv_heads in 1..16, d_head 64 or 128, at most 1024 query heads.
  *   Rows    packed tensors are [tokens][ld] with a token's heads side by side from the pointer on; ld in elements, a multiple
- *           of 8, at least heads * d_head (so the three parts of one projection's output can be passed as they lie).
+ *           of 8, at least heads * d_head (so the three parts of one projection's output can be passed as they lie).  Of no
+ *           tokens (a call with none does nothing) they may be NULL.
  *   Cache   wsvd_paged_cache with k_codes / v_codes the pools [n_pages][n_kv_heads][page_rows][d_head] of dtype, k_meta /
  *           v_meta unused (may be NULL); page_rows a multiple of 16, at most 4096, max_pages * page_rows at most 2^27.
  *           seq_lens[b] = rows of sequence b, the tokens of the call COUNTED; these entry points only read it (a caller that

@@ -26,8 +26,9 @@ wsvd_status check_pages(const wsvd_paged_cache* c) {
   return WSVD_OK;
 }
 
-// a token's heads lie side by side; tokens ld elements apart, in whole 16-byte pieces
-wsvd_status check_rows(const void* p, int64_t ld, int64_t width) {
+// a token's heads lie side by side; tokens ld elements apart, in whole 16-byte pieces.  Tensors of no tokens may have no memory.
+wsvd_status check_rows(const void* p, int64_t ld, int64_t width, int64_t n) {
+  if (n == 0 && !p) return WSVD_OK;
   if (!p) return WSVD_E_NULL;
   if (ld < width || ld > kMostLd) return WSVD_E_SHAPE;
   if (!aligned16(p) || ld % 8 != 0) return WSVD_E_ALIGN;
@@ -73,16 +74,16 @@ wsvd_status wsvd_dense_append_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, 
   WSVD_TRY(check_desc(desc));
   WSVD_TRY(check_pages(cache));
   const int64_t wq = (int64_t)desc->n_q_heads * desc->d_head, wkv = (int64_t)desc->n_kv_heads * desc->d_head;
-  if (!q != !q_out) return WSVD_E_NULL;
+  if (!q != !q_out && n_tokens != 0) return WSVD_E_NULL;
   if (q) {
-    WSVD_TRY(check_rows(q, q_ld, wq));
-    WSVD_TRY(check_rows(q_out, q_out_ld, wq));
+    WSVD_TRY(check_rows(q, q_ld, wq, n_tokens));
+    WSVD_TRY(check_rows(q_out, q_out_ld, wq, n_tokens));
     if (q == q_out && q_ld != q_out_ld) return WSVD_E_SHAPE;
   }
-  WSVD_TRY(check_rows(k, k_ld, wkv));
-  WSVD_TRY(check_rows(v, v_ld, wkv));
+  WSVD_TRY(check_rows(k, k_ld, wkv, n_tokens));
+  WSVD_TRY(check_rows(v, v_ld, wkv, n_tokens));
   if (k_out) {
-    WSVD_TRY(check_rows(k_out, k_out_ld, wkv));
+    WSVD_TRY(check_rows(k_out, k_out_ld, wkv, n_tokens));
     if (k == k_out && k_ld != k_out_ld) return WSVD_E_SHAPE;
   }
   if (!aligned4(cu_tokens) || !aligned4(positions) || ((uintptr_t)inv_freq & 7u)) return WSVD_E_ALIGN;
@@ -99,7 +100,7 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   if (!ctx || !out) return WSVD_E_NULL;
   WSVD_TRY(check_desc(desc));
   WSVD_TRY(check_pages(cache));
-  WSVD_TRY(check_rows(q, q_ld, (int64_t)desc->n_q_heads * desc->d_head));
+  WSVD_TRY(check_rows(q, q_ld, (int64_t)desc->n_q_heads * desc->d_head, desc->batch));
   if (!aligned16(out)) return WSVD_E_ALIGN;
   if (max_seq_len < 0) return WSVD_E_SHAPE;
   if (max_seq_len > (int64_t)cache->max_pages * cache->page_rows) return WSVD_E_CAPACITY;
@@ -126,12 +127,12 @@ wsvd_status wsvd_dense_prefill_attn(wsvd_ctx* ctx, const wsvd_dense_desc* desc, 
   if (!ctx || !cu_q) return WSVD_E_NULL;
   WSVD_TRY(check_desc(desc));
   const int64_t wq = (int64_t)desc->n_q_heads * desc->d_head, wkv = (int64_t)desc->n_kv_heads * desc->d_head;
-  WSVD_TRY(check_rows(q, q_ld, wq));
+  WSVD_TRY(check_rows(q, q_ld, wq, n_q));
   if (n_kv != 0) {                                   // (without keys there may be no tensors)
-    WSVD_TRY(check_rows(k, k_ld, wkv));
-    WSVD_TRY(check_rows(v, v_ld, wkv));
+    WSVD_TRY(check_rows(k, k_ld, wkv, n_kv));
+    WSVD_TRY(check_rows(v, v_ld, wkv, n_kv));
   }
-  WSVD_TRY(check_rows(out, out_ld, wq));
+  WSVD_TRY(check_rows(out, out_ld, wq, n_q));
   if (!aligned4(cu_q) || !aligned4(cu_kv)) return WSVD_E_ALIGN;
   if (n_q < 0 || n_q > kMostTokens || n_kv < 0 || n_kv > kMostRows || (!cu_kv && n_kv != n_q)) return WSVD_E_SHAPE;
   if (causal != 0 && causal != 1) return WSVD_E_SHAPE;
@@ -155,8 +156,8 @@ wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* 
   WSVD_TRY(check_desc(desc));
   WSVD_TRY(check_pages(cache));
   const int64_t wq = (int64_t)desc->n_q_heads * desc->d_head;
-  WSVD_TRY(check_rows(q, q_ld, wq));
-  WSVD_TRY(check_rows(out, out_ld, wq));
+  WSVD_TRY(check_rows(q, q_ld, wq, n_q));
+  WSVD_TRY(check_rows(out, out_ld, wq, n_q));
   if (!aligned4(cu_q)) return WSVD_E_ALIGN;
   if (n_q < 0 || n_q > kMostTokens) return WSVD_E_SHAPE;
   if (n_q == 0) return WSVD_OK;

@@ -278,3 +278,18 @@ def test_launches_hold_their_work(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-I", CSRC, str(source), "-o", str(program)], check=True)
     r = subprocess.run([str(program)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+def test_calls_without_tokens_take_tensors_without_memory(ctx):
+    """An empty tensor has no address: such calls have nothing to do, as with any other address."""
+    append(ctx, n=0, cu=A, q=0, k=0, v=0, q_out=0, k_out=0)
+    append(ctx, n=0, cu=A, q=None, k=None, v=None, q_out=None, k_out=None)
+    append(ctx, n=0, cu=A, q=0, k=0, v=0, q_out=A, k_out=A)
+    prompt(ctx, n_q=0, n_kv=0, q=0, k=0, v=0, out=0)
+    prompt(ctx, n_q=0, n_kv=7, q=0, out=0, cu_kv=A)
+    chunk(ctx, n_q=0, q=0, out=0)
+    refuses(W.E_NULL, prompt, ctx, n_q=0, n_kv=7, q=0, out=0, k=0, cu_kv=A)
+    for f, kw in ((append, dict(n=0, cu=A, k=A + 8)), (prompt, dict(n_q=0, n_kv=0, q=A + 2)), (chunk, dict(n_q=0, out=A + 8))):
+        refuses(W.E_ALIGN, f, ctx, **kw)
+    for f in (prompt, chunk):
+        refuses(W.E_NULL, f, ctx, n_q=0, cu_q=None, **({"n_kv": 0} if f is prompt else {}))
