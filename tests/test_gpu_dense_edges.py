@@ -1,12 +1,12 @@
-"""Dense-layer attention on the GPU where single numbers decide: weights far below the largest, infinite values and scores, what other
-calls left in the workspace; against plain 64-bit forms."""
+"""Dense-layer operators on the GPU where single numbers decide: weights far below the largest, infinite values and scores, what other
+calls left in the workspace; and the forms that only large calls take.  Against plain 64-bit forms."""
 import math
 
 import pytest
 import torch
 
 import paper_2604_02570_amd as W
-from dense_ref import DTYPES, F64, Pool, attend, attend_fast, check, prefix, randn
+from dense_ref import DTYPES, F64, Pool, attend, attend_fast, check, half_step, prefix, randn, rotate
 from test_gpu_dense import Layer, gen
 
 pytestmark = pytest.mark.gpu
@@ -327,3 +327,76 @@ def test_one_workspace_serves_latent_and_dense_layers_in_turn(name, over):
         for a, b in ((alone.k_codes, shared.k_codes), (alone.v_codes, shared.v_codes)):
             assert torch.equal(a, b)
     alone.close(), shared.close()
+
+
+# ------------------------------------------------------------------------------------------------ forms that large calls take
+def large_append(hq, hkv, d, dtype, before, new, page_rows, ld_extra=0):
+    """Every token of a large append against the rotation in 64 bits; rows of nobody stay as they were."""
+    g, T, B = gen(sum(new) + d), sum(new), len(new)
+    L = Layer(B, hq, hkv, d, dtype)
+    pool = Pool(g, [a + n for a, n in zip(before, new)], hkv, d, page_rows, dtype, fill_rows=False)
+    cache = L.cache(pool)
+    ld = (hq + 2 * hkv) * d + ld_extra
+    x = randn(g, dtype, T, ld)
+    inv = 10000.0 ** (-torch.arange(0, d, 2, dtype=F64) / d)
+    q_out, k_out = (torch.full((T, h * d + 8), 7.0, dtype=DTYPES[dtype], device="cuda") for h in (hq, hkv))
+    xd = x.cuda()
+    W.wsvd_dense_append_paged(L.ctx, L.desc, xd, ld, xd[:, hq * d:], ld, xd[:, (hq + hkv) * d:], ld, T, prefix(new).cuda(), None, inv.cuda(),
+                              q_out, hq * d + 8, k_out, hkv * d + 8, cache)
+    y = x[:, : (hq + 2 * hkv) * d].view(T, hq + 2 * hkv, d)
+    b = torch.repeat_interleave(torch.arange(B), torch.tensor(new))
+    pos = torch.tensor(before)[b] + torch.arange(T) - prefix(new).long()[b]
+    want = rotate(y[:, :hq + hkv], pos, inv)
+    pair = torch.hypot(want[..., : d // 2], want[..., d // 2:]).repeat(1, 1, 2)
+    # the result's rounding, and fp32 products of a pair: 3 roundings of at most sqrt(2) times the pair's length
+    tol = half_step(dtype) * want.abs() + 2.0 ** -21 * pair + (2.0 ** -25 if dtype == "f16" else 0)
+    near = lambda got, part: bool(((got.to(F64) - want[:, part]).abs() <= tol[:, part]).all())
+    assert near(q_out[:, : hq * d].cpu().view(T, hq, d), slice(0, hq))
+    assert near(k_out[:, : hkv * d].cpu().view(T, hkv, d), slice(hq, hq + hkv))
+    assert (q_out[:, hq * d:] == 7).all() and (k_out[:, hkv * d:] == 7).all()
+    page, row = pool.table[b, pos // page_rows].long(), pos % page_rows
+    k, v = L.k.cpu(), L.v.cpu()
+    assert near(k[page, :, row], slice(hq, hq + hkv)) and torch.equal(v[page, :, row], y[:, hq + hkv:])
+    touched = torch.zeros(k.shape[0], page_rows, dtype=torch.bool)
+    touched[page, row] = True
+    for x in (k, v):
+        assert torch.isnan(x.transpose(1, 2)[~touched]).all()
+    L.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,tokens", [
+    (16, 2, 128, "bf16", 2307),                 # two tokens a workgroup
+    (16, 2, 128, "f16", 9901),                  # the same, past the caches
+    (28, 4, 128, "bf16", 2049),                 # one token, within them
+    (32, 32, 128, "bf16", 2113),                # one token, past them
+    (32, 32, 64, "f16", 4501),
+    (4, 2, 64, "f16", 2050),                    # four tokens
+    (4, 2, 64, "bf16", 48901),                  # four tokens, past the caches
+])
+def test_append_forms_of_large_calls(hq, hkv, d, dtype, tokens):
+    part = [tokens // 7, 0, tokens // 3 + 1, 1]
+    large_append(hq, hkv, d, dtype, [5, 90, 0, 333, 18], part + [tokens - sum(part)], 48, ld_extra=8)
+
+
+@pytest.mark.parametrize("min_chunk", [0, 128])
+def test_decode_gives_a_sequence_the_same_bits_in_every_place(min_chunk):
+    """The same sequences in another order, in other pages: their outputs move with them, bit for bit."""
+    g = gen(3)
+    hq, hkv, d, lens = 8, 2, 128, [900, 3000, 17, 0, 1300, 1, 640]
+    q, k, v = randn(g, "bf16", len(lens), hq, d), [randn(g, "bf16", n, hkv, d) for n in lens], [randn(g, "bf16", n, hkv, d) for n in lens]
+    first = run_decode("bf16", q, k, v, min_chunk=min_chunk)
+    for order in ([6, 5, 4, 3, 2, 1, 0], [2, 0, 5, 1, 6, 3, 4]):
+        again = run_decode("bf16", q[order], [k[i] for i in order], [v[i] for i in order], min_chunk=min_chunk, page_rows=32)
+        assert torch.equal(again, first[order])
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,nq,nk,page_rows,batch", [
+    (4, 4, 128, "bf16", [700, 3, 257], [700, 3, 257], 0, 0), (28, 4, 128, "bf16", [333, 90], [1834, 400], 16, 0),
+    (8, 1, 64, "f16", [5, 70], [2600, 1200], 16, 0), (2, 1, 128, "f16", [300, 129, 511], [300, 129, 511], 0, 2100)])
+def test_prompts_repeat_themselves_bit_for_bit(hq, hkv, d, dtype, nq, nk, page_rows, batch):
+    """Whole tiles, shared ones, two a workgroup: nothing depends on which workgroup comes first."""
+    g = gen(4)
+    q, k, v = randn(g, dtype, sum(nq), hq, d), randn(g, dtype, sum(nk), hkv, d), randn(g, dtype, sum(nk), hkv, d)
+    first = run_prompt(dtype, q, k, v, nq, nk, page_rows=page_rows, batch=batch)
+    for _ in range(3):
+        assert torch.equal(run_prompt(dtype, q, k, v, nq, nk, page_rows=page_rows, batch=batch), first)
