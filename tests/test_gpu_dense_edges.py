@@ -400,3 +400,22 @@ def test_prompts_repeat_themselves_bit_for_bit(hq, hkv, d, dtype, nq, nk, page_r
     first = run_prompt(dtype, q, k, v, nq, nk, page_rows=page_rows, batch=batch)
     for _ in range(3):
         assert torch.equal(run_prompt(dtype, q, k, v, nq, nk, page_rows=page_rows, batch=batch), first)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16")])
+def test_infinite_values_change_no_other_output(d, dtype):
+    """With and without them: other dims, other heads and queries that do not see them come out with the same bits."""
+    g = gen(61)
+    rows, queries = 700, 150
+    q, k, v = randn(g, dtype, queries, 4, d), randn(g, dtype, rows, 2, d), randn(g, dtype, rows, 2, d)
+    odd = v.clone()
+    key = rows - queries + 60                                      # the first 60 queries do not see it
+    odd[key, 1, 3], odd[key, 1, 9], odd[key, 1, d - 1] = math.inf, math.nan, -math.inf
+    touched = torch.zeros(queries, 4, d, dtype=torch.bool)
+    touched[60:, 2:, 3], touched[60:, 2:, 9], touched[60:, 2:, d - 1] = True, True, True
+    for page_rows in (0, 16):
+        plain, other = (run_prompt(dtype, q, k, x, [queries], [rows], page_rows=page_rows) for x in (v, odd))
+        assert torch.equal(plain[~touched], other[~touched]) and not torch.isfinite(other[touched]).any()
+    for min_chunk in (0, 128):
+        plain, other = (run_decode(dtype, q[-1:], [k], [x], min_chunk=min_chunk) for x in (v, odd))
+        assert torch.equal(plain[~touched[-1:]], other[~touched[-1:]]) and not torch.isfinite(other[touched[-1:]]).any()
