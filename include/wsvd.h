@@ -302,7 +302,9 @@ wsvd_status wsvd_decode_step(wsvd_ctx *ctx, const wsvd_layer_desc *desc, const v
                              const void *A_K, const void *A_V, const void *q, const void *q_scale, const void *B_K,
                              const void *B_V, wsvd_cache *cache, int32_t max_seq_len, void *out, void *hip_stream);
 
-/* Synchronise the stream and return (then clear) the device-side error word. */
+/* Synchronise the stream and return (then clear) the device-side error word.  WSVD_E_HIP recorded there: a workgroup's bounded wait for
+ * another one's partial results ran out; outputs of the calls since the last check are not valid, and what came late may lie in the
+ * workspace: call wsvd_set_workspace again before the next call. */
 wsvd_status wsvd_check(wsvd_ctx *ctx, void *hip_stream);
 
 const char *wsvd_status_str(wsvd_status s);
@@ -475,7 +477,13 @@ wsvd_status wsvd_linear_w4a8_split(wsvd_ctx *ctx, const int8_t *x, const void *x
  * leaves alone, and the backbone the latent layers are compared with), over a paged cache of plain 16-bit rows, with the
  * same page tables as the latent layers' pools.
  *
- *   dtype   BF16 or F16: queries, keys, values and outputs.  Scores, softmax statistics and sums are fp32.
+ *   dtype   BF16 or F16: queries, keys, values and outputs.  Scores, softmax statistics (the sum of the weights among them) and
+ *           accumulators are fp32.  The weights that meet the values are 16-bit operands: the decode attention takes each as a
+ *           pair (off by at most 2^-17 of itself in bf16, 2^-23 in f16), the prompt attentions round it once to dtype (by at most 2^-8
+ *           and 2^-11 of itself: their outputs are off by 1.1 to 1.35 times what the output's own rounding alone makes).  An f16 weight
+ *           is in addition off by up to 2^-36 of the largest.  Scores (sm_scale * q . k) may be as large as 2^26 in either direction.
+ *   Numbers that are none   Infinite and NaN values that a query sees come out as the formula has them, and change nothing else: not
+ *           the other dims, nor other queries.
  *   Heads   n_q_heads / n_kv_heads in 1..16, d_head 64 or 128, at most 1024 query heads.
  *   Rows    packed tensors are [tokens][ld] with a token's heads side by side from the pointer on; ld in elements, a multiple
  *           of 8, at least heads * d_head (so the three parts of one projection's output can be passed as they lie).  Of no
@@ -498,8 +506,10 @@ typedef struct {
   float sm_scale;  /* softmax scale; 0 means 1/sqrt(d_head) */
 } wsvd_dense_desc;
 
-/* Scratch of the three dense attention calls (HOST output; tens of MB, most of it for prompts of few tiles, whose keys several
- * workgroups share); without it they return WSVD_E_WORKSPACE.  A context's workspace may serve latent and dense layers in turn. */
+/* Scratch of the three dense attention calls (HOST output); without it they return WSVD_E_WORKSPACE.  At least 34 MB (17 at d_head
+ * 64), for prompts of few tiles, whose keys several workgroups share; 8 * (d_head + 2) bytes per sequence and query head where
+ * that is more (32 heads of 128: 136 MB for 4096 sequences).  A context's workspace of the larger size may serve latent and
+ * dense layers in turn. */
 wsvd_status wsvd_dense_workspace_bytes(const wsvd_dense_desc *desc, size_t *bytes);
 
 /*
@@ -526,7 +536,11 @@ wsvd_status wsvd_dense_append_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, 
  * (as does a row whose scores are all -inf).  q [batch][q_ld], out [batch][n_q_heads][d_head] of dtype.  The rows of all
  * sequences are divided over the chip by the lengths found on the device and joined in a fixed order, so the result does
  * not depend on timing; max_seq_len is a HOST upper bound, at most max_pages * page_rows (a longer sequence records
- * WSVD_E_SHAPE and is attended over its first max_seq_len rows).  The min_chunk setting of the context applies.
+ * WSVD_E_SHAPE and is attended over its first max_seq_len rows).  The min_chunk setting of the context applies.  The bound also
+ * chooses the form of the launch (and with it the order of sums, nothing else): a tight one is faster where sequences are short and many (up to 1024 rows:
+ * smaller workgroups; short enough to stay whole: no search for the cuts; small in all: rows stay in the caches).  With 8192 in
+ * place of the longest length, 1024 sequences of up to 100 rows take 258 us instead of 36, 44 of one row 23 instead of 10, 64
+ * of up to 500 13 instead of 10, 32 of up to 1000 the same.
  */
 wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld,
                                          const wsvd_paged_cache *cache, int32_t max_seq_len, void *out, void *hip_stream);

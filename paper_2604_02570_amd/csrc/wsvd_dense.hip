@@ -15,8 +15,8 @@ WSVD_DEV void store_row(V* p, V v) { if (ONCE) __builtin_nontemporal_store(v, p)
 // ---------------------------------------------------------------- append
 // Rotation of the new tokens' queries and keys (dims i and i + d/2 turned by position * inv_freq[i]) and their keys and values
 // stored in the pages.  Bound: memory, every element read and written once (16 prompts of 2048 tokens and less, 32 heads of 128:
-// 1.03 GB in 178 us, 5.75 TB/s, where a copy of 1 GiB reaches 5.08); few tokens: three dependent loads (32 tokens of 28 / 4
-// heads: 3.2 us).
+// 1.03 GB in 183 us, 5.6 TB/s, where a copy of 1 GiB reaches 4.9 to 5.2); few tokens: three dependent loads (32 tokens of 28 / 4
+// heads: 3.7 us on the GPU).
 //   A wave finds its token's sequence, row and page, and its lanes the token's d / 2 angles, once for all heads: in 64 bits as
 // far as whole turns go (an fp32 product of a position of 1e5 would be off by 6e-3 radians), the sine and cosine of what is
 // left in 32.  Then the workgroup goes over the (token, head) pairs, 16 bytes of each half per thread.
@@ -110,8 +110,8 @@ __global__ __launch_bounds__(256) void k_dense_append(DenseAppendParams p) {
 // head and 4 of 16 rows; its 8 weights of 32 rows are, as they lie, its part of the second product's operand (the contraction over
 // rows may run in any order, V is taken in that one).  V's operand is made in registers: a lane loads 8 rows' same dims in whole
 // lines and pairs them up with one byte permute per two elements.
-// Bound: HBM.  32 x 8192 rows of 4 heads of 128 (537 MB): 86.6 us, 6.2 TB/s (a kernel that only reads them: 81 us); 640 rows of 32
-// heads (10.5 MB): 7.7 us, of which 3.3 are a launch that finds no row, and the rest a CU's stream of 74 GB/s.
+// Bound: HBM.  32 x 8192 rows of 4 heads of 128 (537 MB): 86.8 us, 6.2 TB/s (a kernel that only reads them: 81 us); 640 rows of 32
+// heads (10.5 MB): 7.8 us, of which 3.3 are a launch that finds no row, and the rest a CU's stream of 74 GB/s.
 // A workgroup's place: sequence, chunk of it, chunks it has, its length, the rows of a chunk; false for a workgroup that has none.
 struct DensePlace { int b, chunk, n_chunks, len, rows; };
 
@@ -317,9 +317,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         tile.v[4 * g + i2] = load_row<ONCE>((const typename DenseTile<D>::Piece*)(vp + (4 * qd + i2) * D + c * NJ));
     }
   };
-  // A wave's keys go through LDS of its own: requested in whole lines (asked for as the product's operand, 16 rows of 64 bytes
-  // per request, they cost the CU's address pipeline four times as much: 640 rows in two chunks 14.3 us against 11.8) and read back by key, the
-  // 16-byte pieces of a row permuted so that neither side meets a bank twice.
+  // A wave's keys go through LDS of its own: requested in whole lines (asked for as the product's operand, 16 rows of 64 bytes per
+  // request, they cost the CU's address pipeline four times as much: 640 rows in two chunks 14.3 us against 11.8, when it was tried)
+  // and read back by key, the 16-byte pieces of a row permuted so that neither side meets a bank twice.
   const uint32_t k_lds = lds_address(o_sh) + wave * (64 * D);
   uint32_t k_put[NK], k_get[NK];
 #pragma unroll

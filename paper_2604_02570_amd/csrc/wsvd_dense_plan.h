@@ -48,12 +48,15 @@ WSVD_HD int dense_target(int waves, int Hkv) {
 }
 WSVD_HD int dense_units_of(int len) { return (int)(((unsigned)len + kDenseUnit - 1) / kDenseUnit); }
 WSVD_HD int dense_chunks(int u, int units) { return u > units ? (u + units - 1) / units : 1; }
-// Partial results are folded by groups of kDenseFold chunks and then by groups of those: no sequence has more than kDenseFold^2.
+// Partial results are folded by groups of kDenseFold chunks and then by groups of those: no sequence has more than kDenseFold^2, which
+// leaves CUs without rows where one long sequence has few kv heads (with 2, 128 workgroups have some, with 1, 64).
 // (Groups of 16: 1 x 65001 rows of 2 heads 18.7 us, of 8: 15.5.  A group's end takes 7 chunks in 2 us, a second level costs 3: all
 // of 16 chunks by the last one's workgroup, 7 at a time, take 15.2 us where two levels take 12.7.)
 constexpr int kDenseFold = 8;
 // The most units of a chunk: all, where the longest sequence has no more than alone_units (one CU streams 74 GB/s, so that 330 KB
-// take as long as the hand-over that a cut costs); else at least min_units, and for up to 64 sequences the least at which there
+// take as long as the hand-over that a cut costs: one sequence, heads of 128, 32 / 32, 32 / 8 and 28 / 4 of them, 640 rows whole 7.7, 7.3
+// and 7.7 us, in two 8.5, 8.7, 9.8, in three 7.9, 8.2, 9.1; 768 rows whole 8.7, 7.9, 8.2, in three 8.7, 8.0, 8.8; 1024 whole 10.7, 9.1, 9.5, in
+// four 9.5, 8.1, 9.0); else at least min_units, and for up to 64 sequences the least at which there
 // are at most `target` chunks (a chunk too many is a second round of workgroups: 23 ragged sequences of up to 3001 rows, 8 kv
 // heads: 43.8 -> 36.5 us).  count(units): the chunks of all sequences.
 template <class Count>

@@ -10,14 +10,21 @@
 // head) pair, token-major, so the G heads of a kv head share every staged key block, and a tile covers few tokens: less of
 // the causal triangle is computed for nothing.
 //
+// Weights are fp32 up to the second product and in the sum, and rounded once to the 16 bits of its operand (off by at most 2^-8 of a
+// weight in bf16, 2^-11 in f16).  Outputs are then off from 64 bits by 2.1e-3 to 2.3e-3 in bf16 and 2.2e-4 to 2.8e-4 in f16, where the output's own
+// rounding makes 1.6e-3 to 1.7e-3 and 2.0e-4 to 2.1e-4: a pair of words a weight, as in the decode attention, would be half as many matrix
+// products again in a loop that they bind.
+//
 // A workgroup is 4 waves of 32 query rows; two workgroups share a CU, so that one multiplies while the other starts, waits or ends.
 // Blocks of 64 keys go straight from memory to LDS, two stages deep.  A wave runs one block's softmax under the next block's score
 // products and its own first value products, and the next block's maximum under the other value products; what it costs is then
-//   * matrix products: 1024 cycles per block and wave at d 128 (56 % of the time at 8192 tokens, all heads),
+//   * matrix products: 1024 cycles per block and wave at d 128,
 //   * vector instructions: about 120 and 32 exponentials, about as long, spread evenly over the products,
 //   * power: at full load the chip runs at 1.9 GHz instead of 2.4 (the same call on zeros takes 0.84 of the time).
-// 1 x 8192 tokens, 32 heads of 128: 1.17 PFLOP/s without a mask, 1.08 causal (products of 16384^2 matrices: 1.37); 16 x 2048 tokens:
-// 0.91, with 1.07 GB of queries, keys, values and outputs.  d 64: 0.93.
+// Counted at 16 x 2048 tokens, of a SIMD's time: matrix cores 53 %, vector instructions 50 %, LDS instructions 40 % of a CU's, no bank
+// conflicts.  Matrix and vector instructions of a SIMD's two waves hardly overlap.
+// 1 x 8192 tokens, 32 heads of 128: 1.13 PFLOP/s without a mask, 1.08 causal (products of 16384^2 matrices on that card: 1.35); 16 x 2048
+// tokens: 0.89, with 1.07 GB of queries, keys, values and outputs.  d 64: 0.97 without a mask, 0.90 causal.
 // Tried and not faster: 8 waves to a workgroup (0.86 where 4 have 0.90 at 16 x 2048); 64 rows a wave, one wave a SIMD (0.71: the
 // accumulators no longer fit the vector registers); the weights' sum by the matrix cores; the longest tiles of all sequences first
 // (16 x 2048: 0.57, keys and values no longer stay in the L2); lines of later blocks fetched to the L2 ahead.
@@ -34,7 +41,8 @@ constexpr int kLeastBlocks = 6;
 
 // lds_copy16 without the compiler's knowledge: it would let every later read of LDS wait for the copy (the next block's, while
 // this one is worked on: 16 x 2048 tokens 1124 us, with the loops' other waits gone 763).  The copies are waited for by
-// lds_copy_wait_barrier alone.  (M0 is written by whoever uses it; the compiler keeps nothing there.)
+// lds_copy_wait_barrier alone.  (M0 is a reserved register: the compiler gives it to no value, writes it right before an instruction of its
+// own that reads it, of which there is none here, and takes no clobber of it: it warns that one has no defined effect.)
 WSVD_DEV void copy16(uint32_t lds, const uint8_t* base, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
