@@ -537,10 +537,10 @@ wsvd_status wsvd_dense_append_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, 
  * sequences are divided over the chip by the lengths found on the device and joined in a fixed order, so the result does
  * not depend on timing; max_seq_len is a HOST upper bound, at most max_pages * page_rows (a longer sequence records
  * WSVD_E_SHAPE and is attended over its first max_seq_len rows).  The min_chunk setting of the context applies.  The bound also
- * chooses the form of the launch (and with it the order of sums, nothing else): a tight one is faster where sequences are short and many (up to 1024 rows:
- * smaller workgroups; short enough to stay whole: no search for the cuts; small in all: rows stay in the caches).  With 8192 in
- * place of the longest length, 1024 sequences of up to 100 rows take 258 us instead of 36, 44 of one row 23 instead of 10, 64
- * of up to 500 13 instead of 10, 32 of up to 1000 the same.
+ * chooses the form of the launch (and with it the order of sums, nothing else): a tight one is faster where sequences are
+ * short and many (up to 1024 rows: smaller workgroups; short enough to stay whole: no search for the cuts; small in all: rows
+ * stay in the caches).  With 8192 in place of the longest length, 1024 sequences of up to 100 rows take 258 us instead of 36,
+ * 44 of one row 23 instead of 10, 64 of up to 500 13 instead of 10, 32 of up to 1000 the same.
  */
 wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld,
                                          const wsvd_paged_cache *cache, int32_t max_seq_len, void *out, void *hip_stream);

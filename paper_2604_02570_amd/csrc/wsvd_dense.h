@@ -10,7 +10,7 @@
 //   The softmax's weights are operands too, 2^(score - reference).  The reference is set kRaise below the largest score so far, and set anew when
 // a weight would pass 2^kTop.  A bf16 weight can be as small as an fp32 one.  An f16 one has all its bits down to 2^-14 and is gone below
 // 2^-25, where the sum of the weights, in fp32, still counts it (65001 rows 26 powers of two below one whose value is 0: output 9 % off).
-// So the largest f16 weights are 2^11 to 2^15.9 (65504 is 2^16 less half a step): full relative precision 25 powers of two below the largest
+// So the largest f16 weights are 2^11 to 2^15.9 (the type ends at 65504, 2^15.999): full relative precision 25 powers of two below the largest
 // score, and no weight off by more than 2^-36 of the largest.  (Anew at 4.9 more: scores of a later block rarely pass the first one's by more;
 // 2048 tokens behind 6144, f16: 217.7 us, at 4 more 219.5, 2^7 to 2^15 218.3.)
 struct DenseBf16 {
