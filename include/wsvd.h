@@ -562,6 +562,83 @@ wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx *ctx, const wsvd_dense_desc *
                                           const int32_t *cu_q, const wsvd_paged_cache *cache, void *out, int64_t out_ld,
                                           void *hip_stream);
 
+/*
+ * The cache of dense layers in 8 bits: the calls above over pages of E4M3 codes (4 significant bits, up to 448) with a scale for each
+ * block of 16 rows and kv head, half the bytes of a 16-bit cache.
+ *
+ *   Block   16 consecutive rows of one kv head.  Its keys have one scale, its values another, each a power of two held as the byte
+ *           exponent + 127; what a code stands for is code * scale.  The append chooses the least exponent e >= -100 with
+ *           (largest finite magnitude) <= 448 * 2^e, so a value keeps 4 significant bits down to 2^-14 of 448 scales, and below that is
+ *           off by at most 2^-10 scales.  A code is rounded to nearest even; values that are infinite or none are stored as none (the
+ *           NaN code) and do not count for the scale.  Nothing that is stored passes the type: where 256 scales would, codes end at 240.
+ *   Pools   k_codes / v_codes: [n_pages][n_kv_heads][page_rows / 16] blocks of 16 * d_head bytes; k_meta / v_meta: their scales, a byte
+ *           each, [n_pages][n_kv_heads][page_rows / 16].  Byte of (row r, dim x) in a block:
+ *             keys    (x / 16) * 256 + r * 16 + x % 16
+ *             values  (x / 64) * 1024 + (r / 4) * 256 + (x % 64) * 4 + r % 4
+ *           A caller that fills pools itself keeps to scale bytes 27 .. 247 and to values that the type holds.  All else about the
+ *           cache, its lengths, table and errors, is as for the 16-bit calls; k_meta / v_meta may not be NULL.
+ */
+
+/* Bytes of ONE code pool and ONE scale pool (K or V) of n_pages pages (HOST outputs). */
+wsvd_status wsvd_dense_f8_cache_bytes(const wsvd_dense_desc *desc, int32_t page_rows, int32_t n_pages, size_t *codes_bytes,
+                                      size_t *scale_bytes);
+
+/*
+ * wsvd_dense_append_paged with the rows quantised.  What is quantised is rot(k) rounded to dtype (k_out, where given) and v.
+ * A block that a call fills from its first row on takes the scale of the call's rows.  One that held rows keeps its scale where that is
+ * large enough; where it is not, it takes the new one and the codes of its earlier rows move to it (rounded again, which
+ * changes only what becomes smaller than 2^-14 of 448 scales).  Bytes of rows that the call neither writes nor moves stay as they are.
+ * Sequences of one call have no block in common that the call writes to.
+ */
+wsvd_status wsvd_dense_append_paged_f8(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld, const void *k,
+                                       int64_t k_ld, const void *v, int64_t v_ld, int64_t n_tokens, const int32_t *cu_tokens,
+                                       const int32_t *positions, const double *inv_freq, void *q_out, int64_t q_out_ld,
+                                       void *k_out, int64_t k_out_ld, wsvd_paged_cache *cache, void *hip_stream);
+
+/* wsvd_dense_decode_attn_paged and wsvd_dense_prefill_attn_paged over such pages: keys and values are code * scale, exact as numbers of
+ * dtype; precision, workspace and everything else as there.  A value that is none makes none of every output that sees its row. */
+wsvd_status wsvd_dense_decode_attn_paged_f8(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld,
+                                            const wsvd_paged_cache *cache, int32_t max_seq_len, void *out, void *hip_stream);
+wsvd_status wsvd_dense_prefill_attn_paged_f8(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld, int64_t n_q,
+                                             const int32_t *cu_q, const wsvd_paged_cache *cache, void *out, int64_t out_ld,
+                                             void *hip_stream);
+
+/*
+ * Page tables kept on the GPU: the free pages are a list on the device, pages of finished sequences go back to it and new tokens take
+ * from it, so that a serving step (and a graph of it) needs no table from the host.  For any of the paged caches above (several layers
+ * share one table).  Both calls read seq_lens and n_free and write seq_lens_out and n_free_out, which may be the same memory; they
+ * need no workspace.
+ */
+typedef struct {
+  int32_t *block_table;      /* DEVICE [batch][max_pages] */
+  int32_t *free_pages;       /* DEVICE [n_pages]: the first *n_free entries are pages that no sequence has */
+  int32_t batch, page_rows, max_pages, n_pages;   /* page_rows and max_pages as for the caches; n_pages * page_rows below 2^31 */
+} wsvd_page_pool;
+
+/*
+ * Rows for new_lens[b] new tokens of every sequence b (new_lens NULL: one each, n_tokens == batch):
+ *   seq_lens_out[b] = seq_lens[b] + new_lens[b]; table entries of the pages that these rows reach and the earlier ones did not are
+ *   taken from the end of the free list, sequence by sequence and page by page; n_free_out = what is left.
+ *   cu_tokens [batch + 1]: prefix sums of new_lens, the packed tokens' borders.  positions [n_tokens]: a token's row in its sequence.
+ *   slots [n_tokens]: page * page_rows + row in the page.  Each of the three may be NULL.
+ * n_tokens, at most 2^24, is what positions and slots have room for; entries behind the last token are left as they are.
+ * Where the free list ends, the entries that it cannot serve are -1, as are their tokens' slots, and WSVD_E_CAPACITY is recorded in the
+ * status word (wsvd_check): appends store nothing there and report it.  Rows above max_pages * page_rows have no page: -1 and
+ * WSVD_E_CAPACITY likewise.  More tokens than n_tokens, negative numbers, lengths above max_pages * page_rows and entries that are no
+ * page record WSVD_E_SHAPE (numbers are taken as the nearest that is allowed).
+ */
+wsvd_status wsvd_pages_grow(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int32_t *new_lens, int64_t n_tokens,
+                            const int32_t *seq_lens, const int32_t *n_free, int32_t *seq_lens_out, int32_t *n_free_out,
+                            int32_t *cu_tokens, int32_t *positions, int32_t *slots, void *hip_stream);
+
+/*
+ * The pages of every sequence with done[b] != 0 go to the end of the free list, in the order of sequences and rows, and its length
+ * becomes 0; table entries outside [0, n_pages) are left out.  The entries themselves stay as they are.  A list that would hold more
+ * than n_pages pages (one given back twice) ends there, and WSVD_E_SHAPE is recorded.
+ */
+wsvd_status wsvd_pages_release(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int32_t *done, const int32_t *seq_lens,
+                               const int32_t *n_free, int32_t *seq_lens_out, int32_t *n_free_out, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

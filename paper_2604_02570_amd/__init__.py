@@ -31,7 +31,8 @@ EXPORTS = ["wsvd_create", "wsvd_destroy", "wsvd_cache_bytes", "wsvd_workspace_by
            "wsvd_rmsnorm_quant_i8", "wsvd_swiglu_quant_i8", "wsvd_prefill_append",
            "wsvd_prefill_attn", "wsvd_shared_workspace_bytes", "wsvd_decode_attn_shared", "wsvd_timeline_set_buffer",
            "wsvd_dense_workspace_bytes", "wsvd_dense_append_paged", "wsvd_dense_decode_attn_paged", "wsvd_dense_prefill_attn",
-           "wsvd_dense_prefill_attn_paged"]
+           "wsvd_dense_prefill_attn_paged", "wsvd_dense_f8_cache_bytes", "wsvd_dense_append_paged_f8", "wsvd_dense_decode_attn_paged_f8",
+           "wsvd_dense_prefill_attn_paged_f8", "wsvd_pages_grow", "wsvd_pages_release"]
 
 
 class WsvdError(RuntimeError):
@@ -61,6 +62,11 @@ class PagedCache(ctypes.Structure):
 class DenseDesc(ctypes.Structure):
     _fields_ = [("batch", c_int32), ("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("d_head", c_int32), ("dtype", c_int32),
                 ("sm_scale", c_float)]
+
+
+class PagePool(ctypes.Structure):
+    _fields_ = [("block_table", c_void_p), ("free_pages", c_void_p), ("batch", c_int32), ("page_rows", c_int32), ("max_pages", c_int32),
+                ("n_pages", c_int32)]
 
 
 _lib = None
@@ -157,6 +163,11 @@ def lib():
                                               c_int64, c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p]
         L.wsvd_dense_prefill_attn_paged.argtypes = [c_void_p, POINTER(DenseDesc), c_void_p, c_int64, c_int64, c_void_p, POINTER(PagedCache),
                                                     c_void_p, c_int64, c_void_p]
+        L.wsvd_dense_f8_cache_bytes.argtypes = [POINTER(DenseDesc), c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
+        for name in ("append_paged", "decode_attn_paged", "prefill_attn_paged"):
+            getattr(L, f"wsvd_dense_{name}_f8").argtypes = getattr(L, f"wsvd_dense_{name}").argtypes
+        L.wsvd_pages_grow.argtypes = [c_void_p, POINTER(PagePool), c_void_p, c_int64] + [c_void_p] * 8
+        L.wsvd_pages_release.argtypes = [c_void_p, POINTER(PagePool)] + [c_void_p] * 6
         for name in EXPORTS:
             if name not in ("wsvd_status_str",):
                 getattr(L, name).restype = c_int
@@ -489,3 +500,64 @@ def wsvd_dense_prefill_attn_paged(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out
         status = call(*_addresses(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, on))
     if status:
         raise WsvdError(status, "wsvd_dense_prefill_attn_paged")
+
+
+def wsvd_dense_f8_cache_bytes(desc, page_rows, n_pages):
+    a, b = c_size_t(), c_size_t()
+    _ck(lib().wsvd_dense_f8_cache_bytes(byref(desc), int(page_rows), int(n_pages), byref(a), byref(b)), "wsvd_dense_f8_cache_bytes")
+    return a.value, b.value
+
+
+def wsvd_dense_append_paged_f8(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_tokens, cu_tokens, positions, inv_freq, q_out, q_out_ld, k_out, k_out_ld,
+                            cache, stream=None):
+    call, on = (_lib or lib()).wsvd_dense_append_paged_f8, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, desc, None if q is None else q.data_ptr(), q_ld, k.data_ptr(), k_ld, v.data_ptr(), v_ld, n_tokens,
+                      None if cu_tokens is None else cu_tokens.data_ptr(), None if positions is None else positions.data_ptr(),
+                      None if inv_freq is None else inv_freq.data_ptr(), None if q_out is None else q_out.data_ptr(), q_out_ld,
+                      None if k_out is None else k_out.data_ptr(), k_out_ld, cache, on)
+    except AttributeError:                                             # addresses in place of tensors
+        status = call(*_addresses(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_tokens, cu_tokens, positions, inv_freq, q_out, q_out_ld, k_out,
+                                  k_out_ld, cache, on))
+    if status:
+        raise WsvdError(status, "wsvd_dense_append_paged_f8")
+
+
+def wsvd_dense_decode_attn_paged_f8(ctx, desc, q, q_ld, cache, max_seq_len, out, stream=None):
+    call, on = (_lib or lib()).wsvd_dense_decode_attn_paged_f8, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, desc, q.data_ptr(), q_ld, cache, max_seq_len, out.data_ptr(), on)
+    except AttributeError:
+        status = call(*_addresses(ctx, desc, q, q_ld, cache, max_seq_len, out, on))
+    if status:
+        raise WsvdError(status, "wsvd_dense_decode_attn_paged_f8")
+
+
+def wsvd_dense_prefill_attn_paged_f8(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, stream=None):
+    call, on = (_lib or lib()).wsvd_dense_prefill_attn_paged_f8, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, desc, q.data_ptr(), q_ld, n_q, cu_q.data_ptr(), cache, out.data_ptr(), out_ld, on)
+    except AttributeError:
+        status = call(*_addresses(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, on))
+    if status:
+        raise WsvdError(status, "wsvd_dense_prefill_attn_paged_f8")
+
+
+def make_page_pool(block_table, free_pages, batch, page_rows, max_pages, n_pages) -> PagePool:
+    p = PagePool(_ptr(block_table), _ptr(free_pages), int(batch), int(page_rows), int(max_pages), int(n_pages))
+    p._keep = (block_table, free_pages)   # keep the tensors alive
+    return p
+
+
+def wsvd_pages_grow(ctx, pool, new_lens, n_tokens, seq_lens, n_free, seq_lens_out, n_free_out, cu_tokens=None, positions=None, slots=None,
+                    stream=None):
+    status = (_lib or lib()).wsvd_pages_grow(*_addresses(ctx, pool, new_lens, n_tokens, seq_lens, n_free, seq_lens_out, n_free_out, cu_tokens,
+                                                         positions, slots, _stream_addr(stream)))
+    if status:
+        raise WsvdError(status, "wsvd_pages_grow")
+
+
+def wsvd_pages_release(ctx, pool, done, seq_lens, n_free, seq_lens_out, n_free_out, stream=None):
+    status = (_lib or lib()).wsvd_pages_release(*_addresses(ctx, pool, done, seq_lens, n_free, seq_lens_out, n_free_out, _stream_addr(stream)))
+    if status:
+        raise WsvdError(status, "wsvd_pages_release")

@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libwsvd.so")
 LIB_TIMELINE = os.path.join(HERE, "libwsvd_timeline.so")     # profiling build: in-kernel wall-clock stamps compiled in
 SOURCES = ["wsvd_api.hip", "wsvd_quant.hip", "wsvd_append.hip", "wsvd_step.hip", "wsvd_attn_generic.hip", "wsvd_attn_mfma.hip",
            "wsvd_block.hip", "wsvd_layer.hip", "wsvd_prefill.hip", "wsvd_project.hip", "wsvd_shared.hip", "wsvd_dense.hip",
-           "wsvd_dense_prefill.hip", "wsvd_dense_api.hip"]
+           "wsvd_dense_prefill.hip", "wsvd_dense_f8.hip", "wsvd_dense_api.hip", "wsvd_pages.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]
 # per-file additions.  The prompt attention reads every score tile back into the vector ALU, which binds it: its matrix

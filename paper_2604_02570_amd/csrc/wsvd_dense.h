@@ -84,6 +84,8 @@ struct DensePages {
   int page_rows, max_pages, n_pages;
   uint32_t page_magic;          // dense_page_magic
 };
+// 8-bit pages alone, whose k and v point to codes (see wsvd_dense_f8.h): the blocks' scales, [n_pages][Hkv][page_rows / 16].
+struct DenseScales { uint8_t *k, *v; };
 struct DenseAppendParams {
   const uint16_t *q, *k, *v;
   uint16_t *q_out, *k_out;
@@ -93,6 +95,7 @@ struct DenseAppendParams {
   DensePages pages;
   int n_tokens, B, Hq, Hkv;
   int* err_word;
+  DenseScales scales;
 };
 struct DenseDecodeParams {
   const uint16_t* q;
@@ -104,6 +107,7 @@ struct DenseDecodeParams {
   int alone;                    // no sequence is cut
   float c_scale;                // sm_scale * log2(e)
   int* err_word;
+  DenseScales scales;
 };
 struct DensePromptParams {
   const uint16_t *q, *k, *v;    // k, v: packed rows (not paged)
@@ -115,8 +119,12 @@ struct DensePromptParams {
   int B, Hkv, G, causal, n_q, n_kv, splits, pairs;
   float c_scale;
   int* err_word;
+  DenseScales scales;
 };
 
 hipError_t wsvd_launch_dense_append(const DenseAppendParams& p, int dtype, int d, hipStream_t s);
 hipError_t wsvd_launch_dense_decode(const DenseDecodeParams& p, int dtype, int d, hipStream_t s);
-hipError_t wsvd_launch_dense_prompt(DensePromptParams& p, int dtype, int d, bool paged, hipStream_t s);
+enum class DenseKeys { packed, paged, paged_f8 };
+hipError_t wsvd_launch_dense_prompt(DensePromptParams& p, int dtype, int d, DenseKeys keys, hipStream_t s);
+hipError_t wsvd_launch_dense_append_f8(const DenseAppendParams& p, int dtype, int d, hipStream_t s);
+hipError_t wsvd_launch_dense_decode_f8(const DenseDecodeParams& p, int dtype, int d, hipStream_t s);

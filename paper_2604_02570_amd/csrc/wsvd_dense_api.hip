@@ -18,8 +18,9 @@ wsvd_status check_desc(const wsvd_dense_desc* d) {
   return WSVD_OK;
 }
 
-wsvd_status check_pages(const wsvd_paged_cache* c) {
+wsvd_status check_pages(const wsvd_paged_cache* c, bool f8) {
   if (!c || !c->k_codes || !c->v_codes || !c->seq_lens || !c->block_table) return WSVD_E_NULL;
+  if (f8 && (!c->k_meta || !c->v_meta)) return WSVD_E_NULL;
   if (c->page_rows < 16 || c->page_rows % 16 != 0 || c->page_rows > 4096 || c->max_pages < 1 || c->n_pages < 1) return WSVD_E_SHAPE;
   if ((int64_t)c->max_pages * c->page_rows > kMostRows) return WSVD_E_SHAPE;
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned4(c->seq_lens) || !aligned4(c->block_table)) return WSVD_E_ALIGN;
@@ -39,6 +40,7 @@ DensePages pages_of(const wsvd_paged_cache* c) {
   return {(uint16_t*)c->k_codes, (uint16_t*)c->v_codes, c->seq_lens, c->block_table, c->page_rows, c->max_pages, c->n_pages,
           dense_page_magic(c->page_rows)};
 }
+DenseScales scales_of(const wsvd_paged_cache* c) { return {(uint8_t*)c->k_meta, (uint8_t*)c->v_meta}; }
 float scale_of(const wsvd_dense_desc* d) {
   const float s = d->sm_scale != 0.f ? d->sm_scale : 1.f / __builtin_sqrtf((float)d->d_head);
   return s * kLog2e;
@@ -66,13 +68,12 @@ wsvd_status wsvd_dense_workspace_bytes(const wsvd_dense_desc* desc, size_t* byte
   return WSVD_OK;
 }
 
-wsvd_status wsvd_dense_append_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, const void* k,
-                                    int64_t k_ld, const void* v, int64_t v_ld, int64_t n_tokens, const int32_t* cu_tokens,
-                                    const int32_t* positions, const double* inv_freq, void* q_out, int64_t q_out_ld, void* k_out,
-                                    int64_t k_out_ld, wsvd_paged_cache* cache, void* hip_stream) {
+static wsvd_status append(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, const void* k, int64_t k_ld, const void* v,
+                          int64_t v_ld, int64_t n_tokens, const int32_t* cu_tokens, const int32_t* positions, const double* inv_freq, void* q_out,
+                          int64_t q_out_ld, void* k_out, int64_t k_out_ld, wsvd_paged_cache* cache, bool f8, void* hip_stream) {
   if (!ctx) return WSVD_E_NULL;
   WSVD_TRY(check_desc(desc));
-  WSVD_TRY(check_pages(cache));
+  WSVD_TRY(check_pages(cache, f8));
   const int64_t wq = (int64_t)desc->n_q_heads * desc->d_head, wkv = (int64_t)desc->n_kv_heads * desc->d_head;
   if (!q != !q_out && n_tokens != 0) return WSVD_E_NULL;
   if (q) {
@@ -91,15 +92,28 @@ wsvd_status wsvd_dense_append_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, 
   if (n_tokens == 0) return WSVD_OK;
   DenseAppendParams p = {(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, (uint16_t*)q_out, (uint16_t*)k_out, q_ld, k_ld, v_ld,
                          q_out_ld, k_out_ld, cu_tokens, positions, inv_freq, pages_of(cache), (int)n_tokens, desc->batch, desc->n_q_heads,
-                         desc->n_kv_heads, ctx->err_word};
-  return launched(wsvd_launch_dense_append(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
+                         desc->n_kv_heads, ctx->err_word, scales_of(cache)};
+  return launched((f8 ? wsvd_launch_dense_append_f8 : wsvd_launch_dense_append)(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
 }
 
-wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld,
-                                         const wsvd_paged_cache* cache, int32_t max_seq_len, void* out, void* hip_stream) {
+wsvd_status wsvd_dense_append_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, const void* k,
+                                    int64_t k_ld, const void* v, int64_t v_ld, int64_t n_tokens, const int32_t* cu_tokens,
+                                    const int32_t* positions, const double* inv_freq, void* q_out, int64_t q_out_ld, void* k_out,
+                                    int64_t k_out_ld, wsvd_paged_cache* cache, void* hip_stream) {
+  return append(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_tokens, cu_tokens, positions, inv_freq, q_out, q_out_ld, k_out, k_out_ld, cache, false, hip_stream);
+}
+wsvd_status wsvd_dense_append_paged_f8(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, const void* k,
+                                       int64_t k_ld, const void* v, int64_t v_ld, int64_t n_tokens, const int32_t* cu_tokens,
+                                       const int32_t* positions, const double* inv_freq, void* q_out, int64_t q_out_ld, void* k_out,
+                                       int64_t k_out_ld, wsvd_paged_cache* cache, void* hip_stream) {
+  return append(ctx, desc, q, q_ld, k, k_ld, v, v_ld, n_tokens, cu_tokens, positions, inv_freq, q_out, q_out_ld, k_out, k_out_ld, cache, true, hip_stream);
+}
+
+static wsvd_status decode(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, const wsvd_paged_cache* cache,
+                          int32_t max_seq_len, void* out, bool f8, void* hip_stream) {
   if (!ctx || !out) return WSVD_E_NULL;
   WSVD_TRY(check_desc(desc));
-  WSVD_TRY(check_pages(cache));
+  WSVD_TRY(check_pages(cache, f8));
   WSVD_TRY(check_rows(q, q_ld, (int64_t)desc->n_q_heads * desc->d_head, desc->batch));
   if (!aligned16(out)) return WSVD_E_ALIGN;
   if (max_seq_len < 0) return WSVD_E_SHAPE;
@@ -117,8 +131,17 @@ wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* d
   if (!dense_launchable(dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0), 64 * p.waves)) return WSVD_E_SHAPE;
   WSVD_TRY(check_workspace(ctx, desc));
   p.parts = (unsigned long long*)((int*)ctx->ws + kWsCounterInts);
-  p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
-  return launched(wsvd_launch_dense_decode(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
+  p.c_scale = scale_of(desc); p.err_word = ctx->err_word; p.scales = scales_of(cache);
+  return launched((f8 ? wsvd_launch_dense_decode_f8 : wsvd_launch_dense_decode)(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
+}
+
+wsvd_status wsvd_dense_decode_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld,
+                                         const wsvd_paged_cache* cache, int32_t max_seq_len, void* out, void* hip_stream) {
+  return decode(ctx, desc, q, q_ld, cache, max_seq_len, out, false, hip_stream);
+}
+wsvd_status wsvd_dense_decode_attn_paged_f8(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld,
+                                            const wsvd_paged_cache* cache, int32_t max_seq_len, void* out, void* hip_stream) {
+  return decode(ctx, desc, q, q_ld, cache, max_seq_len, out, true, hip_stream);
 }
 
 wsvd_status wsvd_dense_prefill_attn(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, const void* k,
@@ -146,15 +169,14 @@ wsvd_status wsvd_dense_prefill_attn(wsvd_ctx* ctx, const wsvd_dense_desc* desc, 
   WSVD_TRY(check_workspace(ctx, desc));
   p.parts = (float*)ctx->ws + kWsCounterInts;
   p.n_q = (int)n_q; p.n_kv = (int)n_kv; p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
-  return launched(wsvd_launch_dense_prompt(p, desc->dtype, desc->d_head, false, (hipStream_t)hip_stream));
+  return launched(wsvd_launch_dense_prompt(p, desc->dtype, desc->d_head, DenseKeys::packed, (hipStream_t)hip_stream));
 }
 
-wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, int64_t n_q,
-                                          const int32_t* cu_q, const wsvd_paged_cache* cache, void* out, int64_t out_ld,
-                                          void* hip_stream) {
+static wsvd_status chunk(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, int64_t n_q, const int32_t* cu_q,
+                         const wsvd_paged_cache* cache, void* out, int64_t out_ld, bool f8, void* hip_stream) {
   if (!ctx || !cu_q) return WSVD_E_NULL;
   WSVD_TRY(check_desc(desc));
-  WSVD_TRY(check_pages(cache));
+  WSVD_TRY(check_pages(cache, f8));
   const int64_t wq = (int64_t)desc->n_q_heads * desc->d_head;
   WSVD_TRY(check_rows(q, q_ld, wq, n_q));
   WSVD_TRY(check_rows(out, out_ld, wq, n_q));
@@ -168,8 +190,29 @@ wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* 
   if (!dense_launchable(dense_prompt_grid(n_q, p.B, p.Hkv, p.G, true).workgroups, 256)) return WSVD_E_SHAPE;
   WSVD_TRY(check_workspace(ctx, desc));
   p.parts = (float*)ctx->ws + kWsCounterInts;
-  p.n_q = (int)n_q; p.c_scale = scale_of(desc); p.err_word = ctx->err_word;
-  return launched(wsvd_launch_dense_prompt(p, desc->dtype, desc->d_head, true, (hipStream_t)hip_stream));
+  p.n_q = (int)n_q; p.c_scale = scale_of(desc); p.err_word = ctx->err_word; p.scales = scales_of(cache);
+  return launched(wsvd_launch_dense_prompt(p, desc->dtype, desc->d_head, f8 ? DenseKeys::paged_f8 : DenseKeys::paged, (hipStream_t)hip_stream));
+}
+
+wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, int64_t n_q,
+                                          const int32_t* cu_q, const wsvd_paged_cache* cache, void* out, int64_t out_ld,
+                                          void* hip_stream) {
+  return chunk(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, false, hip_stream);
+}
+wsvd_status wsvd_dense_prefill_attn_paged_f8(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void* q, int64_t q_ld, int64_t n_q,
+                                             const int32_t* cu_q, const wsvd_paged_cache* cache, void* out, int64_t out_ld,
+                                             void* hip_stream) {
+  return chunk(ctx, desc, q, q_ld, n_q, cu_q, cache, out, out_ld, true, hip_stream);
+}
+
+wsvd_status wsvd_dense_f8_cache_bytes(const wsvd_dense_desc* desc, int32_t page_rows, int32_t n_pages, size_t* codes_bytes, size_t* scale_bytes) {
+  if (!codes_bytes || !scale_bytes) return WSVD_E_NULL;
+  WSVD_TRY(check_desc(desc));
+  if (page_rows < 16 || page_rows % 16 != 0 || page_rows > 4096 || n_pages < 1) return WSVD_E_SHAPE;
+  const size_t blocks = (size_t)n_pages * desc->n_kv_heads * (page_rows / 16);
+  *codes_bytes = blocks * 16 * desc->d_head;
+  *scale_bytes = blocks;
+  return WSVD_OK;
 }
 
 }  // extern "C"

@@ -87,6 +87,19 @@ WSVD_HD int dense_append_tokens(int64_t n_tokens, int items) {
   if (n_tokens < 2048 || (items >= 256 && dense_launchable(n_tokens, 256))) return 1;
   return items >= 128 ? 2 : 4;
 }
+// The append over 8-bit pages: tokens of a workgroup, whose units (the new rows of a block of 16) it has, and workgroups that share their
+// heads, four a round.
+struct DenseF8Append { int tokens, splits; };
+WSVD_HD DenseF8Append dense_f8_append(int64_t n_tokens, int batch, int heads, bool packed) {
+  const int tokens = packed && n_tokens >= 4096 && n_tokens >= 16 * (int64_t)batch ? 16 : 1;
+  const int64_t units = packed ? n_tokens / 16 + (batch < n_tokens ? batch : n_tokens) : n_tokens, rounds = (heads + 3) / 4, fill = 2048 / units;
+  return {tokens, (int)(fill < 1 ? 1 : fill < rounds ? fill : rounds)};
+}
+// Workgroups that a step's tokens are dealt out to, 1024 threads each.
+WSVD_HD unsigned pages_workgroups(int64_t n_tokens) {
+  const int64_t n = (n_tokens + 1023) / 1024;
+  return (unsigned)(n < 1 ? 1 : n > 128 ? 128 : n);
+}
 WSVD_HD int64_t dense_decode_workgroups(int B, int Hkv, int target, bool alone) { return (alone ? (int64_t)B : (int64_t)target + B) * Hkv; }
 // The prompt attention's, at most: every sequence ends inside a tile.  Two tiles a workgroup where there are many and they differ: the second
 // one's first keys and queries are asked for under the first one's last products, so that every other tile starts without a wait (16 x 2048

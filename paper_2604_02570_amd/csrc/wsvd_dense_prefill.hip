@@ -31,7 +31,7 @@
 #include <algorithm>
 #include <type_traits>
 #include "wsvd_attn_common.h"
-#include "wsvd_dense.h"
+#include "wsvd_dense_f8.h"
 
 namespace {
 
@@ -116,8 +116,9 @@ WSVD_DEV float* prompt_part(const DensePromptParams& p, int idx, int kv, int spl
   return p.parts + (((size_t)idx * p.Hkv + kv) * p.splits + split) * rows * (d + 2);
 }
 
-template <class T, int D, bool PAGED, int NW>
+template <class T, int D, DenseKeys KEYS, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3))) void k_dense_prompt(DensePromptParams p) {
+  constexpr bool PAGED = KEYS != DenseKeys::packed, F8 = KEYS == DenseKeys::paged_f8;
   constexpr int ROWS = 32 * NW;                      // query rows of a workgroup
   constexpr int PIECES = D / 8, RPI = 64 / PIECES;   // 16-byte pieces of a row; rows that one copy of a wave brings
   constexpr int COPIES = kKeys / NW / RPI;
@@ -154,18 +155,64 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   // Paged: a wave's rows of a block lie in one granule of 16.  Where they lie is looked up for 64 blocks at a time, a lane for each.
   static_assert(16 % (kKeys / NW) == 0, "");
   bool bad = false;
-  uint32_t at_low = 0, at_high = 0;
+  uint32_t at_low = 0, at_high = 0, scales = 0;      // (8-bit: where a block's codes are, and its scales' bytes)
   int looked_up = 0;                                 // the first of those blocks
   auto look_up = [&](int kb) {
     looked_up = kb;
     const int granule = min((key0 + (kb + lane) * kKeys + wave * (kKeys / NW)) >> 4, (at.nk - 1) >> 4), pg = dense_page_index(granule, p.pages.page_magic);
     const int page = dense_page(p.pages.block_table[(size_t)b * p.pages.max_pages + pg], p.pages.n_pages, bad);
-    const uint64_t bytes = dense_pool_row(page, granule, pg, kv, p.Hkv, p.pages.page_rows) * ROW_BYTES;
+    const uint64_t bytes = dense_pool_row(page, granule, pg, kv, p.Hkv, p.pages.page_rows) * (F8 ? D : ROW_BYTES);
+    if constexpr (F8) {
+      const uint64_t block = f8_block(page, granule, pg, kv, p.Hkv, p.pages.page_rows);
+      scales = (uint32_t)p.scales.k[block] | (uint32_t)p.scales.v[block] << 8;
+    }
     at_low = (uint32_t)bytes; at_high = (uint32_t)(bytes >> 32);
+  };
+  // 8-bit: keys to the rows and pieces that the copies have.  Values lie in LDS as operands, [16 keys][half of a wave][d] of 8 keys, the dims of
+  // 64 by their number modulo 4 first: what a lane gets from memory, 4 dims of 4 rows (and of the 4 rows 8 further on), goes there in
+  // whole pieces, 16 lanes side by side.
+  auto put_f8 = [&](const uint8_t* from, uint32_t to, float scale, bool keys) {
+    typedef __attribute__((address_space(3))) v4i lds_v4i;
+    typedef __attribute__((address_space(3))) v2i lds_v2i;
+    const int i = anew(lane);
+    if (keys) {
+      const int row = i & 15, sw = D == 128 ? row : row >> 1;
+#pragma unroll
+      for (int j = 0; j < D / 64; j++) {
+        const v4i x = *(const v4i*)(from + j * 1024 + i * 16);
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+          const uint32_t c0 = (uint32_t)x[2 * y], c1 = (uint32_t)x[2 * y + 1];
+          *(lds_v4i*)(uintptr_t)(to + row * ROW_BYTES + (((2 * (j * 4 + (i >> 4)) + y) ^ sw) & (PIECES - 1)) * 16) =
+              v4i{f8_pair<T, false>(c0, scale), f8_pair<T, true>(c0, scale), f8_pair<T, false>(c1, scale), f8_pair<T, true>(c1, scale)};
+        }
+      }
+    } else if (D == 128) {
+      const int x = i & 15, h = (i >> 4) & 1, c = i >> 5;
+      const v4i a = *(const v4i*)(from + c * 1024 + h * 256 + x * 16), b = *(const v4i*)(from + c * 1024 + h * 256 + 512 + x * 16);
+#pragma unroll
+      for (int y = 0; y < 4; y++)
+        *(lds_v4i*)(uintptr_t)(to + (h * D + c * 64 + y * 16 + x) * 16) =
+            v4i{f8_pair<T, false>((uint32_t)a[y], scale), f8_pair<T, true>((uint32_t)a[y], scale), f8_pair<T, false>((uint32_t)b[y], scale), f8_pair<T, true>((uint32_t)b[y], scale)};
+    } else {
+      const int x = i & 15, rg = i >> 4;
+      const v4i a = *(const v4i*)(from + i * 16);
+#pragma unroll
+      for (int y = 0; y < 4; y++)
+        *(lds_v2i*)(uintptr_t)(to + ((rg & 1) * D + y * 16 + x) * 16 + (rg >> 1) * 8) = v2i{f8_pair<T, false>((uint32_t)a[y], scale), f8_pair<T, true>((uint32_t)a[y], scale)};
+    }
   };
   // (rows of a copy are a scalar's distance apart: what a lane adds is the same for every block)
   auto stage = [&](int kb, int buf, bool keys) {
     const uint32_t to = lds0 + buf * STAGE + (keys ? 0 : PLANE) + wave * (16 * ROW_BYTES);
+    if constexpr (F8) {                              // a wave's block of 16 rows, made 16-bit numbers on the way
+      const int i = kb - looked_up;
+      const uint8_t* from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) +
+                            ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, i) << 32);
+      const uint32_t byte = (uint32_t)__builtin_amdgcn_readlane(scales, i);
+      put_f8(from, to, __uint_as_float((keys ? byte & 255 : byte >> 8) << 23), keys);
+      return;
+    }
     const uint32_t stride = keys ? k_stride : v_stride;
     if (!PAGED && (kb + 1) * kKeys > nk) {           // a block that ends before its last row: that one in the place of those behind it
       const uint8_t* from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)at.kv_start + key0 + kb * kKeys) * (keys ? p.k_ld : p.v_ld) + kv * D);
@@ -199,6 +246,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     for (int d = 0; d < ND; d++) {
       const int chunk = D == 128 ? d ^ (i >> 2) : d ^ (i >> 3);
       v_at[d] = lds0 + PLANE + key * ROW_BYTES + chunk * 64 + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+      if (F8) v_at[d] = lds0 + PLANE + (half * D + 32 * d + n) * 16;
     }
   }
   typedef short v4s __attribute__((ext_vector_type(4)));
@@ -207,6 +255,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   };
   auto read_v = [&](uint32_t stage, int d, int s) {  // 16 keys from 16 s, 32 dims from 32 d
     const uint32_t at = v_at[d] + stage + s * 16 * ROW_BYTES;
+    if constexpr (F8) return *(const __attribute__((address_space(3))) v4i*)(uintptr_t)at;
     const v2i lo = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)at));
     const v2i hi = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(at + 8 * ROW_BYTES)));
     return v4i{lo[0], lo[1], hi[0], hi[1]};
@@ -361,7 +410,21 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
         o[d] = T::mfma32(a, pw, o[d]);
       }
     }
-    if (__ballot(odd != 0)) {
+    if (F8 && __ballot(odd != 0)) {                  // (codes are finite or none: a value that is none makes none of what sees it, whatever its weight)
+      const int rel = limit - kb * kKeys, half = anew(lane) >> 5;
+#pragma unroll 1
+      for (int key = 0; key < kKeys; key++) {
+        const uint32_t row_at = lds0 + at + PLANE + (key >> 4) * 16 * ROW_BYTES + (key >> 2 & 1) * (D * 16) + (key >> 3 & 1) * 8 + (key & 3) * 2;
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) {
+            const uint32_t x = *(const __attribute__((address_space(3))) uint16_t*)(uintptr_t)(row_at + (32 * d + 8 * (i >> 2) + 4 * half + (i & 3)) * 16);
+            if (key <= rel && (dense_odd<T>(x) & 0x8000u)) o[d][i] = __builtin_nanf("");
+          }
+      }
+    }
+    if (!F8 && __ballot(odd != 0)) {
       const int rel = limit - kb * kKeys, half = anew(lane) >> 5;
       uint32_t none = 0;                             // of this lane's keys, those with a score of -inf
 #pragma unroll 1
@@ -506,6 +569,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
       const int i0 = anew(lane), half = i0 >> 5, r = 32 * wave + (i0 & 31);
       const float sum = halves_sum(l[0] + l[1]);
       if (half == 0) { part[2 * r] = m; part[2 * r + 1] = sum; }
+      if constexpr (F8) {                            // (row 16 y + x of two tiles is dim 4 x + y, and 4 x + y + 2)
+#pragma unroll
+        for (int d = 0; d < ND; d += 2)
+#pragma unroll
+          for (int i = 0; i < 8; i++)
+            *(v4f*)(part + 2 * ROWS + r * D + 32 * d + 32 * (i >> 2) + 16 * half + 4 * (i & 3)) = v4f{o[d][i], o[d][8 + i], o[d + 1][i], o[d + 1][8 + i]};
+        break;
+      }
 #pragma unroll
       for (int d = 0; d < ND; d++)
 #pragma unroll
@@ -526,7 +597,16 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     const int i0 = anew(lane), row = wrow + (i0 & 31);
     if (row < NR) {
       const int tok = row / p.G;
-      uint16_t* const to = p.out + (int64_t)(q_start + tok) * p.out_ld + (kv * p.G + row - tok * p.G) * D + (i0 >> 5) * 8;
+      uint16_t* const to = p.out + (int64_t)(q_start + tok) * p.out_ld + (kv * p.G + row - tok * p.G) * D + (i0 >> 5) * (F8 ? 16 : 8);
+      if constexpr (F8) {                            // a half has 16 dims in a row of 32
+#pragma unroll
+        for (int d = 0; d < ND; d += 2)
+#pragma unroll
+          for (int i = 0; i < 8; i += 2)
+            *(v4i*)(to + 32 * d + 32 * (i >> 2) + 4 * (i & 3)) =
+                v4i{(int)dense_pack<T>(o[d][i] * inv, o[d][8 + i] * inv), (int)dense_pack<T>(o[d + 1][i] * inv, o[d + 1][8 + i] * inv),
+                    (int)dense_pack<T>(o[d][i + 1] * inv, o[d][9 + i] * inv), (int)dense_pack<T>(o[d + 1][i + 1] * inv, o[d + 1][9 + i] * inv)};
+      } else
 #pragma unroll
       for (int d = 0; d < ND; d++)
 #pragma unroll
@@ -598,8 +678,9 @@ __global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) 
   __builtin_memcpy(__builtin_assume_aligned(p.out + (int64_t)(at.q_start + t) * p.out_ld + (kv * p.G + row - t * p.G) * D + x, N * 2), out, N * 2);
 }
 
-template <class T, int D, bool PAGED>
+template <class T, int D, DenseKeys KEYS>
 hipError_t launch(DensePromptParams& p, hipStream_t s) {
+  constexpr bool PAGED = KEYS != DenseKeys::packed;
   constexpr int NW = 4, ROWS = 32 * NW;
   static_assert(ROWS == kDensePromptRows, "");
   const DensePromptGrid grid = dense_prompt_grid(p.n_q, p.B, p.Hkv, p.G, p.causal != 0);
@@ -609,18 +690,19 @@ hipError_t launch(DensePromptParams& p, hipStream_t s) {
   const int64_t keys = PAGED ? (int64_t)p.pages.max_pages * p.pages.page_rows : p.n_kv;
   const int64_t most = std::min<int64_t>({32, kDensePromptParts / wgs, (keys + kKeys - 1) / kKeys / kLeastBlocks});
   p.splits = p.pairs ? 1 : (int)std::max<int64_t>(most, 1);
-  k_dense_prompt<T, D, PAGED, NW><<<dim3((unsigned)(wgs * p.splits)), 64 * NW, 0, s>>>(p);
+  k_dense_prompt<T, D, KEYS, NW><<<dim3((unsigned)(wgs * p.splits)), 64 * NW, 0, s>>>(p);
   if (p.splits > 1) k_dense_prompt_join<T, D, PAGED, ROWS><<<dim3((unsigned)wgs, ROWS / 16), 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t wsvd_launch_dense_prompt(DensePromptParams& p, int dtype, int d, bool paged, hipStream_t s) {
-  if (dtype == WSVD_BF16) {
-    if (d == 128) return paged ? launch<DenseBf16, 128, true>(p, s) : launch<DenseBf16, 128, false>(p, s);
-    return paged ? launch<DenseBf16, 64, true>(p, s) : launch<DenseBf16, 64, false>(p, s);
-  }
-  if (d == 128) return paged ? launch<DenseF16, 128, true>(p, s) : launch<DenseF16, 128, false>(p, s);
-  return paged ? launch<DenseF16, 64, true>(p, s) : launch<DenseF16, 64, false>(p, s);
+template <class T, int D>
+static hipError_t launch_keys(DensePromptParams& p, DenseKeys keys, hipStream_t s) {
+  return keys == DenseKeys::packed ? launch<T, D, DenseKeys::packed>(p, s) : keys == DenseKeys::paged ? launch<T, D, DenseKeys::paged>(p, s)
+                                                                                                 : launch<T, D, DenseKeys::paged_f8>(p, s);
+}
+hipError_t wsvd_launch_dense_prompt(DensePromptParams& p, int dtype, int d, DenseKeys keys, hipStream_t s) {
+  if (dtype == WSVD_BF16) return d == 128 ? launch_keys<DenseBf16, 128>(p, keys, s) : launch_keys<DenseBf16, 64>(p, keys, s);
+  return d == 128 ? launch_keys<DenseF16, 128>(p, keys, s) : launch_keys<DenseF16, 64>(p, keys, s);
 }

@@ -1,0 +1,238 @@
+// Page tables kept on the GPU: the pages of finished sequences back to a free list, and pages from it for the new tokens of a step, with the
+// tokens' prefix sums, positions and slots.  Latency is what counts: a step's tables are a few KB to a MB.
+#include "wsvd_dense.h"
+
+namespace {
+
+constexpr int kSeqs = 1024;                          // sequences at a time: one a thread
+
+struct PagesParams {
+  int *table, *free_pages;
+  const int *lens, *n_free, *what;                   // what: new tokens, or which sequences are done
+  int *lens_out, *n_free_out;
+  int *cu, *positions, *slots;
+  int B, R, max_pages, n_pages, n_tokens;
+  int* err_word;
+  int* counter;                                      // of workgroups, zero between launches
+};
+
+// Exclusive prefix sum of one number a thread over the workgroup, and the sum of all.  Numbers are at most 2^24; sums within a wave that pass
+// 2^25 are taken as that, so that nothing overflows (and what begins behind such a one begins behind 2^24).
+struct Scan { int wave[kSeqs / 64]; };
+WSVD_DEV int scan_exclusive(Scan& sh, int x, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockDim.x >> 6;
+  const int incl = min(wave_prefix_int(x), 1 << 25);
+  __syncthreads();                                   // (the sums of the call before have been read)
+  if (lane == 63) sh.wave[wave] = incl;
+  __syncthreads();
+  const int sums = wave_prefix_int(lane < n ? sh.wave[lane] : 0);
+  total = __builtin_amdgcn_readlane(sums, 63);
+  return incl - x + (wave > 0 ? __shfl(sums, wave - 1) : 0);
+}
+// The last i in [0, n) with first[i] <= x, where first[0] <= x.
+WSVD_DEV int last_at_most(const int* first, int n, int x) {
+  int i = 0;
+  for (int step = kSeqs / 2; step > 0; step >>= 1)
+    if (i + step < n && first[i + step] <= x) i += step;
+  return i;
+}
+
+// Every workgroup finds all sequences' first tokens and pages from the lengths, in one pass; table entries and tokens are dealt out.  A new
+// page is the free list's, not the table's: nobody reads what another workgroup writes.  Lengths and the free list's length may be
+// updated in place, so the last workgroup to come writes them, when all have read them.
+__global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
+  __shared__ Scan scan;
+  __shared__ int cu_sh[kSeqs], page_sh[kSeqs], len_sh[kSeqs];
+  __shared__ int last_sh;
+  const int tid = threadIdx.x, wg = blockIdx.x, wgs = gridDim.x;
+  const int R = p.R, cap = p.max_pages * R;
+  const int n_free = min(max(*p.n_free, 0), p.n_pages);
+  int err = 0;
+  auto free_page = [&](int i) {
+    if (i >= n_free) { err = err ? err : (int)WSVD_E_CAPACITY; return -1; }
+    const int page = p.free_pages[n_free - 1 - i];
+    if (page < 0 || page >= p.n_pages) { err = WSVD_E_SHAPE; return -1; }
+    return page;
+  };
+  // a thread's sequence: rows before, new ones, pages before, new ones, the first token and the first new page's number in the step
+  int len, add, have, need, t0, p0;
+  int tokens = 0, pages = 0;                         // of the sequences before
+  auto place = [&](int base) {
+    const int b = base + tid, old = b < p.B ? p.lens[b] : 0, more = b >= p.B ? 0 : p.what ? p.what[b] : 1;
+    len = min(max(old, 0), cap);
+    add = min(max(more, 0), 1 << 24);
+    int total;
+    t0 = tokens + scan_exclusive(scan, add, total);
+    add = max(min(add, p.n_tokens - t0), 0);
+    t0 = min(t0, p.n_tokens);
+    tokens = min(tokens + total, p.n_tokens);
+    if (len != old || add != more) err = WSVD_E_SHAPE;
+    else if (add > cap - len) err = err ? err : (int)WSVD_E_CAPACITY;
+    have = (len + R - 1) / R;
+    need = min((len + add + R - 1) / R, p.max_pages) - have;
+    p0 = pages + scan_exclusive(scan, need, total);
+    pages += total;
+  };
+  auto commit = [&](int base) { if (base + tid < p.B) p.lens_out[base + tid] = len + add; };
+  for (int base = 0; base < p.B; base += kSeqs) {
+    const int b = base + tid, n_here = min(p.B - base, kSeqs), first_token = tokens, first_page = pages;
+    place(base);
+    cu_sh[tid] = t0; page_sh[tid] = p0; len_sh[tid] = len;
+    if (wg == 0 && p.cu && b < p.B) p.cu[b] = t0;
+    __syncthreads();
+    for (int i = first_page + wg * kSeqs + tid; i < pages; i += wgs * kSeqs) {
+      const int s = last_at_most(page_sh, n_here, i);
+      p.table[(size_t)(base + s) * p.max_pages + (len_sh[s] + R - 1) / R + i - page_sh[s]] = free_page(i);
+    }
+    if (p.positions || p.slots)
+      for (int t = first_token + wg * kSeqs + tid; t < tokens; t += wgs * kSeqs) {
+        const int s = last_at_most(cu_sh, n_here, t), row = len_sh[s] + t - cu_sh[s];
+        if (p.positions) p.positions[t] = row;
+        if (p.slots) {
+          const int pg = row / R, had = (len_sh[s] + R - 1) / R;
+          int page = -1;
+          if (pg < had) {
+            page = p.table[(size_t)(base + s) * p.max_pages + pg];
+            if (page < 0 || page >= p.n_pages) { page = -1; err = WSVD_E_SHAPE; }
+          } else if (pg < p.max_pages) {
+            page = free_page(page_sh[s] + pg - had);
+          }
+          p.slots[t] = page < 0 ? -1 : page * R + row - pg * R;
+        }
+      }
+    if (wgs == 1) commit(base);                      // (what is read of the lengths later is other sequences')
+  }
+  if (err) atomicExch(p.err_word, err);
+  if (wgs > 1) {
+    __syncthreads();
+    if (tid == 0) {
+      last_sh = atomicAdd(p.counter, 1) == wgs - 1;
+      if (last_sh) atomicExch(p.counter, 0);
+    }
+    __syncthreads();
+    if (!last_sh) return;
+    const int all_tokens = tokens, all_pages = pages;
+    if (p.B > kSeqs) tokens = pages = 0;
+    for (int base = 0; base < p.B; base += kSeqs) {
+      if (p.B > kSeqs) place(base);
+      commit(base);
+    }
+    tokens = all_tokens; pages = all_pages;
+  }
+  if (tid == 0) {
+    *p.n_free_out = max(n_free - pages, 0);
+    if (p.cu) p.cu[p.B] = tokens;
+  }
+}
+
+// Pages of the sequences that are done, in the order of sequences and rows, behind the free list's last; entries that are no page are left
+// out.  A wave counts a sequence's pages, and writes them once it is known where they begin.
+__global__ __launch_bounds__(kSeqs) void k_pages_release(PagesParams p) {
+  __shared__ Scan scan;
+  __shared__ int count_sh[kSeqs], first_sh[kSeqs];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n_free = min(max(*p.n_free, 0), p.n_pages);
+  int at = n_free;
+  bool bad = false;
+  for (int base = 0; base < p.B; base += kSeqs) {
+    const int b = base + tid, n_here = min(p.B - base, kSeqs);
+    const int len = b < p.B ? min(max(p.lens[b], 0), p.max_pages * p.R) : 0;
+    const bool done = b < p.B && p.what[b] != 0;
+    __syncthreads();
+    first_sh[tid] = done ? (len + p.R - 1) / p.R : 0;
+    count_sh[tid] = 0;
+    __syncthreads();
+    auto each = [&](auto use) {
+      for (int s = wave; s < n_here; s += kSeqs / 64) {
+        const int n = __builtin_amdgcn_readfirstlane(use.pages(s));
+        int before = 0;
+        for (int i0 = 0; i0 < n; i0 += 64) {
+          const int i = i0 + lane, page = i < n ? p.table[(size_t)(base + s) * p.max_pages + i] : -1;
+          const unsigned long long m = __ballot(page >= 0 && page < p.n_pages);
+          use.put(s, before + __builtin_popcountll(m & ((1ull << lane) - 1)), page, (m >> lane) & 1);
+          before += __builtin_popcountll(m);
+        }
+        use.counted(s, before);
+      }
+    };
+    struct Count {
+      int *n, *count, lane;
+      WSVD_DEV int pages(int s) { return n[s]; }
+      WSVD_DEV void put(int, int, int, bool) {}
+      WSVD_DEV void counted(int s, int k) { if (lane == 0) count[s] = k; }
+    };
+    each(Count{first_sh, count_sh, lane});
+    __syncthreads();
+    const int pages = first_sh[tid], mine = count_sh[tid];
+    int total;
+    const int first = at + scan_exclusive(scan, mine, total);
+    count_sh[tid] = pages; first_sh[tid] = first;
+    __syncthreads();
+    struct Write {
+      int *n, *first, *free_pages, n_pages; bool* bad;
+      WSVD_DEV int pages(int s) { return n[s]; }
+      WSVD_DEV void put(int s, int i, int page, bool valid) {
+        if (!valid) return;
+        if (first[s] + i < n_pages) free_pages[first[s] + i] = page; else *bad = true;       // (a page given back twice)
+      }
+      WSVD_DEV void counted(int, int) {}
+    };
+    each(Write{count_sh, first_sh, p.free_pages, p.n_pages, &bad});
+    at += total;
+    if (b < p.B) p.lens_out[b] = done ? 0 : p.lens[b];
+  }
+  if (bad) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+  if (tid == 0) *p.n_free_out = min(at, p.n_pages);
+}
+
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+wsvd_status check_pool(const wsvd_page_pool* c) {
+  if (!c || !c->block_table || !c->free_pages) return WSVD_E_NULL;
+  if (c->batch < 1 || c->batch > 65536 || c->page_rows < 16 || c->page_rows % 16 != 0 || c->page_rows > 4096 || c->max_pages < 1 || c->n_pages < 1) return WSVD_E_SHAPE;
+  if ((int64_t)c->max_pages * c->page_rows > ((int64_t)1 << 27) || (int64_t)c->n_pages * c->page_rows > 0x7FFFFFFF) return WSVD_E_SHAPE;
+  if (!aligned4(c->block_table) || !aligned4(c->free_pages)) return WSVD_E_ALIGN;
+  return WSVD_OK;
+}
+PagesParams params_of(const wsvd_ctx* ctx, const wsvd_page_pool* c) {
+  PagesParams p = {};
+  p.table = c->block_table; p.free_pages = c->free_pages;
+  p.B = c->batch; p.R = c->page_rows; p.max_pages = c->max_pages; p.n_pages = c->n_pages;
+  p.err_word = ctx->err_word; p.counter = ctx->readers;
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+wsvd_status wsvd_pages_grow(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int32_t* new_lens, int64_t n_tokens, const int32_t* seq_lens,
+                            const int32_t* n_free, int32_t* seq_lens_out, int32_t* n_free_out, int32_t* cu_tokens, int32_t* positions,
+                            int32_t* slots, void* hip_stream) {
+  if (!ctx || !seq_lens || !n_free || !seq_lens_out || !n_free_out) return WSVD_E_NULL;
+  const wsvd_status st = check_pool(pool);
+  if (st != WSVD_OK) return st;
+  for (const void* x : {(const void*)new_lens, (const void*)seq_lens, (const void*)n_free, (const void*)seq_lens_out, (const void*)n_free_out,
+                        (const void*)cu_tokens, (const void*)positions, (const void*)slots})
+    if (!aligned4(x)) return WSVD_E_ALIGN;
+  if (n_tokens < 0 || n_tokens > ((int64_t)1 << 24) || (!new_lens && n_tokens != pool->batch)) return WSVD_E_SHAPE;
+  PagesParams p = params_of(ctx, pool);
+  p.lens = seq_lens; p.n_free = n_free; p.what = new_lens; p.lens_out = seq_lens_out; p.n_free_out = n_free_out;
+  p.cu = cu_tokens; p.positions = positions; p.slots = slots; p.n_tokens = (int)n_tokens;
+  k_pages_grow<<<pages_workgroups(n_tokens), kSeqs, 0, (hipStream_t)hip_stream>>>(p);
+  return hipGetLastError() == hipSuccess ? WSVD_OK : WSVD_E_HIP;
+}
+
+wsvd_status wsvd_pages_release(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int32_t* done, const int32_t* seq_lens, const int32_t* n_free,
+                               int32_t* seq_lens_out, int32_t* n_free_out, void* hip_stream) {
+  if (!ctx || !done || !seq_lens || !n_free || !seq_lens_out || !n_free_out) return WSVD_E_NULL;
+  const wsvd_status st = check_pool(pool);
+  if (st != WSVD_OK) return st;
+  for (const void* x : {(const void*)done, (const void*)seq_lens, (const void*)n_free, (const void*)seq_lens_out, (const void*)n_free_out})
+    if (!aligned4(x)) return WSVD_E_ALIGN;
+  PagesParams p = params_of(ctx, pool);
+  p.lens = seq_lens; p.n_free = n_free; p.what = done; p.lens_out = seq_lens_out; p.n_free_out = n_free_out;
+  k_pages_release<<<1, kSeqs, 0, (hipStream_t)hip_stream>>>(p);
+  return hipGetLastError() == hipSuccess ? WSVD_OK : WSVD_E_HIP;
+}
+
+}  // extern "C"
