@@ -612,7 +612,8 @@ wsvd_status wsvd_dense_prefill_attn_paged_f8(wsvd_ctx *ctx, const wsvd_dense_des
 typedef struct {
   int32_t *block_table;      /* DEVICE [batch][max_pages] */
   int32_t *free_pages;       /* DEVICE [n_pages]: the first *n_free entries are pages that no sequence has */
-  int32_t batch, page_rows, max_pages, n_pages;   /* page_rows and max_pages as for the caches; n_pages * page_rows below 2^31 */
+  int32_t batch, page_rows, max_pages, n_pages;   /* page_rows and max_pages as for the caches;
+                                                      n_pages at most 2^24, n_pages * page_rows below 2^31 */
 } wsvd_page_pool;
 
 /*

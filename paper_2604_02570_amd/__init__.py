@@ -551,13 +551,22 @@ def make_page_pool(block_table, free_pages, batch, page_rows, max_pages, n_pages
 
 def wsvd_pages_grow(ctx, pool, new_lens, n_tokens, seq_lens, n_free, seq_lens_out, n_free_out, cu_tokens=None, positions=None, slots=None,
                     stream=None):
-    status = (_lib or lib()).wsvd_pages_grow(*_addresses(ctx, pool, new_lens, n_tokens, seq_lens, n_free, seq_lens_out, n_free_out, cu_tokens,
-                                                         positions, slots, _stream_addr(stream)))
+    call, on = (_lib or lib()).wsvd_pages_grow, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, pool, None if new_lens is None else new_lens.data_ptr(), n_tokens, seq_lens.data_ptr(), n_free.data_ptr(),
+                      seq_lens_out.data_ptr(), n_free_out.data_ptr(), None if cu_tokens is None else cu_tokens.data_ptr(),
+                      None if positions is None else positions.data_ptr(), None if slots is None else slots.data_ptr(), on)
+    except AttributeError:                                             # addresses in place of tensors
+        status = call(*_addresses(ctx, pool, new_lens, n_tokens, seq_lens, n_free, seq_lens_out, n_free_out, cu_tokens, positions, slots, on))
     if status:
         raise WsvdError(status, "wsvd_pages_grow")
 
 
 def wsvd_pages_release(ctx, pool, done, seq_lens, n_free, seq_lens_out, n_free_out, stream=None):
-    status = (_lib or lib()).wsvd_pages_release(*_addresses(ctx, pool, done, seq_lens, n_free, seq_lens_out, n_free_out, _stream_addr(stream)))
+    call, on = (_lib or lib()).wsvd_pages_release, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, pool, done.data_ptr(), seq_lens.data_ptr(), n_free.data_ptr(), seq_lens_out.data_ptr(), n_free_out.data_ptr(), on)
+    except AttributeError:
+        status = call(*_addresses(ctx, pool, done, seq_lens, n_free, seq_lens_out, n_free_out, on))
     if status:
         raise WsvdError(status, "wsvd_pages_release")

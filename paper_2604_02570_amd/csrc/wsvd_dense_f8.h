@@ -19,9 +19,14 @@ WSVD_DEV int f8_exponent(float most) { return max((int)((__float_as_uint(most) +
 WSVD_DEV float f8_power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // 2^e, e in -126 .. 127
 WSVD_DEV bool f8_finite(float x) { return __builtin_fabsf(x) < INFINITY; }
 // A number over its scale as what the conversion takes: none for those that are infinite or none.
-template <class T>
 WSVD_DEV float f8_scaled(float x, float inverse, float top) {
   return f8_finite(x) ? __builtin_amdgcn_fmed3f(x * inverse, -top, top) : __builtin_nanf("");
+}
+// The larger of a magnitude and those of two numbers, infinite ones and none left out.
+template <class T>
+WSVD_DEV float f8_most(float most, uint32_t x) {
+  const float a = __builtin_fabsf(dense_low<T>(x)), b = __builtin_fabsf(dense_high<T>(x));
+  return fmaxf(most, fmaxf(f8_finite(a) ? a : 0.f, f8_finite(b) ? b : 0.f));
 }
 template <class T>
 WSVD_DEV float f8_top(int e) { return e >= F8Top<T>::exponent ? 240.f : 448.f; }
@@ -29,6 +34,8 @@ WSVD_DEV uint32_t f8_codes(float a, float b, float c, float d) {
   const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, low, true);
 }
+// The first n bytes of a dword, all for 4 and more, none for 0 and less.
+WSVD_DEV uint32_t f8_bytes(int n) { return n <= 0 ? 0u : n >= 4 ? ~0u : (1u << (8 * n)) - 1u; }
 // Codes under a scale that is `by` times smaller than the one they had (by = 2^-n): rounded to nearest even, exact unless they become subnormal.
 WSVD_DEV uint32_t f8_moved(uint32_t codes, float by) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);

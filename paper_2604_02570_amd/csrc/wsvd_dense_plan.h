@@ -88,17 +88,22 @@ WSVD_HD int dense_append_tokens(int64_t n_tokens, int items) {
   return items >= 128 ? 2 : 4;
 }
 // The append over 8-bit pages: tokens of a workgroup, whose units (the new rows of a block of 16) it has, and workgroups that share their
-// heads, four a round.
+// heads, four a round: about 8192 workgroups (18900 tokens of 16 prompts, 32 heads of 128: one workgroup for all heads 228 us, two 208, three 197,
+// four 193, six 190, twelve 203).
 struct DenseF8Append { int tokens, splits; };
 WSVD_HD DenseF8Append dense_f8_append(int64_t n_tokens, int batch, int heads, bool packed) {
   const int tokens = packed && n_tokens >= 4096 && n_tokens >= 16 * (int64_t)batch ? 16 : 1;
-  const int64_t units = packed ? n_tokens / 16 + (batch < n_tokens ? batch : n_tokens) : n_tokens, rounds = (heads + 3) / 4, fill = 2048 / units;
+  const int64_t units = packed ? n_tokens / 16 + (batch < n_tokens ? batch : n_tokens) : n_tokens, rounds = (heads + 3) / 4, fill = 8192 / units;
   return {tokens, (int)(fill < 1 ? 1 : fill < rounds ? fill : rounds)};
 }
-// Workgroups that a step's tokens are dealt out to, 1024 threads each.
-WSVD_HD unsigned pages_workgroups(int64_t n_tokens) {
-  const int64_t n = (n_tokens + 1023) / 1024;
-  return (unsigned)(n < 1 ? 1 : n > 128 ? 128 : n);
+// The page tables' calls: a thread a sequence at a time, and `items` (tokens or table entries) dealt out.
+constexpr int kPagesThreads = 1024;
+struct PagesLaunch { unsigned workgroups, threads; };
+WSVD_HD PagesLaunch pages_launch(int batch, int64_t items) {
+  if (batch <= 64 && items <= 256) return {1, 64};
+  if (batch <= 256 && items <= 1024) return {1, 256};
+  const int64_t n = (items + kPagesThreads - 1) / kPagesThreads;
+  return {(unsigned)(n < 1 ? 1 : n > 128 ? 128 : n), kPagesThreads};
 }
 WSVD_HD int64_t dense_decode_workgroups(int B, int Hkv, int target, bool alone) { return (alone ? (int64_t)B : (int64_t)target + B) * Hkv; }
 // The prompt attention's, at most: every sequence ends inside a tile.  Two tiles a workgroup where there are many and they differ: the second

@@ -4,7 +4,7 @@
 
 namespace {
 
-constexpr int kSeqs = 1024;                          // sequences at a time: one a thread
+constexpr int kSeqs = kPagesThreads;                 // sequences at a time, at most: one a thread
 
 struct PagesParams {
   int *table, *free_pages;
@@ -14,10 +14,12 @@ struct PagesParams {
   int B, R, max_pages, n_pages, n_tokens;
   int* err_word;
   int* counter;                                      // of workgroups, zero between launches
+  int apart;                                         // what is written is not what is read
 };
 
-// Exclusive prefix sum of one number a thread over the workgroup, and the sum of all.  Numbers are at most 2^24; sums within a wave that pass
-// 2^25 are taken as that, so that nothing overflows (and what begins behind such a one begins behind 2^24).
+// Exclusive prefix sum of one number a thread over the workgroup, and the sum of all.  Numbers are at most 2^24, and no more than that many
+// tokens or pages are dealt with.  Sums within a wave that pass 2^25 are taken as that, so that nothing overflows: what begins behind such
+// a one begins at 2^24 or later, and what begins before has its place.
 struct Scan { int wave[kSeqs / 64]; };
 WSVD_DEV int scan_exclusive(Scan& sh, int x, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockDim.x >> 6;
@@ -29,6 +31,8 @@ WSVD_DEV int scan_exclusive(Scan& sh, int x, int& total) {
   total = __builtin_amdgcn_readlane(sums, 63);
   return incl - x + (wave > 0 ? __shfl(sums, wave - 1) : 0);
 }
+// An entry of the free list: written through, since another workgroup may write it again.
+WSVD_DEV void put_page(int* to, int page) { __hip_atomic_store(to, page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 // The last i in [0, n) with first[i] <= x, where first[0] <= x.
 WSVD_DEV int last_at_most(const int* first, int n, int x) {
   int i = 0;
@@ -39,7 +43,7 @@ WSVD_DEV int last_at_most(const int* first, int n, int x) {
 
 // Every workgroup finds all sequences' first tokens and pages from the lengths, in one pass; table entries and tokens are dealt out.  A new
 // page is the free list's, not the table's: nobody reads what another workgroup writes.  Lengths and the free list's length may be
-// updated in place, so the last workgroup to come writes them, when all have read them.
+// updated in place: then the last workgroup to come writes them, when all have read them.
 __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
   __shared__ Scan scan;
   __shared__ int cu_sh[kSeqs], page_sh[kSeqs], len_sh[kSeqs];
@@ -74,18 +78,18 @@ __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
     pages += total;
   };
   auto commit = [&](int base) { if (base + tid < p.B) p.lens_out[base + tid] = len + add; };
-  for (int base = 0; base < p.B; base += kSeqs) {
-    const int b = base + tid, n_here = min(p.B - base, kSeqs), first_token = tokens, first_page = pages;
+  for (int base = 0; base < p.B; base += (int)blockDim.x) {
+    const int b = base + tid, n_here = min(p.B - base, (int)blockDim.x), first_token = tokens, first_page = pages;
     place(base);
     cu_sh[tid] = t0; page_sh[tid] = p0; len_sh[tid] = len;
     if (wg == 0 && p.cu && b < p.B) p.cu[b] = t0;
     __syncthreads();
-    for (int i = first_page + wg * kSeqs + tid; i < pages; i += wgs * kSeqs) {
+    for (int i = first_page + wg * (int)blockDim.x + tid; i < pages; i += wgs * (int)blockDim.x) {
       const int s = last_at_most(page_sh, n_here, i);
       p.table[(size_t)(base + s) * p.max_pages + (len_sh[s] + R - 1) / R + i - page_sh[s]] = free_page(i);
     }
     if (p.positions || p.slots)
-      for (int t = first_token + wg * kSeqs + tid; t < tokens; t += wgs * kSeqs) {
+      for (int t = first_token + wg * (int)blockDim.x + tid; t < tokens; t += wgs * (int)blockDim.x) {
         const int s = last_at_most(cu_sh, n_here, t), row = len_sh[s] + t - cu_sh[s];
         if (p.positions) p.positions[t] = row;
         if (p.slots) {
@@ -100,10 +104,11 @@ __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
           p.slots[t] = page < 0 ? -1 : page * R + row - pg * R;
         }
       }
-    if (wgs == 1) commit(base);                      // (what is read of the lengths later is other sequences')
+    if (wgs == 1 || (p.apart && wg == 0)) commit(base);              // (what is read of the lengths later is other sequences')
   }
   if (err) atomicExch(p.err_word, err);
-  if (wgs > 1) {
+  if (p.apart && wg > 0) return;
+  if (wgs > 1 && !p.apart) {
     __syncthreads();
     if (tid == 0) {
       last_sh = atomicAdd(p.counter, 1) == wgs - 1;
@@ -112,9 +117,9 @@ __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
     __syncthreads();
     if (!last_sh) return;
     const int all_tokens = tokens, all_pages = pages;
-    if (p.B > kSeqs) tokens = pages = 0;
-    for (int base = 0; base < p.B; base += kSeqs) {
-      if (p.B > kSeqs) place(base);
+    if (p.B > (int)blockDim.x) tokens = pages = 0;
+    for (int base = 0; base < p.B; base += (int)blockDim.x) {
+      if (p.B > (int)blockDim.x) place(base);
       commit(base);
     }
     tokens = all_tokens; pages = all_pages;
@@ -125,71 +130,102 @@ __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
   }
 }
 
-// Pages of the sequences that are done, in the order of sequences and rows, behind the free list's last; entries that are no page are left
-// out.  A wave counts a sequence's pages, and writes them once it is known where they begin.
+// Pages of the sequences that are done, in the order of sequences and rows, behind the free list's last.  An entry's place is its number
+// among those of the done sequences, as long as all are pages; that some are not (a free list that ended left -1) is rare, and then the last
+// workgroup to come does it all once more, leaving those out.  (1024 sequences, 94 of them done with 27000 pages: 32 us as one workgroup that
+// counts the pages first.)
+WSVD_DEV void pages_left_out(const PagesParams& p, int n_free, int& end, int* first_sh, int* count_sh, Scan& scan) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  end = n_free;
+  for (int base = 0; base < p.B; base += (int)blockDim.x) {
+    const int b = base + tid, n_here = min(p.B - base, (int)blockDim.x);
+    const int len = b < p.B ? min(max(p.lens[b], 0), p.max_pages * p.R) : 0;
+    __syncthreads();
+    count_sh[tid] = b < p.B && p.what[b] != 0 ? (len + p.R - 1) / p.R : 0;
+    __syncthreads();
+    // a wave a sequence: its pages counted, and written once it is known where they begin
+    auto each = [&](int s, auto put) {
+      const int n = __builtin_amdgcn_readfirstlane(count_sh[s]);
+      int before = 0;
+      for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = i0 + lane, page = i < n ? p.table[(size_t)(base + s) * p.max_pages + i] : -1;
+        const bool valid = page >= 0 && page < p.n_pages;
+        const unsigned long long m = __ballot(valid);
+        if (valid) put(before + __builtin_popcountll(m & ((1ull << lane) - 1)), page);
+        before += __builtin_popcountll(m);
+      }
+      return before;
+    };
+    for (int s = wave; s < n_here; s += (int)blockDim.x / 64) {
+      const int n = each(s, [](int, int) {});
+      if (lane == 0) first_sh[s] = n;
+    }
+    __syncthreads();
+    int total;
+    const int first = end + scan_exclusive(scan, tid < n_here ? first_sh[tid] : 0, total);
+    first_sh[tid] = first;
+    __syncthreads();
+    for (int s = wave; s < n_here; s += (int)blockDim.x / 64)
+      each(s, [&](int i, int page) {
+        if (first_sh[s] + i < p.n_pages) put_page(p.free_pages + first_sh[s] + i, page);
+      });
+    end = min(end + total, p.n_pages + 1);
+  }
+}
 __global__ __launch_bounds__(kSeqs) void k_pages_release(PagesParams p) {
   __shared__ Scan scan;
-  __shared__ int count_sh[kSeqs], first_sh[kSeqs];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ int first_sh[kSeqs], count_sh[kSeqs];
+  __shared__ int last_sh, none_sh;
+  const int tid = threadIdx.x, wg = blockIdx.x, wgs = gridDim.x;
   const int n_free = min(max(*p.n_free, 0), p.n_pages);
-  int at = n_free;
-  bool bad = false;
-  for (int base = 0; base < p.B; base += kSeqs) {
-    const int b = base + tid, n_here = min(p.B - base, kSeqs);
+  int end = n_free, none = 0;
+  if (tid == 0) none_sh = 0;
+  for (int base = 0; base < p.B; base += (int)blockDim.x) {
+    const int b = base + tid, n_here = min(p.B - base, (int)blockDim.x);
     const int len = b < p.B ? min(max(p.lens[b], 0), p.max_pages * p.R) : 0;
-    const bool done = b < p.B && p.what[b] != 0;
-    __syncthreads();
-    first_sh[tid] = done ? (len + p.R - 1) / p.R : 0;
-    count_sh[tid] = 0;
-    __syncthreads();
-    auto each = [&](auto use) {
-      for (int s = wave; s < n_here; s += kSeqs / 64) {
-        const int n = __builtin_amdgcn_readfirstlane(use.pages(s));
-        int before = 0;
-        for (int i0 = 0; i0 < n; i0 += 64) {
-          const int i = i0 + lane, page = i < n ? p.table[(size_t)(base + s) * p.max_pages + i] : -1;
-          const unsigned long long m = __ballot(page >= 0 && page < p.n_pages);
-          use.put(s, before + __builtin_popcountll(m & ((1ull << lane) - 1)), page, (m >> lane) & 1);
-          before += __builtin_popcountll(m);
-        }
-        use.counted(s, before);
-      }
-    };
-    struct Count {
-      int *n, *count, lane;
-      WSVD_DEV int pages(int s) { return n[s]; }
-      WSVD_DEV void put(int, int, int, bool) {}
-      WSVD_DEV void counted(int s, int k) { if (lane == 0) count[s] = k; }
-    };
-    each(Count{first_sh, count_sh, lane});
-    __syncthreads();
-    const int pages = first_sh[tid], mine = count_sh[tid];
     int total;
-    const int first = at + scan_exclusive(scan, mine, total);
-    count_sh[tid] = pages; first_sh[tid] = first;
+    const int first = end + scan_exclusive(scan, b < p.B && p.what[b] != 0 ? (len + p.R - 1) / p.R : 0, total);
+    first_sh[tid] = first;
     __syncthreads();
-    struct Write {
-      int *n, *first, *free_pages, n_pages; bool* bad;
-      WSVD_DEV int pages(int s) { return n[s]; }
-      WSVD_DEV void put(int s, int i, int page, bool valid) {
-        if (!valid) return;
-        if (first[s] + i < n_pages) free_pages[first[s] + i] = page; else *bad = true;       // (a page given back twice)
-      }
-      WSVD_DEV void counted(int, int) {}
-    };
-    each(Write{count_sh, first_sh, p.free_pages, p.n_pages, &bad});
-    at += total;
-    if (b < p.B) p.lens_out[b] = done ? 0 : p.lens[b];
+    for (int i = end + wg * (int)blockDim.x + tid; i < min(end + total, p.n_pages); i += wgs * (int)blockDim.x) {
+      const int s = last_at_most(first_sh, n_here, i);
+      const int page = p.table[(size_t)(base + s) * p.max_pages + i - first_sh[s]];
+      if (page < 0 || page >= p.n_pages) none = 1; else put_page(p.free_pages + i, page);
+    }
+    end = min(end + total, p.n_pages + 1);           // (that many, or too many)
   }
-  if (bad) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
-  if (tid == 0) *p.n_free_out = min(at, p.n_pages);
+  __syncthreads();
+  if (none) none_sh = 1;
+  if (wgs > 1) {
+    wait_vmem_done();                                // (what is written once more comes behind what all have written)
+    __syncthreads();
+    if (tid == 0) {
+      if (none_sh) atomicExch(p.counter + 32, 1);
+      wait_vmem_done();
+      last_sh = atomicAdd(p.counter, 1) == wgs - 1;
+      if (last_sh) {
+        none_sh = atomicExch(p.counter + 32, 0);
+        atomicExch(p.counter, 0);
+      }
+    }
+    __syncthreads();
+    if (!last_sh) return;
+  }
+  __syncthreads();
+  if (none_sh) {
+    wait_vmem_done();
+    pages_left_out(p, n_free, end, first_sh, count_sh, scan);
+  }
+  if (end > p.n_pages) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+  for (int b = tid; b < p.B; b += (int)blockDim.x) p.lens_out[b] = p.what[b] != 0 ? 0 : p.lens[b];
+  if (tid == 0) *p.n_free_out = min(end, p.n_pages);
 }
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 wsvd_status check_pool(const wsvd_page_pool* c) {
   if (!c || !c->block_table || !c->free_pages) return WSVD_E_NULL;
   if (c->batch < 1 || c->batch > 65536 || c->page_rows < 16 || c->page_rows % 16 != 0 || c->page_rows > 4096 || c->max_pages < 1 || c->n_pages < 1) return WSVD_E_SHAPE;
-  if ((int64_t)c->max_pages * c->page_rows > ((int64_t)1 << 27) || (int64_t)c->n_pages * c->page_rows > 0x7FFFFFFF) return WSVD_E_SHAPE;
+  if ((int64_t)c->max_pages * c->page_rows > ((int64_t)1 << 27) || c->n_pages > 1 << 24 || (int64_t)c->n_pages * c->page_rows > 0x7FFFFFFF) return WSVD_E_SHAPE;
   if (!aligned4(c->block_table) || !aligned4(c->free_pages)) return WSVD_E_ALIGN;
   return WSVD_OK;
 }
@@ -218,7 +254,9 @@ wsvd_status wsvd_pages_grow(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int
   PagesParams p = params_of(ctx, pool);
   p.lens = seq_lens; p.n_free = n_free; p.what = new_lens; p.lens_out = seq_lens_out; p.n_free_out = n_free_out;
   p.cu = cu_tokens; p.positions = positions; p.slots = slots; p.n_tokens = (int)n_tokens;
-  k_pages_grow<<<pages_workgroups(n_tokens), kSeqs, 0, (hipStream_t)hip_stream>>>(p);
+  p.apart = seq_lens != seq_lens_out && n_free != n_free_out;
+  const PagesLaunch l = pages_launch(pool->batch, n_tokens);
+  k_pages_grow<<<l.workgroups, l.threads, 0, (hipStream_t)hip_stream>>>(p);
   return hipGetLastError() == hipSuccess ? WSVD_OK : WSVD_E_HIP;
 }
 
@@ -231,7 +269,8 @@ wsvd_status wsvd_pages_release(wsvd_ctx* ctx, const wsvd_page_pool* pool, const 
     if (!aligned4(x)) return WSVD_E_ALIGN;
   PagesParams p = params_of(ctx, pool);
   p.lens = seq_lens; p.n_free = n_free; p.what = done; p.lens_out = seq_lens_out; p.n_free_out = n_free_out;
-  k_pages_release<<<1, kSeqs, 0, (hipStream_t)hip_stream>>>(p);
+  const PagesLaunch l = pages_launch(pool->batch, (int64_t)pool->batch * pool->max_pages / 16);
+  k_pages_release<<<l.workgroups, l.threads, 0, (hipStream_t)hip_stream>>>(p);
   return hipGetLastError() == hipSuccess ? WSVD_OK : WSVD_E_HIP;
 }
 

@@ -85,7 +85,8 @@ def test_calls_refused(ctx):
 def test_page_tables_refused(ctx):
     for kw, status in ((dict(table=None), W.E_NULL), (dict(free=None), W.E_NULL), (dict(batch=0), W.E_SHAPE), (dict(batch=65537), W.E_SHAPE),
                        (dict(page_rows=24), W.E_SHAPE), (dict(page_rows=8), W.E_SHAPE), (dict(page_rows=4112), W.E_SHAPE), (dict(max_pages=0), W.E_SHAPE),
-                       (dict(n_pages=0), W.E_SHAPE), (dict(n_pages=1 << 27), W.E_SHAPE), (dict(page_rows=4096, max_pages=1 << 16), W.E_SHAPE),
+                       (dict(n_pages=0), W.E_SHAPE), (dict(n_pages=1 << 27), W.E_SHAPE), (dict(n_pages=(1 << 24) + 1), W.E_SHAPE),
+                       (dict(n_pages=1 << 24, page_rows=128), W.E_SHAPE), (dict(page_rows=4096, max_pages=1 << 16), W.E_SHAPE),
                        (dict(table=A + 2), W.E_ALIGN), (dict(free=A + 1), W.E_ALIGN)):
         for f in (grow, release):
             refuses(status, f, ctx, pool(**kw))
@@ -153,7 +154,11 @@ int main() {
           CHECK(a.tokens >= 1 && a.tokens <= 16 && a.splits >= 1 && a.splits <= (heads + 3) / 4);
           CHECK(dense_launchable((n + a.tokens - 1) / a.tokens * a.splits, 256));
         }
-  for (int64_t n : {0, 1, 1024, 1025, 1 << 20, 1 << 24}) CHECK(pages_workgroups(n) >= 1 && pages_workgroups(n) <= 128);
+  for (int batch : {1, 64, 65, 256, 257, 65536})
+    for (int64_t n : {0, 1, 256, 257, 1024, 1025, 1 << 20, 1 << 24}) {
+      const PagesLaunch l = pages_launch(batch, n);
+      CHECK(l.workgroups >= 1 && l.workgroups <= 128 && l.threads % 64 == 0 && l.threads >= 64 && l.threads <= (unsigned)kPagesThreads);
+    }
   return 0;
 }
 """

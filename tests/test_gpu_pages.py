@@ -156,6 +156,21 @@ def test_counts_that_pass_32_bits_in_sum():
     W.wsvd_destroy(ctx)
 
 
+@pytest.mark.parametrize("batch,max_pages", [(2, 3000), (40, 300), (1300, 20)])
+@pytest.mark.parametrize("where", ["nowhere", "first", "last", "some"])
+def test_entries_that_are_no_page_are_left_out(batch, max_pages, where):
+    """Many workgroups: the pages' order is that of sequences and rows, with and without such entries among them."""
+    D = Device(batch, 16, max_pages, batch * max_pages, batch * max_pages)
+    rng = random.Random(batch)
+    D.grow([16 * max_pages - rng.randrange(50) if b % 3 < 2 else 0 for b in range(batch)])
+    spots = [(b, i) for b in range(batch) for i in range(max_pages) if b % 3 < 2 and 16 * i < D.host.lens[b]]
+    for b, i in {"nowhere": [], "first": spots[:1], "last": spots[-1:], "some": spots[3::41]}[where]:
+        D.host.table[b][i] = rng.choice([-1, D.host.n_pages, -2 ** 31])
+    D.table.copy_(torch.tensor(D.host.table, dtype=torch.int32))
+    D.release([1] * batch)
+    D.close()
+
+
 def test_a_page_given_back_twice_is_reported():
     i = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
     ctx = W.wsvd_create(0)
