@@ -187,7 +187,7 @@ static wsvd_status chunk(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void*
   p.q = (const uint16_t*)q; p.out = (uint16_t*)out; p.q_ld = q_ld; p.out_ld = out_ld;
   p.cu_q = cu_q; p.pages = pages_of(cache);
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads; p.causal = 1;
-  if (!dense_launchable(dense_prompt_grid(n_q, p.B, p.Hkv, p.G, true).workgroups, 256)) return WSVD_E_SHAPE;
+  if (!dense_launchable(dense_prompt_grid(n_q, p.B, p.Hkv, p.G, !f8).workgroups, 256)) return WSVD_E_SHAPE;
   WSVD_TRY(check_workspace(ctx, desc));
   p.parts = (float*)ctx->ws + kWsCounterInts;
   p.n_q = (int)n_q; p.c_scale = scale_of(desc); p.err_word = ctx->err_word; p.scales = scales_of(cache);

@@ -38,6 +38,12 @@ namespace {
 constexpr int kKeys = 64;                            // keys of a staged block
 // Blocks that a workgroup of several for one tile has at least: the join is a second launch of 4 to 5 us, a block takes 1 to 1.5.
 constexpr int kLeastBlocks = 6;
+// Over 8-bit pages more workgroups share a tile that several share at all: a block takes about as long, but the codes of a workgroup's first
+// blocks are there sooner (7 tokens behind 3000 rows, 32 / 8 heads: 19.1 us with 6 blocks at least, 17.9 with 4, 17.8 with 3, 19.4 with 2; 8 x 16 behind
+// 1000, 28 / 4: 21.4, 19.1, 20.1, 21.3; 2 x 200 behind 300, of up to 8 blocks: 17.0 for tiles left whole, 19.8 for those of 8 in two).
+constexpr int kLeastBlocksF8 = 4;
+template <bool F8>
+WSVD_HD int prompt_shares(int blocks) { return F8 ? (blocks < 2 * kLeastBlocks ? 1 : blocks / kLeastBlocksF8) : blocks / kLeastBlocks; }
 
 // lds_copy16 without the compiler's knowledge: it would let every later read of LDS wait for the copy (the next block's, while
 // this one is worked on: 16 x 2048 tokens 1124 us, with the loops' other waits gone 763).  The copies are waited for by
@@ -53,6 +59,8 @@ WSVD_DEV int anew(int x) {
   asm volatile("" : "+v"(x));
   return x;
 }
+// LDS that all waves have written so far is there, and read.
+WSVD_DEV void lds_wait_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 WSVD_DEV int anew_scalar(int x) {
   asm volatile("" : "+s"(x));
   return x;
@@ -73,8 +81,9 @@ WSVD_DEV int prompt_blocks(const DensePromptParams& p, const PromptPlace& at, in
   const int seen = p.causal ? min(at.nk, (min((tile + 1) * ROWS, at.nq * p.G) - 1) / p.G + at.ahead + 1) : at.nk;
   return seen > 0 ? (seen + kKeys - 1) / kKeys : 0;
 }
-template <bool PAGED, int ROWS>
+template <DenseKeys KEYS, int ROWS>
 WSVD_DEV bool prompt_place(const DensePromptParams& p, int idx, int lane, PromptPlace& at) {
+  constexpr bool PAGED = KEYS != DenseKeys::packed;
   const int most = PAGED ? p.pages.max_pages * p.pages.page_rows : p.n_kv;
   for (int base = 0, before = 0; base < p.B; base += 64) {
     const int i = base + lane;
@@ -107,7 +116,7 @@ WSVD_DEV bool prompt_place(const DensePromptParams& p, int idx, int lane, Prompt
       at.nk = min(max(at.nk, 0), most);
     }
     at.ahead = at.nk - at.nq;
-    at.splits = max(1, min(p.splits, prompt_blocks<ROWS>(p, at, at.tile) / kLeastBlocks));
+    at.splits = max(1, min(p.splits, prompt_shares<KEYS == DenseKeys::paged_f8>(prompt_blocks<ROWS>(p, at, at.tile))));
     return true;
   }
   return false;
@@ -130,7 +139,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   const int n = lane & 31, half = lane >> 5;
   const int kv = blockIdx.x % p.Hkv, split = blockIdx.x / p.Hkv % p.splits, idx = blockIdx.x / p.Hkv / p.splits;
   PromptPlace at;
-  if (!prompt_place<PAGED, ROWS>(p, idx, lane, at) || split >= at.splits) return;
+  if (!prompt_place<KEYS, ROWS>(p, idx, lane, at) || split >= at.splits) return;
+  if (F8) at.second = -1;                            // (no pairs: see launch)
   // A workgroup of several for a tile has a part of the tile's blocks: key0 on, everything below counts from there.
   int tile = at.tile, n_blocks = prompt_blocks<ROWS>(p, at, tile);
   const int block0 = dense_share(split, n_blocks, at.splits), key0 = block0 * kKeys;
@@ -168,51 +178,58 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
     }
     at_low = (uint32_t)bytes; at_high = (uint32_t)(bytes >> 32);
   };
-  // 8-bit: keys to the rows and pieces that the copies have.  Values lie in LDS as operands, [16 keys][half of a wave][d] of 8 keys, the dims of
-  // 64 by their number modulo 4 first: what a lane gets from memory, 4 dims of 4 rows (and of the 4 rows 8 further on), goes there in
-  // whole pieces, 16 lanes side by side.
-  auto put_f8 = [&](const uint8_t* from, uint32_t to, float scale, bool keys) {
-    typedef __attribute__((address_space(3))) v4i lds_v4i;
-    typedef __attribute__((address_space(3))) v2i lds_v2i;
-    const int i = anew(lane);
-    if (keys) {
-      const int row = i & 15, sw = D == 128 ? row : row >> 1;
+  // 8-bit: a wave's block of codes waits in registers, and goes to its stage as 16-bit numbers, a part at a time.  Keys take the rows and
+  // pieces that the copies above have.  Values lie in LDS as operands, [16 keys][half of a wave][d] of 8 keys, the dims of 64 by their
+  // number modulo 4 first: what a lane has of them, 4 dims of 4 rows (and of the 4 rows 8 further on), goes there in whole pieces, 16
+  // lanes side by side.
+  constexpr int NC = D / 64, K_PARTS = 2 * NC, V_PARTS = 4;
+  v4i k_codes[NC], v_codes[NC];
+  struct Codes { const uint8_t *k, *v; float k_scale, v_scale; uint32_t k_to, v_to; } codes;     // where the next ones are; scales and stages of those that are there
+  auto block_at = [&](int kb) { return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, kb - looked_up) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, kb - looked_up) << 32; };
+  auto scale_at = [&](int kb, bool keys) {
+    const uint32_t byte = (uint32_t)__builtin_amdgcn_readlane(scales, kb - looked_up);
+    return __uint_as_float((keys ? byte & 255 : byte >> 8) << 23);
+  };
+  // (a lane's places, which the parts' differ from by a constant)
+  const uint32_t k_place = (lane & 15) * ROW_BYTES + ((2 * (lane >> 4)) ^ (D == 128 ? lane & 15 : (lane & 15) >> 1)) * 16;
+  const uint32_t v_place = D == 128 ? ((lane >> 4 & 1) * D + (lane >> 5) * 64 + (lane & 15)) * 16 : ((lane >> 4 & 1) * D + (lane & 15)) * 16 + (lane >> 5) * 8;
+  auto ask_k = [&](const uint8_t* from, int j) { k_codes[j] = *(const v4i*)(from + j * 1024 + lane * 16); };
+  auto ask_v = [&](const uint8_t* from) {
+    const int at = D == 128 ? (lane * 16 & 0x1F0) + (lane >> 5) * 1024 : lane * 16;
 #pragma unroll
-      for (int j = 0; j < D / 64; j++) {
-        const v4i x = *(const v4i*)(from + j * 1024 + i * 16);
-#pragma unroll
-        for (int y = 0; y < 2; y++) {
-          const uint32_t c0 = (uint32_t)x[2 * y], c1 = (uint32_t)x[2 * y + 1];
-          *(lds_v4i*)(uintptr_t)(to + row * ROW_BYTES + (((2 * (j * 4 + (i >> 4)) + y) ^ sw) & (PIECES - 1)) * 16) =
-              v4i{f8_pair<T, false>(c0, scale), f8_pair<T, true>(c0, scale), f8_pair<T, false>(c1, scale), f8_pair<T, true>(c1, scale)};
-        }
-      }
-    } else if (D == 128) {
-      const int x = i & 15, h = (i >> 4) & 1, c = i >> 5;
-      const v4i a = *(const v4i*)(from + c * 1024 + h * 256 + x * 16), b = *(const v4i*)(from + c * 1024 + h * 256 + 512 + x * 16);
-#pragma unroll
-      for (int y = 0; y < 4; y++)
-        *(lds_v4i*)(uintptr_t)(to + (h * D + c * 64 + y * 16 + x) * 16) =
-            v4i{f8_pair<T, false>((uint32_t)a[y], scale), f8_pair<T, true>((uint32_t)a[y], scale), f8_pair<T, false>((uint32_t)b[y], scale), f8_pair<T, true>((uint32_t)b[y], scale)};
+    for (int j = 0; j < NC; j++) v_codes[j] = *(const v4i*)(from + at + j * 512);
+  };
+  auto put_k = [&](int part, float scale, uint32_t to) {
+    const uint32_t c0 = (uint32_t)k_codes[part >> 1][2 * (part & 1)], c1 = (uint32_t)k_codes[part >> 1][2 * (part & 1) + 1];
+    *(__attribute__((address_space(3))) v4i*)(uintptr_t)((k_place ^ ((part & 1) * 16 + (part >> 1) * 128)) + to) =
+        v4i{f8_pair<T, false>(c0, scale), f8_pair<T, true>(c0, scale), f8_pair<T, false>(c1, scale), f8_pair<T, true>(c1, scale)};
+  };
+  auto put_v = [&](int part, float scale, uint32_t to) {
+    const uint32_t c0 = (uint32_t)v_codes[0][part], c1 = (uint32_t)v_codes[NC - 1][part];
+    const v2i lo = {f8_pair<T, false>(c0, scale), f8_pair<T, true>(c0, scale)};
+    if constexpr (D == 128)
+      *(__attribute__((address_space(3))) v4i*)(uintptr_t)(v_place + to + part * 256) = v4i{lo[0], lo[1], f8_pair<T, false>(c1, scale), f8_pair<T, true>(c1, scale)};
+    else
+      *(__attribute__((address_space(3))) v2i*)(uintptr_t)(v_place + to + part * 256) = lo;
+  };
+  const uint32_t wave_at = lds0 + wave * (16 * ROW_BYTES);           // (behind it: stage, and plane of keys or values)
+  // A part of what block kb's products have beside them: block kb + 2's keys and kb + 1's values to their stages, the next ones asked for.
+  auto put_part = [&](int part) {
+    if (part < K_PARTS) {
+      put_k(part, codes.k_scale, codes.k_to);
+      if (part & 1) ask_k(codes.k, part >> 1);
     } else {
-      const int x = i & 15, rg = i >> 4;
-      const v4i a = *(const v4i*)(from + i * 16);
-#pragma unroll
-      for (int y = 0; y < 4; y++)
-        *(lds_v2i*)(uintptr_t)(to + ((rg & 1) * D + y * 16 + x) * 16 + (rg >> 1) * 8) = v2i{f8_pair<T, false>((uint32_t)a[y], scale), f8_pair<T, true>((uint32_t)a[y], scale)};
+      put_v(part - K_PARTS, codes.v_scale, codes.v_to);
+      if (part == K_PARTS + V_PARTS - 1) ask_v(codes.v);
     }
+  };
+  auto put_all = [&] {
+#pragma unroll
+    for (int i = 0; i < K_PARTS + V_PARTS; i++) put_part(i);
   };
   // (rows of a copy are a scalar's distance apart: what a lane adds is the same for every block)
   auto stage = [&](int kb, int buf, bool keys) {
     const uint32_t to = lds0 + buf * STAGE + (keys ? 0 : PLANE) + wave * (16 * ROW_BYTES);
-    if constexpr (F8) {                              // a wave's block of 16 rows, made 16-bit numbers on the way
-      const int i = kb - looked_up;
-      const uint8_t* from = (const uint8_t*)(keys ? p.pages.k : p.pages.v) +
-                            ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, i) << 32);
-      const uint32_t byte = (uint32_t)__builtin_amdgcn_readlane(scales, i);
-      put_f8(from, to, __uint_as_float((keys ? byte & 255 : byte >> 8) << 23), keys);
-      return;
-    }
     const uint32_t stride = keys ? k_stride : v_stride;
     if (!PAGED && (kb + 1) * kKeys > nk) {           // a block that ends before its last row: that one in the place of those behind it
       const uint8_t* from = (const uint8_t*)((keys ? p.k : p.v) + ((int64_t)at.kv_start + key0 + kb * kKeys) * (keys ? p.k_ld : p.v_ld) + kv * D);
@@ -350,6 +367,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
         }
 #pragma unroll
         for (int j = i * 4 * EARLY / NP; j < (i + 1) * 4 * EARLY / NP; j++) weigh(r, w, j);
+        if (F8 && MORE && i % (NP / K_PARTS) == NP / K_PARTS - 1) put_part(i / (NP / K_PARTS));
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
@@ -379,6 +397,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
             most[i & 1] = fmaxf(most[i & 1], next.s[at >> 4][at & 15]);
           }
         }
+        if (F8 && MORE && d == ND - 1) put_part(K_PARTS + x);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -463,6 +482,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
   // the last block come the first keys of the workgroup's second tile.
   int next_blocks = at.second >= 0 ? prompt_blocks<ROWS>(p, at, at.second) : 0;
   auto sync = [&](int kb) {
+    if constexpr (F8) {                              // (a block behind the last is the last once more: it goes to a stage that nobody reads)
+      lds_wait_barrier();
+      if (kb + 3 >= looked_up + 64) look_up(anew_scalar(kb + 1));
+      const int last = n_blocks - 1;
+      codes = {(const uint8_t*)p.pages.k + block_at(min(kb + 3, last)), (const uint8_t*)p.pages.v + block_at(min(kb + 2, last)), scale_at(min(kb + 2, last), true),
+               scale_at(min(kb + 1, last), false), wave_at + (kb & 1) * STAGE, wave_at + ((kb + 1) & 1) * STAGE + PLANE};
+      return;
+    }
     lds_copy_wait_barrier<0>();
     if (PAGED && kb + 2 >= looked_up + 64) look_up(anew_scalar(kb + 1));
     if (kb + 2 < n_blocks) stage(kb + 2, kb & 1, true);
@@ -477,14 +504,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
 #pragma unroll
     for (int s = 0; s < NS; s++) asm volatile("" : "+v"(q[s]));
   };
-  if (n_blocks > 0) {
-    if (PAGED) look_up(0);
-    stage(0, 0, true);
-    if (n_blocks > 1) stage(1, 1, true);
-    stage(0, 0, false);
+  if constexpr (F8) {
+    if (n_blocks > 0) {
+      look_up(0);
+      const int last = n_blocks - 1, b1 = min(1, last), b2 = min(2, last);
+      for (int j = 0; j < NC; j++) ask_k((const uint8_t*)p.pages.k + block_at(0), j);
+      ask_v((const uint8_t*)p.pages.v + block_at(0));
+      queries_there();
+      codes = {(const uint8_t*)p.pages.k + block_at(b1), (const uint8_t*)p.pages.v + block_at(b1), scale_at(0, true), scale_at(0, false), wave_at, wave_at + PLANE};
+      put_all();
+#pragma unroll
+      for (int i = 0; i < K_PARTS; i++) put_k(i, scale_at(b1, true), wave_at + STAGE);
+      for (int j = 0; j < NC; j++) ask_k((const uint8_t*)p.pages.k + block_at(b2), j);
+      lds_wait_barrier();
+    }
+  } else {
+    if (n_blocks > 0) {
+      if (PAGED) look_up(0);
+      stage(0, 0, true);
+      if (n_blocks > 1) stage(1, 1, true);
+      stage(0, 0, false);
+    }
+    queries_there();
+    if (n_blocks > 0) lds_copy_wait_barrier<0>();
   }
-  queries_there();
-  if (n_blocks > 0) lds_copy_wait_barrier<0>();
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
 #pragma unroll 1
@@ -506,6 +549,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
         refer(largest(r0), no);
       }
       sync(0);                                       // (the third block's keys go where the first one's were)
+      if (F8 && n_mine == 0 && n_blocks > 1) put_all();
       if (n_mine > 0) {
         for (; kb + 2 < n_whole; kb += 2) {
           __builtin_amdgcn_s_setprio(1);             // (the wave that multiplies goes before the one that copies or waits: 4 % at 8192 tokens)
@@ -527,7 +571,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
       }
       if (next_blocks > 0) load_q(at.second);        // (the last scores are there)
       if (n_mine > 0) step(r0, r1, (kb & 1) * STAGE, 0, 0, no, no);
-      for (; kb + 1 < n_blocks; kb++) sync(kb + 1);  // (waves whose queries see no more of the keys still copy)
+      if (F8 && n_mine > 0 && kb + 1 < n_blocks) put_all();
+      for (; kb + 1 < n_blocks; kb++) {              // (waves whose queries see no more of the keys still copy)
+        sync(kb + 1);
+        if (F8 && kb + 2 < n_blocks) put_all();
+      }
 
       // Something is no number: it may be a value that met a weight of 0.  All once more, carefully (results that should be no
       // numbers come out the same).
@@ -547,8 +595,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
         if (next_blocks > 0) { load_q(tile); queries_there(); }
         for (kb = 0; kb < n_blocks; kb++) {
           if (PAGED && kb % 64 == 0) look_up(anew_scalar(kb));
-          stage(kb, kb & 1, true);
-          stage(kb, kb & 1, false);
+          if constexpr (F8) {
+            for (int j = 0; j < NC; j++) ask_k((const uint8_t*)p.pages.k + block_at(kb), j);
+            ask_v((const uint8_t*)p.pages.v + block_at(kb));
+            codes = {(const uint8_t*)p.pages.k, (const uint8_t*)p.pages.v, scale_at(kb, true), scale_at(kb, false), wave_at + (kb & 1) * STAGE, wave_at + (kb & 1) * STAGE + PLANE};
+            put_all();
+          } else {
+            stage(kb, kb & 1, true);
+            stage(kb, kb & 1, false);
+          }
           lds_copy_wait_barrier<0>();
           if (kb < n_mine) careful(kb);
         }
@@ -632,12 +687,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 12
 
 // The parts of the tiles that several workgroups share, joined in their order: 16 rows of a tile per workgroup, 8 or 4 dims of a
 // row per thread.
-template <class T, int D, bool PAGED, int ROWS>
+template <class T, int D, DenseKeys KEYS, int ROWS>
 __global__ __launch_bounds__(256) void k_dense_prompt_join(DensePromptParams p) {
   constexpr int N = D / 16;
   const int lane = threadIdx.x & 63, kv = blockIdx.x % p.Hkv, idx = blockIdx.x / p.Hkv;
   PromptPlace at;
-  if (!prompt_place<PAGED, ROWS>(p, idx, lane, at) || at.splits == 1) return;
+  if (!prompt_place<KEYS, ROWS>(p, idx, lane, at) || at.splits == 1) return;
   const int r = blockIdx.y * 16 + threadIdx.x / 16, x = threadIdx.x % 16 * N, row = at.tile * ROWS + r;
   if (row >= at.nq * p.G) return;
   float M = -INFINITY, L = 0.f, O[N];
@@ -683,15 +738,15 @@ hipError_t launch(DensePromptParams& p, hipStream_t s) {
   constexpr bool PAGED = KEYS != DenseKeys::packed;
   constexpr int NW = 4, ROWS = 32 * NW;
   static_assert(ROWS == kDensePromptRows, "");
-  const DensePromptGrid grid = dense_prompt_grid(p.n_q, p.B, p.Hkv, p.G, p.causal != 0);
+  const DensePromptGrid grid = dense_prompt_grid(p.n_q, p.B, p.Hkv, p.G, p.causal != 0 && KEYS != DenseKeys::paged_f8);
   const int64_t wgs = grid.workgroups;
   p.pairs = grid.pairs;
-  // no sequence has more keys than there are, and no workgroup of several fewer than kLeastBlocks blocks of them
+  // no sequence has more keys than there are, and no workgroup of several fewer than the least number of blocks of them
   const int64_t keys = PAGED ? (int64_t)p.pages.max_pages * p.pages.page_rows : p.n_kv;
-  const int64_t most = std::min<int64_t>({32, kDensePromptParts / wgs, (keys + kKeys - 1) / kKeys / kLeastBlocks});
+  const int64_t most = std::min<int64_t>({32, kDensePromptParts / wgs, prompt_shares<KEYS == DenseKeys::paged_f8>((int)((keys + kKeys - 1) / kKeys))});
   p.splits = p.pairs ? 1 : (int)std::max<int64_t>(most, 1);
   k_dense_prompt<T, D, KEYS, NW><<<dim3((unsigned)(wgs * p.splits)), 64 * NW, 0, s>>>(p);
-  if (p.splits > 1) k_dense_prompt_join<T, D, PAGED, ROWS><<<dim3((unsigned)wgs, ROWS / 16), 256, 0, s>>>(p);
+  if (p.splits > 1) k_dense_prompt_join<T, D, KEYS, ROWS><<<dim3((unsigned)wgs, ROWS / 16), 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
