@@ -124,8 +124,9 @@ static wsvd_status decode(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads;
   p.max_len = max_seq_len; p.waves = dense_waves(p.B, p.Hkv, max_seq_len);
   p.target = dense_target(p.waves, p.Hkv);
-  // (in rows twice as many at half the row length; the min_chunk setting, where given, is taken for both)
-  p.alone_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : 5 * 128 / desc->d_head;
+  // (in rows twice as many at half the row length; the min_chunk setting, where given, is taken for both.  8-bit rows: one sequence of heads of 128,
+  // 32 / 32, 32 / 8 and 28 / 4 of them, 768 rows whole 7.1, 7.3 and 7.7 us, cut 7.8, 8.0, 8.8; 1024 whole 8.1, 8.3, 8.6, cut 7.9, 8.0, 9.1.)
+  p.alone_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : (f8 ? 7 : 5) * 128 / desc->d_head;
   p.min_units = ctx->opt.min_chunk ? p.alone_units : 2 * 128 / desc->d_head;
   p.alone = dense_units_of(max_seq_len) <= p.alone_units;
   if (!dense_launchable(dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0), 64 * p.waves)) return WSVD_E_SHAPE;

@@ -230,15 +230,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k
 
 // ---------------------------------------------------------------- decode attention
 // k_dense_decode's mathematics (wsvd_dense.hip) over codes: 16x16x32 products with the heads as the 16 columns, a lane owns one head and 4
-// of 16 rows.  Both operands are made from the codes as they lie, a conversion of two with their block's scale each.
+// of 16 rows.  Both operands are made from the codes as they lie, a conversion of two with their block's scale each (at full rate).
+// Bound: HBM.  32 x 8192 rows of 4 heads of 128 (270 MB): 47.4 us, 5.7 TB/s; the same launches and requests without the arithmetic 46.2, a kernel
+// that only reads so many bytes 41.1.  640 rows of 32 heads (5.3 MB): 6.5 us, without arithmetic 4.7, of which 3.3 are a launch that finds no row.
+// (Tiles of 64 rows, so that twice as much is asked for ahead: 48.1 us and 6.9; workgroups of 4 waves, two to a CU: 51.2 and 7.0; one chunk a
+// sequence, on half of the CUs: 52.8.)
+constexpr int kF8Tile = 2;
 template <int D>
 struct F8Tile {
-  v4i k[2][D / 64], v[2][D / 64];                    // two blocks
+  v4i k[kF8Tile][D / 64], v[kF8Tile][D / 64];        // two blocks
 };
 
 template <class T, int D, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode_f8(DenseDecodeParams p) {
-  constexpr int ND = D / 64, NK = D / 32, NJ = D / 16;
+  constexpr int ND = D / 64, NK = D / 32, NJ = D / 16, NB = kF8Tile, ROWS = 16 * NB, AHEAD = 64 / NB;        // rows of a tile; tiles looked up at a time
   extern __shared__ __attribute__((aligned(256))) float o_sh[];      // [NW][G][D]
   __shared__ float m_sh[NW][16], l_sh[NW][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -249,7 +254,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   if (at.chunk == 0 && kv == 0 && threadIdx.x == 0 && p.pages.seq_lens[at.b] > p.max_len) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   const int G = p.G;
   const int first = at.chunk * at.rows, end = min(at.len, first + at.rows);
-  const int n_tiles = (max(end - first, 0) + 31) >> 5;
+  const int n_tiles = (max(end - first, 0) + ROWS - 1) / ROWS;
 
   // queries as the second operand: column c = head of the group, dims in the order in which a lane has a key's
   v4i q[NK];
@@ -262,23 +267,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int i = 0; i < 4; i++) q[j][i] = c < G ? x[i] : 0;
     }
   }
-  // Where the wave's next 32 tiles lie, a lane for each of a tile's blocks.
+  // Where the wave's next AHEAD tiles lie, a lane for each of a tile's blocks.
   const int* table = p.pages.block_table + (size_t)at.b * p.pages.max_pages;
   const int last_granule = (at.len - 1) >> 4;
   bool bad = false;
   uint32_t at_low = 0, at_high = 0, k_scale = 0, v_scale = 0;
   auto look_up = [&](int t) {
-    const int granule = min((first >> 4) + 2 * (t + NW * (lane >> 1)) + (lane & 1), last_granule);
+    const int granule = min((first >> 4) + NB * (t + NW * (lane / NB)) + lane % NB, last_granule);
     const int pg = dense_page_index(granule, p.pages.page_magic);
     const int page = dense_page(table[pg], p.pages.n_pages, bad);
     const uint64_t block = f8_block(page, granule, pg, kv, p.Hkv, p.pages.page_rows), at = block * (kF8Rows * D);
     at_low = (uint32_t)at; at_high = (uint32_t)(at >> 32);
     k_scale = (uint32_t)p.scales.k[block] << 23; v_scale = (uint32_t)p.scales.v[block] << 23;
   };
-  auto load = [&](F8Tile<D>& tile, int i) {          // i: the tile's number among those looked up
+  auto load = [&](F8Tile<D>& tile, int i) {      // i: the tile's number among those looked up
 #pragma unroll
-    for (int g = 0; g < 2; g++) {
-      const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, 2 * i + g) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, 2 * i + g) << 32;
+    for (int g = 0; g < NB; g++) {
+      const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_low, NB * i + g) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_high, NB * i + g) << 32;
       const uint8_t *kp = (const uint8_t*)p.pages.k + base, *vp = (const uint8_t*)p.pages.v + base;
 #pragma unroll
       for (int j = 0; j < ND; j++) tile.k[g][j] = load_row<ONCE>((const v4i*)(kp + j * 1024 + lane * 16));
@@ -293,11 +298,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
   auto attend = [&](F8Tile<D>& tile, int t, int i) {
 #pragma clang fp contract(off)                       // (a score is the same number against the limit and in its weight)
-    const int r0 = first + t * 32;
-    float s[8];
+    const int r0 = first + t * ROWS;
+    float s[4 * NB];
 #pragma unroll
-    for (int g = 0; g < 2; g++) {
-      const float scale = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(k_scale, 2 * i + g));
+    for (int g = 0; g < NB; g++) {
+      const float scale = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(k_scale, NB * i + g));
       v4f x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < NK; j++) {
@@ -307,22 +312,21 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
       for (int y = 0; y < 4; y++) s[4 * g + y] = x[y] * p.c_scale;
     }
-    if (r0 + 32 > end) {                             // rows behind the sequence's end: no weight, and no value that could be NaN
+    if (r0 + ROWS > end) {                           // rows behind the sequence's end: no weight, and no value that could be NaN
 #pragma unroll
-      for (int g = 0; g < 2; g++) {
-        const int n = min(max(end - (r0 + 16 * g + 4 * qd), 0), 4);
-        const uint32_t seen = n == 4 ? ~0u : (1u << (8 * n)) - 1u;
+      for (int g = 0; g < NB; g++) {
+        const int n = end - (r0 + 16 * g + 4 * qd);
 #pragma unroll
         for (int y = 0; y < 4; y++) s[4 * g + y] = y < n ? s[4 * g + y] : -INFINITY;
 #pragma unroll
         for (int j = 0; j < ND; j++)
 #pragma unroll
-          for (int y = 0; y < 4; y++) tile.v[g][j][y] &= (int)seen;
+          for (int y = 0; y < 4; y++) tile.v[g][j][y] &= (int)f8_bytes(n);
       }
     }
     float most = s[0];
 #pragma unroll
-    for (int y = 1; y < 8; y++) most = fmaxf(most, s[y]);
+    for (int y = 1; y < 4 * NB; y++) most = fmaxf(most, s[y]);
     if (__ballot(most - m > T::kTop)) {              // (see the element types)
       const float top = quarters_max(most), low = top - T::kRaise;
       const float mn = fmaxf(m, top - low > T::kTop ? top : low);    // (steps of 16, between scores of 2^27 and 2^28)
@@ -346,7 +350,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       hi[y] = (int)h;
       lo[y] = (int)dense_pack<T>(w[2 * y] - dense_low<T>(h), w[2 * y + 1] - dense_high<T>(h));
     }
-    const float s0 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_scale, 2 * i)), s1 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_scale, 2 * i + 1));
+    const float s0 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_scale, NB * i)), s1 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_scale, NB * i + 1));
 #pragma unroll
     for (int j = 0; j < NJ; j++) {
       const uint32_t c0 = (uint32_t)tile.v[0][j >> 2][j & 3], c1 = (uint32_t)tile.v[1][j >> 2][j & 3];
@@ -355,9 +359,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       o[j] = T::mfma16(a, lo, o[j]);
     }
   };
-  for (int t = wave; t < n_tiles; t += 32 * NW) {    // 32 tiles of the wave
+  for (int t = wave; t < n_tiles; t += AHEAD * NW) {
     look_up(t);
-    const int n = min(32, (n_tiles - t + NW - 1) / NW);
+    const int n = min(AHEAD, (n_tiles - t + NW - 1) / NW);
     F8Tile<D> t0, t1;
     load(t0, 0);
     int i = 0;
