@@ -1,4 +1,5 @@
 // Dense layers over 8-bit pages: rotary embedding with the append that quantises, and the attention of one new token per sequence.
+#include <type_traits>
 #include "wsvd_dense_f8.h"
 #include "wsvd_dense_join.h"
 
@@ -6,41 +7,59 @@ namespace {
 
 // ---------------------------------------------------------------- append
 // Rotation of the new tokens' queries and keys, keys and values quantised into the blocks of their sequences.  A unit is the new rows of one
-// block (1 to 16 of them): who has a unit has all that the block's scales depend on, so that no two workgroups write to one block and
-// nothing is handed over.  A workgroup has the units that begin with its TOK tokens.
+// block (1 to 16 of them): who has a head of a unit has all that the block's scale depends on, so that no two waves write to one block and
+// nothing is handed over.  A workgroup has one unit, or a share of its heads.
 //   The new rows' largest magnitude gives the scale that they need; a block that held rows keeps the larger of its scale and that one, and
 // where its own was the smaller one its codes move (rarely: their exponents shift).  A key is quantised as the 16-bit number that k_out has.
-//   Bound: memory, every element read once, 16-bit ones and codes written once.  18900 tokens of 32 heads of 128 (936 MB): 181 us, 5.2 TB/s, where a
+//   Bound: memory, every element read once, 16-bit ones and codes written once.  18900 tokens of 32 heads of 128 (936 MB): 171 us, 5.5 TB/s, where a
 // copy of 1 GiB reaches 5.1.  Loads and stores go in whole lines (a lane with 16 dims of a row, two requests that share lines: 271 us, with 8 dims of
 // two rows 244); rows as data that is used once (208 of 219 us with two workgroups a unit); the workgroups of a unit side by side (205 -> 197 with
-// three); four waves a SIMD (three, with the next head asked for ahead: 196).  32 tokens of 28 / 4 heads: 5.8 us on the GPU, six dependent steps:
-// lengths, page, scale and rows, the wave's maximum, the store.
+// three); four waves a SIMD (three, with the next head asked for ahead: 196); units found from the lengths (by workgroups of 16 tokens each: 181; of
+// one, most of which have none: 4 x 300 tokens of 32 / 8 heads 25.9 us, now 11.7).  32 tokens of 28 / 4 heads: 6.4 us on the GPU, five dependent
+// steps: lengths, page, scale and rows, the wave's maximum, the store.
 struct F8Unit { int t, n, row; int64_t block; };     // first token, tokens, the first one's row; block in the pools, -1: nothing is stored
-// The unit that begins with token t, n = 0 where none does.  A wave's work: sequence, borders and length in one look at them.
-WSVD_DEV F8Unit f8_unit(const DenseAppendParams& p, int t, int lane) {
-  F8Unit u = {t, 0, 0, -1};
-  if (t >= p.n_tokens) return u;
-  int b = t, from = t, to = t + 1, len = 0;
+// The call's unit number idx, in the tokens' order; n = 0 where there is none.  A wave's work: 256 sequences' borders and lengths are asked for at
+// once, a lane for each of 64.
+WSVD_DEV F8Unit f8_unit(const DenseAppendParams& p, int idx, int lane) {
+  F8Unit u = {idx, 0, 0, -1};
+  int b = idx;
   if (p.cu) {
-    int found = -1;
-    for (int base = 0; base < p.B && found < 0; base += 64) {
-      const int i = min(base + lane, p.B - 1);
-      const int c0 = p.cu[i], c1 = p.cu[i + 1], l = p.pages.seq_lens[i];
-      const unsigned long long m = __ballot(base + lane < p.B && c1 > t);
-      if (m) {
-        const int at = __builtin_ctzll(m);
-        found = base + at;
-        from = __builtin_amdgcn_readlane(c0, at); to = __builtin_amdgcn_readlane(c1, at); len = __builtin_amdgcn_readlane(l, at);
+    b = -1;
+    int before = 0;
+    auto look = [&](int base, auto groups) {
+      constexpr int N = decltype(groups)::value;
+      int from[N], row[N], n[N], units[N];
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int s = min(base + 64 * i + lane, p.B - 1), to = p.cu[s + 1];
+        from[i] = p.cu[s];
+        row[i] = p.pages.seq_lens[s] - (to - from[i]);
+        // (tokens that are not there, and borders that are none: no unit)
+        n[i] = base + 64 * i + lane < p.B && from[i] >= 0 ? min(to, p.n_tokens) - from[i] : 0;
+        units[i] = n[i] > 0 ? ((row[i] + n[i] - 1) >> 4) - (row[i] >> 4) + 1 : 0;
       }
-    }
-    if (found < 0 || t < from) return u;
-    b = found;
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int end = before + wave_prefix_int(units[i]);
+        const unsigned long long m = __ballot(end > idx);
+        if (m && b < 0) {
+          const int at = __builtin_ctzll(m), f = __builtin_amdgcn_readlane(from[i], at), r = __builtin_amdgcn_readlane(row[i], at), k = __builtin_amdgcn_readlane(n[i], at);
+          const int nth = idx - (__builtin_amdgcn_readlane(end, at) - __builtin_amdgcn_readlane(units[i], at));
+          b = base + 64 * i + at;
+          u.row = nth == 0 ? r : ((r >> 4) + nth) * kF8Rows;
+          u.t = f + (u.row - r);
+          u.n = min(kF8Rows - (u.row & (kF8Rows - 1)), k - (u.row - r));
+        }
+        before = __builtin_amdgcn_readlane(end, 63);
+      }
+    };
+    if (p.B <= 64) look(0, std::integral_constant<int, 1>{});
+    else for (int base = 0; base < p.B && b < 0; base += 256) look(base, std::integral_constant<int, 4>{});
+    if (b < 0) return u;
   } else {
-    len = p.pages.seq_lens[b];
+    u.row = p.pages.seq_lens[b] - 1;
+    u.n = 1;
   }
-  u.row = len - (to - t);
-  if (u.row >= 0 && t != from && u.row % kF8Rows != 0) return u;
-  u.n = u.row < 0 ? 1 : min(kF8Rows - u.row % kF8Rows, min(to, p.n_tokens) - t);
   if (u.row < 0 || u.row >= (int64_t)p.pages.max_pages * p.pages.page_rows) {
     if (lane == 0) atomicExch(p.err_word, (int)(u.row < 0 ? WSVD_E_SHAPE : WSVD_E_CAPACITY));
     return u;
@@ -55,176 +74,164 @@ WSVD_DEV F8Unit f8_unit(const DenseAppendParams& p, int t, int lane) {
   return u;
 }
 
-template <class T, int D, int TOK, bool ONCE>
+template <class T, int D, bool ONCE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k_dense_append_f8(DenseAppendParams p, int splits) {
   constexpr int HALF = D / 2, ND = D / 64, PER_ROUND = 1024 / D, ROUNDS = kF8Rows / PER_ROUND;     // rows at a time: in whole lines
   constexpr int N = D / 16;
-  __shared__ F8Unit unit_sh[TOK];
   __shared__ float cs[kF8Rows][2][HALF];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int split = (int)(blockIdx.x % (unsigned)splits), step = splits * 4, heads = p.Hq + 2 * p.Hkv;
   const double freq = p.inv_freq ? p.inv_freq[tid % HALF] : 0.;      // (asked for before anything is known of the tokens)
-  const int t0 = (int)(blockIdx.x / (unsigned)splits * TOK);
-  if (TOK > 1) {
-    for (int i = wave; i < TOK; i += 4) {
-      const F8Unit u = f8_unit(p, t0 + i, lane);
-      if (lane == 0) unit_sh[i] = u;
-    }
-    __syncthreads();
-  }
   const int blocks = p.pages.page_rows / kF8Rows;    // of a kv head in a page
   const int r = lane / (D / 16), x8 = lane % (D / 16) * 8;            // of queries and keys: row of a round, dims of either half
   const int qd = lane >> 4, x4 = lane % 16 * 4;      // of values: group of rows, dims of every 64
-  for (int i = 0; i < TOK; i++) {
-    const F8Unit u = TOK > 1 ? unit_sh[i] : f8_unit(p, t0, lane);
-    if (u.n <= 0) continue;
-    const int r0 = u.row & (kF8Rows - 1), new_end = r0 + u.n;        // the block's rows that are new: r0 .. new_end - 1
-    const bool stored = u.block >= 0;
-    // what a lane has of a head: of queries and keys [round][half of the dims] of 8, of values [row of 4][64 dims] of 4
-    auto fetch = [&](int h, v2i (&w)[N]) {
-      if (h < p.Hq + p.Hkv) {
-        const bool key = h >= p.Hq;
-        if (!key && !p.q_out) return;
-        const uint16_t* const src = (key ? p.k + (h - p.Hq) * D : p.q + h * D) + x8;
-        const int64_t ld = key ? p.k_ld : p.q_ld;
+  const F8Unit u = f8_unit(p, (int)(blockIdx.x / (unsigned)splits), lane);
+  if (u.n <= 0) return;
+  const int r0 = u.row & (kF8Rows - 1), new_end = r0 + u.n;          // the block's rows that are new: r0 .. new_end - 1
+  const bool stored = u.block >= 0;
+  // what a lane has of a head: of queries and keys [round][half of the dims] of 8, of values [row of 4][64 dims] of 4
+  auto fetch = [&](int h, v2i (&w)[N]) {
+    if (h < p.Hq + p.Hkv) {
+      const bool key = h >= p.Hq;
+      if (!key && !p.q_out) return;
+      const uint16_t* const src = (key ? p.k + (h - p.Hq) * D : p.q + h * D) + x8;
+      const int64_t ld = key ? p.k_ld : p.q_ld;
 #pragma unroll
-        for (int y = 0; y < ROUNDS; y++)
+      for (int y = 0; y < ROUNDS; y++)
 #pragma unroll
-          for (int z = 0; z < 2; z++) {
-            const int t = y * PER_ROUND + r;
-            v4i x = {0, 0, 0, 0};
-            if (t < u.n) x = load_row<ONCE>((const v4i*)(src + (int64_t)(u.t + t) * ld + z * HALF));
-            w[4 * y + 2 * z] = v2i{x[0], x[1]};
-            w[4 * y + 2 * z + 1] = v2i{x[2], x[3]};
-          }
-      } else {
-        const uint16_t* const src = p.v + (h - p.Hq - p.Hkv) * D + x4;
+        for (int z = 0; z < 2; z++) {
+          const int t = y * PER_ROUND + r;
+          v4i x = {0, 0, 0, 0};
+          if (t < u.n) x = load_row<ONCE>((const v4i*)(src + (int64_t)(u.t + t) * ld + z * HALF));
+          w[4 * y + 2 * z] = v2i{x[0], x[1]};
+          w[4 * y + 2 * z + 1] = v2i{x[2], x[3]};
+        }
+    } else {
+      const uint16_t* const src = p.v + (h - p.Hq - p.Hkv) * D + x4;
 #pragma unroll
-        for (int j = 0; j < 4; j++)
+      for (int j = 0; j < 4; j++)
 #pragma unroll
-          for (int c = 0; c < ND; c++) {
-            const int row = 4 * qd + j;
-            w[j * ND + c] = v2i{0, 0};
-            if (row >= r0 && row < new_end) w[j * ND + c] = load_row<ONCE>((const v2i*)(src + (int64_t)(u.t + row - r0) * p.v_ld + c * 64));
-          }
-      }
-    };
-    int h = split * 4 + wave;
-    v2i w[N];
-    if (h < heads) fetch(h, w);                      // (under the angles)
-    if (p.inv_freq) {
-      for (int e = tid; e < u.n * HALF; e += 256) {  // (whole turns in 64 bits, the sine and cosine of what is left in 32)
-        const int j = e / HALF, x = e % HALF, pos = p.positions ? p.positions[u.t + j] : u.row + j;
-        const double turns = (double)pos * freq * 0.15915494309189533576888376337251;   // / 2 pi
-        const float f = (float)(turns - __builtin_rint(turns));
-        sincospif(2.f * f, &cs[j][1][x], &cs[j][0][x]);
-      }
-      __syncthreads();
+        for (int c = 0; c < ND; c++) {
+          const int row = 4 * qd + j;
+          w[j * ND + c] = v2i{0, 0};
+          if (row >= r0 && row < new_end) w[j * ND + c] = load_row<ONCE>((const v2i*)(src + (int64_t)(u.t + row - r0) * p.v_ld + c * 64));
+        }
     }
-    for (; h < heads; h += step) {
-      const bool value = h >= p.Hq + p.Hkv, key = !value && h >= p.Hq;
-      const int hh = value ? h - p.Hq - p.Hkv : key ? h - p.Hq : h;
-      const int64_t block = u.block + (int64_t)hh * blocks;
-      uint8_t* const codes = (uint8_t*)(value ? p.pages.v : p.pages.k) + block * (kF8Rows * D);
-      uint8_t* const scale = (value ? p.scales.v : p.scales.k) + block;
-      const int old = (key || value) && stored && r0 > 0 ? (int)*scale - kF8Bias : kF8Least;
-      // bytes of a value dword whose rows are new, or were there
-      const uint32_t fresh = f8_bytes(new_end - 4 * qd) & ~f8_bytes(r0 - 4 * qd), before = f8_bytes(r0 - 4 * qd);
-      v4i was[ND];
-      if (value && stored && fresh != ~0u) {         // (rows that are not the call's stay as they are)
+  };
+  int h = split * 4 + wave;
+  v2i w[N];
+  if (h < heads) fetch(h, w);                      // (under the angles)
+  if (p.inv_freq) {
+    for (int e = tid; e < u.n * HALF; e += 256) {  // (whole turns in 64 bits, the sine and cosine of what is left in 32)
+      const int j = e / HALF, x = e % HALF, pos = p.positions ? p.positions[u.t + j] : u.row + j;
+      const double turns = (double)pos * freq * 0.15915494309189533576888376337251;   // / 2 pi
+      const float f = (float)(turns - __builtin_rint(turns));
+      sincospif(2.f * f, &cs[j][1][x], &cs[j][0][x]);
+    }
+    __syncthreads();
+  }
+  for (; h < heads; h += step) {
+    const bool value = h >= p.Hq + p.Hkv, key = !value && h >= p.Hq;
+    const int hh = value ? h - p.Hq - p.Hkv : key ? h - p.Hq : h;
+    const int64_t block = u.block + (int64_t)hh * blocks;
+    uint8_t* const codes = (uint8_t*)(value ? p.pages.v : p.pages.k) + block * (kF8Rows * D);
+    uint8_t* const scale = (value ? p.scales.v : p.scales.k) + block;
+    const int old = (key || value) && stored && r0 > 0 ? (int)*scale - kF8Bias : kF8Least;
+    // bytes of a value dword whose rows are new, or were there
+    const uint32_t fresh = f8_bytes(new_end - 4 * qd) & ~f8_bytes(r0 - 4 * qd), before = f8_bytes(r0 - 4 * qd);
+    v4i was[ND];
+    if (value && stored && fresh != ~0u) {         // (rows that are not the call's stay as they are)
 #pragma unroll
-        for (int c = 0; c < ND; c++) was[c] = *(const v4i*)(codes + c * 1024 + qd * 256 + x4 * 4);
+      for (int c = 0; c < ND; c++) was[c] = *(const v4i*)(codes + c * 1024 + qd * 256 + x4 * 4);
+    }
+    float most = 0.f;
+    if (!value) {
+      uint16_t* const out = key ? p.k_out : p.q_out;
+#pragma unroll
+      for (int y = 0; y < ROUNDS; y++) {
+        const int t = y * PER_ROUND + r;
+        if (t < u.n && (key || out)) {
+          if (p.inv_freq) {
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+              const int c = x8 + 2 * x;
+              const float c0 = cs[t][0][c], c1 = cs[t][0][c + 1], s0 = cs[t][1][c], s1 = cs[t][1][c + 1];
+              const uint32_t a = (uint32_t)w[4 * y + (x >> 1)][x & 1], b = (uint32_t)w[4 * y + 2 + (x >> 1)][x & 1];
+              const float a0 = dense_low<T>(a), a1 = dense_high<T>(a), b0 = dense_low<T>(b), b1 = dense_high<T>(b);
+              w[4 * y + (x >> 1)][x & 1] = (int)dense_pack<T>(a0 * c0 - b0 * s0, a1 * c1 - b1 * s1);
+              w[4 * y + 2 + (x >> 1)][x & 1] = (int)dense_pack<T>(b0 * c0 + a0 * s0, b1 * c1 + a1 * s1);
+            }
+          }
+          if (out) {
+            uint16_t* const to = out + (int64_t)(u.t + t) * (key ? p.k_out_ld : p.q_out_ld) + hh * D + x8;
+#pragma unroll
+            for (int z = 0; z < 2; z++)
+              store_row<ONCE>((v4i*)(to + z * HALF), v4i{w[4 * y + 2 * z][0], w[4 * y + 2 * z][1], w[4 * y + 2 * z + 1][0], w[4 * y + 2 * z + 1][1]});
+          }
+        }
       }
-      float most = 0.f;
-      if (!value) {
-        uint16_t* const out = key ? p.k_out : p.q_out;
+    }
+    if ((key || value) && stored) {
+#pragma unroll
+      for (int x = 0; x < 2 * N; x++) most = f8_most<T>(most, (uint32_t)w[x >> 1][x & 1]);       // (what a lane has none of is 0)
+      const int e = max(f8_exponent(wave_max(most)), old);
+      const bool moves = r0 > 0 && e > old;
+      const float inverse = f8_power(-e), top = f8_top<T>(e), by = f8_power(max(old - e, -40));
+      if (key) {
+        auto at = [&](int z, int row) {            // 16 dims of a row lie together
+          const int dim = z * HALF + x8;
+          return (v2i*)(codes + ((dim >> 4) * kF8Rows + row) * 16 + (dim & 8));
+        };
 #pragma unroll
         for (int y = 0; y < ROUNDS; y++) {
           const int t = y * PER_ROUND + r;
-          if (t < u.n && (key || out)) {
-            if (p.inv_freq) {
+          if (t < u.n) {
 #pragma unroll
-              for (int x = 0; x < 4; x++) {
-                const int c = x8 + 2 * x;
-                const float c0 = cs[t][0][c], c1 = cs[t][0][c + 1], s0 = cs[t][1][c], s1 = cs[t][1][c + 1];
-                const uint32_t a = (uint32_t)w[4 * y + (x >> 1)][x & 1], b = (uint32_t)w[4 * y + 2 + (x >> 1)][x & 1];
-                const float a0 = dense_low<T>(a), a1 = dense_high<T>(a), b0 = dense_low<T>(b), b1 = dense_high<T>(b);
-                w[4 * y + (x >> 1)][x & 1] = (int)dense_pack<T>(a0 * c0 - b0 * s0, a1 * c1 - b1 * s1);
-                w[4 * y + 2 + (x >> 1)][x & 1] = (int)dense_pack<T>(b0 * c0 + a0 * s0, b1 * c1 + a1 * s1);
+            for (int z = 0; z < 2; z++) {
+              v2i c;
+#pragma unroll
+              for (int x = 0; x < 2; x++) {
+                const uint32_t a = (uint32_t)w[4 * y + 2 * z + x][0], b = (uint32_t)w[4 * y + 2 * z + x][1];
+                c[x] = (int)f8_codes(f8_scaled(dense_low<T>(a), inverse, top), f8_scaled(dense_high<T>(a), inverse, top),
+                                     f8_scaled(dense_low<T>(b), inverse, top), f8_scaled(dense_high<T>(b), inverse, top));
               }
+              store_row<ONCE>(at(z, r0 + t), c);
             }
-            if (out) {
-              uint16_t* const to = out + (int64_t)(u.t + t) * (key ? p.k_out_ld : p.q_out_ld) + hh * D + x8;
+          }
+          if (moves && t < r0) {                   // row t, which the block held before
 #pragma unroll
-              for (int z = 0; z < 2; z++)
-                store_row<ONCE>((v4i*)(to + z * HALF), v4i{w[4 * y + 2 * z][0], w[4 * y + 2 * z][1], w[4 * y + 2 * z + 1][0], w[4 * y + 2 * z + 1][1]});
+            for (int z = 0; z < 2; z++) {
+              v2i c = *at(z, t);
+              c[0] = (int)f8_moved((uint32_t)c[0], by); c[1] = (int)f8_moved((uint32_t)c[1], by);
+              *at(z, t) = c;
             }
           }
         }
-      }
-      if ((key || value) && stored) {
+      } else if (fresh || (moves && before)) {
 #pragma unroll
-        for (int x = 0; x < 2 * N; x++) most = f8_most<T>(most, (uint32_t)w[x >> 1][x & 1]);       // (what a lane has none of is 0)
-        const int e = max(f8_exponent(wave_max(most)), old);
-        const bool moves = r0 > 0 && e > old;
-        const float inverse = f8_power(-e), top = f8_top<T>(e), by = f8_power(max(old - e, -40));
-        if (key) {
-          auto at = [&](int z, int row) {            // 16 dims of a row lie together
-            const int dim = z * HALF + x8;
-            return (v2i*)(codes + ((dim >> 4) * kF8Rows + row) * 16 + (dim & 8));
-          };
+        for (int c = 0; c < ND; c++) {
+          v4i to;
 #pragma unroll
-          for (int y = 0; y < ROUNDS; y++) {
-            const int t = y * PER_ROUND + r;
-            if (t < u.n) {
+          for (int x = 0; x < 4; x++) {
+            float y[4];
 #pragma unroll
-              for (int z = 0; z < 2; z++) {
-                v2i c;
-#pragma unroll
-                for (int x = 0; x < 2; x++) {
-                  const uint32_t a = (uint32_t)w[4 * y + 2 * z + x][0], b = (uint32_t)w[4 * y + 2 * z + x][1];
-                  c[x] = (int)f8_codes(f8_scaled(dense_low<T>(a), inverse, top), f8_scaled(dense_high<T>(a), inverse, top),
-                                       f8_scaled(dense_low<T>(b), inverse, top), f8_scaled(dense_high<T>(b), inverse, top));
-                }
-                store_row<ONCE>(at(z, r0 + t), c);
-              }
+            for (int j = 0; j < 4; j++) {
+              const uint32_t z = (uint32_t)w[j * ND + c][x >> 1];
+              y[j] = f8_scaled(x & 1 ? dense_high<T>(z) : dense_low<T>(z), inverse, top);
             }
-            if (moves && t < r0) {                   // row t, which the block held before
-#pragma unroll
-              for (int z = 0; z < 2; z++) {
-                v2i c = *at(z, t);
-                c[0] = (int)f8_moved((uint32_t)c[0], by); c[1] = (int)f8_moved((uint32_t)c[1], by);
-                *at(z, t) = c;
-              }
+            to[x] = (int)f8_codes(y[0], y[1], y[2], y[3]);
+            if (fresh != ~0u) {
+              uint32_t kept = (uint32_t)was[c][x];
+              if (moves) kept = (f8_moved(kept, by) & before) | (kept & ~before);
+              to[x] = (int)(((uint32_t)to[x] & fresh) | (kept & ~fresh));
             }
           }
-        } else if (fresh || (moves && before)) {
-#pragma unroll
-          for (int c = 0; c < ND; c++) {
-            v4i to;
-#pragma unroll
-            for (int x = 0; x < 4; x++) {
-              float y[4];
-#pragma unroll
-              for (int j = 0; j < 4; j++) {
-                const uint32_t z = (uint32_t)w[j * ND + c][x >> 1];
-                y[j] = f8_scaled(x & 1 ? dense_high<T>(z) : dense_low<T>(z), inverse, top);
-              }
-              to[x] = (int)f8_codes(y[0], y[1], y[2], y[3]);
-              if (fresh != ~0u) {
-                uint32_t kept = (uint32_t)was[c][x];
-                if (moves) kept = (f8_moved(kept, by) & before) | (kept & ~before);
-                to[x] = (int)(((uint32_t)to[x] & fresh) | (kept & ~fresh));
-              }
-            }
-            store_row<ONCE>((v4i*)(codes + c * 1024 + qd * 256 + x4 * 4), to);
-          }
+          store_row<ONCE>((v4i*)(codes + c * 1024 + qd * 256 + x4 * 4), to);
         }
-        if (lane == 0) *scale = (uint8_t)(e + kF8Bias);
       }
-      if (h + step < heads) fetch(h + step, w);
+      if (lane == 0) *scale = (uint8_t)(e + kF8Bias);
     }
-    if (TOK > 1) __syncthreads();                    // (the next unit's angles go where this one's are)
+    if (h + step < heads) fetch(h + step, w);
   }
 }
 
@@ -391,18 +398,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh);
 }
 
-template <class T, int D, int TOK>
-hipError_t launch_append_form(const DenseAppendParams& p, int splits, hipStream_t s) {
-  const unsigned grid = (unsigned)((p.n_tokens + TOK - 1) / TOK * splits);
-  const bool once = (int64_t)p.n_tokens * (2 * p.Hq + 4 * p.Hkv) * D * 2 >= 100000000;
-  if (once) k_dense_append_f8<T, D, TOK, true><<<grid, 256, 0, s>>>(p, splits);
-  else k_dense_append_f8<T, D, TOK, false><<<grid, 256, 0, s>>>(p, splits);
-  return hipGetLastError();
-}
 template <class T, int D>
 hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
   const DenseF8Append a = dense_f8_append(p.n_tokens, p.B, p.Hq + 2 * p.Hkv, p.cu != nullptr);
-  return a.tokens == 1 ? launch_append_form<T, D, 1>(p, a.splits, s) : launch_append_form<T, D, 16>(p, a.splits, s);
+  const bool once = (int64_t)p.n_tokens * (2 * p.Hq + 4 * p.Hkv) * D * 2 >= 100000000;
+  const unsigned grid = (unsigned)(a.units * a.splits);
+  if (once) k_dense_append_f8<T, D, true><<<grid, 256, 0, s>>>(p, a.splits);
+  else k_dense_append_f8<T, D, false><<<grid, 256, 0, s>>>(p, a.splits);
+  return hipGetLastError();
 }
 template <class T, int D, int NW, bool ONCE>
 hipError_t launch_decode_form(const DenseDecodeParams& p, hipStream_t s) {

@@ -87,14 +87,16 @@ WSVD_HD int dense_append_tokens(int64_t n_tokens, int items) {
   if (n_tokens < 2048 || (items >= 256 && dense_launchable(n_tokens, 256))) return 1;
   return items >= 128 ? 2 : 4;
 }
-// The append over 8-bit pages: tokens of a workgroup, whose units (the new rows of a block of 16) it has, and workgroups that share their
-// heads, four a round: about 8192 workgroups (18900 tokens of 16 prompts, 32 heads of 128: one workgroup for all heads 228 us, two 208, three 197,
-// four 193, six 190, twelve 203).
-struct DenseF8Append { int tokens, splits; };
+// The append over 8-bit pages: units (the new rows of a block of 16), at most, and workgroups that share a unit's heads, four a round.  A workgroup costs
+// its place and its angles, so about as many as the chip holds at once, but several a unit where those have many rows, so that a round's end
+// is short (us with 1, 2, 4, 8 and 12 workgroups a unit: 18900 tokens of 16 prompts, 32 heads of 128: 228, 183, 172, 170, 181; 2 x 1000, 32 heads:
+// 59, 35, 25, 23, 26; 4 x 300, 32 / 8: 23, 15, 11.9, 12.3, 11.7; 300 x 12, 8 heads: 20, 14, 18, 22, 22; 1000 x 4, 28 / 4: 27, 36, 56, 98, 89; 256 x 1, 32 / 8:
+// 18, 12.5, 10.6, 16, 17).
+struct DenseF8Append { int64_t units; int splits; };
 WSVD_HD DenseF8Append dense_f8_append(int64_t n_tokens, int batch, int heads, bool packed) {
-  const int tokens = packed && n_tokens >= 4096 && n_tokens >= 16 * (int64_t)batch ? 16 : 1;
-  const int64_t units = packed ? n_tokens / 16 + (batch < n_tokens ? batch : n_tokens) : n_tokens, rounds = (heads + 3) / 4, fill = 8192 / units;
-  return {tokens, (int)(fill < 1 ? 1 : fill < rounds ? fill : rounds)};
+  const int64_t begun = n_tokens / 16 + 2 * (int64_t)batch, units = packed && begun < n_tokens ? begun : n_tokens, rounds = (heads + 3) / 4;
+  const int64_t least = n_tokens >= 8 * units ? 4 : n_tokens >= 2 * units ? 2 : 1, fill = (1024 + units / 2) / units, some = fill < least ? least : fill;
+  return {units, (int)(some < rounds ? some : rounds)};
 }
 // The page tables' calls: a thread a sequence at a time, and `items` (tokens or table entries) dealt out.
 constexpr int kPagesThreads = 1024;

@@ -151,9 +151,22 @@ int main() {
         for (bool packed : {false, true}) {
           if (!packed && n != batch) continue;
           const DenseF8Append a = dense_f8_append(n, batch, heads, packed);
-          CHECK(a.tokens >= 1 && a.tokens <= 16 && a.splits >= 1 && a.splits <= (heads + 3) / 4);
-          CHECK(dense_launchable((n + a.tokens - 1) / a.tokens * a.splits, 256));
+          CHECK(a.units >= 1 && a.units <= n && a.splits >= 1 && a.splits <= (heads + 3) / 4);
+          CHECK(dense_launchable(a.units * a.splits, 256));
         }
+  // a unit for every block that a call writes to, however its tokens are spread and wherever its sequences stand
+  for (int seed = 1; seed < 3000; seed++) {
+    unsigned x = (unsigned)seed * 2654435761u;
+    auto next = [&](unsigned most) { x = x * 1664525u + 1013904223u; return (int)((x >> 8) % most); };
+    const int batch = 1 + next(70);
+    int64_t n = 0, units = 0;
+    for (int b = 0; b < batch; b++) {
+      const int row = next(50), len = next(seed % 3 ? 4 : 200);
+      n += len;
+      if (len > 0) units += (row + len - 1) / 16 - row / 16 + 1;
+    }
+    if (n > 0) CHECK(dense_f8_append(n, batch, 12, true).units >= units);
+  }
   for (int batch : {1, 64, 65, 256, 257, 65536})
     for (int64_t n : {0, 1, 256, 257, 1024, 1025, 1 << 20, 1 << 24}) {
       const PagesLaunch l = pages_launch(batch, n);
