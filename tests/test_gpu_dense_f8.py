@@ -109,7 +109,13 @@ def test_append_many_short_sequences():
     append_case(2, 1, 64, "bf16", [(7 * i) % 40 for i in range(700)], [(i % 12) for i in range(700)], 16)
 
 
+def test_append_one_token_of_many_sequences():
+    append_case(2, 1, 64, "f16", [(7 * i) % 40 for i in range(333)], [1] * 333, 16)
+    append_case(2, 1, 64, "f16", [(7 * i) % 40 for i in range(333)], [1] * 333, 16, packed=True)
+
+
 def test_append_far_positions():
+    append_case(8, 2, 64, "f16", [3, 0, 19], [1, 1, 1], 64, positions=torch.tensor([900001, 5, 131072]))
     append_case(8, 2, 128, "bf16", [3, 0], [40, 9], 64, positions=torch.arange(49) * 21000 + 7)
 
 
@@ -254,6 +260,41 @@ def test_decode_scales_far_apart(dtype):
     decode_case([300, 64, 1000], 8, 2, 64, dtype, 16, spread=9, q_scale=0.3)
 
 
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16")])
+def test_decode_chunks_of_many_tiles(d, dtype):
+    # a wave looks its tiles up 32 at a time
+    decode_case([9001, 20000, 8192 + 8192], 2, 1, d, dtype, 16, min_chunk=32768)
+
+
+def test_decode_of_nothing():
+    L, pool = Layer(3, 4, 2, 64, "bf16"), F8Pool(gen(2), [0, 0, 0], 2, 64, 16, "bf16")
+    out = torch.full((3, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    W.wsvd_dense_decode_attn_paged_f8(L.ctx, L.desc, randn(gen(3), "bf16", 3, 256).cuda(), 256, L.cache(pool), 0, out)
+    assert (out == 0).all()
+    L.close()
+
+
+@pytest.mark.parametrize("what", ["decode", "chunk"])
+def test_sequences_that_share_pages(what):
+    """A prefix that two sequences have in common: its pages are in both rows of the table."""
+    g, hq, hkv, d = gen(5), 4, 2, 128
+    L, pool = Layer(3, hq, hkv, d, "bf16"), F8Pool(g, [100, 70, 100], hkv, d, 16, "bf16").random(g)
+    pool.table[1, :4] = pool.table[0, :4]
+    pool.table[2] = pool.table[0]
+    T = 3 if what == "decode" else 9
+    q, out = randn(g, "bf16", T, hq * d), torch.empty(T, hq * d, dtype=torch.bfloat16, device="cuda")
+    if what == "decode":
+        W.wsvd_dense_decode_attn_paged_f8(L.ctx, L.desc, q.cuda(), hq * d, L.cache(pool), 100, out)
+    else:
+        W.wsvd_dense_prefill_attn_paged_f8(L.ctx, L.desc, q.cuda(), hq * d, T, prefix([3, 3, 3]).cuda(), L.cache(pool), out, hq * d)
+    m = T // 3
+    for b, n in enumerate(pool.lens):
+        k, v = pool.rows(b)
+        want, size = attend_fast(q[b * m:(b + 1) * m].view(m, hq, d), k, v, list(range(n - m, n)), L.scale)
+        check(out[b * m:(b + 1) * m].cpu().view(m, hq, d), want, size, "bf16", what == "chunk")
+    L.close()
+
+
 def test_decode_longer_than_the_bound_is_reported():
     g = gen(4)
     L, pool = Layer(1, 4, 2, 64, "bf16"), F8Pool(g, [100], 2, 64, 16, "bf16").random(g)
@@ -365,6 +406,10 @@ def test_chunk_page_sizes_and_strides(page_rows):
 @pytest.mark.parametrize("hq,hkv,d,dtype", [(4, 1, 128, "bf16"), (8, 2, 64, "f16"), (2, 2, 128, "f16")])
 def test_chunk_shared_by_workgroups(hq, hkv, d, dtype):
     chunk_case([3000, 900], [7, 40], hq, hkv, d, dtype, 64)
+
+
+def test_chunk_many_sequences():
+    chunk_case([(7 * i) % 90 + 5 for i in range(150)], [i % 6 for i in range(150)], 4, 2, 64, "bf16", 16, spare=1)
 
 
 def test_chunk_queries_that_see_nothing_give_zeros():

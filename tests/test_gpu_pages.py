@@ -76,6 +76,17 @@ def test_steps_of_sequences_that_come_and_go(batch, page_rows, most, in_place):
     D.close()
 
 
+def test_lengths_in_place_beside_a_free_list_that_is_not():
+    D = Device(5, 16, 300, 1500, 1500)
+    for step in range(3):
+        new, n_free = [700, 1, 0, 1300, 40], torch.full_like(D.n_free, KEPT)
+        W.wsvd_pages_grow(D.ctx, D.pool, torch.tensor(new, dtype=torch.int32, device="cuda"), sum(new), D.lens, D.n_free, D.lens, n_free)
+        D.host.grow(new)
+        D.n_free = n_free
+        D.same()
+    D.close()
+
+
 def test_one_token_each():
     D = Device(40, 16, 8, 400, 390)
     D.grow([3 * (i % 7) for i in range(40)])
