@@ -11,7 +11,7 @@ namespace {
 // nothing is handed over.  A workgroup has one unit, or a share of its heads.
 //   The new rows' largest magnitude gives the scale that they need; a block that held rows keeps the larger of its scale and that one, and
 // where its own was the smaller one its codes move (rarely: their exponents shift).  A key is quantised as the 16-bit number that k_out has.
-//   Bound: memory, every element read once, 16-bit ones and codes written once.  18900 tokens of 32 heads of 128 (936 MB): 171 us, 5.5 TB/s, where a
+//   Bound: memory, every element read once, 16-bit ones and codes written once.  19029 tokens of 32 heads of 128 (936 MB): 171 us, 5.5 TB/s, where a
 // copy of 1 GiB reaches 5.1.  Loads and stores go in whole lines (a lane with 16 dims of a row, two requests that share lines: 271 us, with 8 dims of
 // two rows 244); rows as data that is used once (208 of 219 us with two workgroups a unit); the workgroups of a unit side by side (205 -> 197 with
 // three); four waves a SIMD (three, with the next head asked for ahead: 196); units found from the lengths (by workgroups of 16 tokens each: 181; of

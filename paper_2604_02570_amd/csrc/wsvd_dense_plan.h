@@ -89,7 +89,7 @@ WSVD_HD int dense_append_tokens(int64_t n_tokens, int items) {
 }
 // The append over 8-bit pages: units (the new rows of a block of 16), at most, and workgroups that share a unit's heads, four a round.  A workgroup costs
 // its place and its angles, so about as many as the chip holds at once, but several a unit where those have many rows, so that a round's end
-// is short (us with 1, 2, 4, 8 and 12 workgroups a unit: 18900 tokens of 16 prompts, 32 heads of 128: 228, 183, 172, 170, 181; 2 x 1000, 32 heads:
+// is short (us with 1, 2, 4, 8 and 12 workgroups a unit: 19029 tokens of 16 prompts, 32 heads of 128: 228, 183, 172, 170, 181; 2 x 1000, 32 heads:
 // 59, 35, 25, 23, 26; 4 x 300, 32 / 8: 23, 15, 11.9, 12.3, 11.7; 300 x 12, 8 heads: 20, 14, 18, 22, 22; 1000 x 4, 28 / 4: 27, 36, 56, 98, 89; 256 x 1, 32 / 8:
 // 18, 12.5, 10.6, 16, 17).
 struct DenseF8Append { int64_t units; int splits; };

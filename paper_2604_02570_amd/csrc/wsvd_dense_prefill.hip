@@ -25,6 +25,10 @@
 // conflicts.  Matrix and vector instructions of a SIMD's two waves hardly overlap.
 // 1 x 8192 tokens, 32 heads of 128: 1.13 PFLOP/s without a mask, 1.08 causal (products of 16384^2 matrices on that card: 1.35); 16 x 2048
 // tokens: 0.89, with 1.07 GB of queries, keys, values and outputs.  d 64: 0.97 without a mask, 0.90 causal.
+// Over 8-bit pages a block's codes wait in registers for a period and go to LDS as 16-bit numbers, a part after every few products (waited for and
+// converted between the barriers, with nothing beside them, 2048 tokens behind 6144 rows: 243 us; by way of LDS 234; beside the products, each part
+// with its addresses anew, 235; with the lane's places kept 225).  2048 tokens behind 6144 rows, 28 / 4 heads, f16: 221 us, over 16-bit pages 222 on that
+// card; 3 x 333 tokens behind 1501, 32 / 8 heads: 47.3 and 45.1.
 // Tried and not faster: 8 waves to a workgroup (0.86 where 4 have 0.90 at 16 x 2048); 64 rows a wave, one wave a SIMD (0.71: the
 // accumulators no longer fit the vector registers); the weights' sum by the matrix cores; the longest tiles of all sequences first
 // (16 x 2048: 0.57, keys and values no longer stay in the L2); lines of later blocks fetched to the L2 ahead.
@@ -738,6 +742,7 @@ hipError_t launch(DensePromptParams& p, hipStream_t s) {
   constexpr bool PAGED = KEYS != DenseKeys::packed;
   constexpr int NW = 4, ROWS = 32 * NW;
   static_assert(ROWS == kDensePromptRows, "");
+  // (8-bit: one tile a workgroup.  A second one's first blocks would be asked for under the first one's last, in registers that hold codes.)
   const DensePromptGrid grid = dense_prompt_grid(p.n_q, p.B, p.Hkv, p.G, p.causal != 0 && KEYS != DenseKeys::paged_f8);
   const int64_t wgs = grid.workgroups;
   p.pairs = grid.pairs;

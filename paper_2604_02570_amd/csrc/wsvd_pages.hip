@@ -132,7 +132,7 @@ __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
 
 // Pages of the sequences that are done, in the order of sequences and rows, behind the free list's last.  An entry's place is its number
 // among those of the done sequences, as long as all are pages; that some are not (a free list that ended left -1) is rare, and then the last
-// workgroup to come does it all once more, leaving those out.  (1024 sequences, 94 of them done with 27000 pages: 32 us as one workgroup that
+// workgroup to come does it all once more, leaving those out.  (1024 sequences, 99 of them done with 26661 pages: 32 us as one workgroup that
 // counts the pages first.)
 WSVD_DEV void pages_left_out(const PagesParams& p, int n_free, int& end, int* first_sh, int* count_sh, Scan& scan) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
