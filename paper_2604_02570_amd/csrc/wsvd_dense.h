@@ -108,6 +108,10 @@ struct DenseDecodeParams {
   float c_scale;                // sm_scale * log2(e)
   int* err_word;
   DenseScales scales;
+  // several tokens a sequence (8-bit pages): packed queries and outputs, heads of a kv head, workgroups that share a tile of 16 (token, head) pairs
+  const int* cu_q;
+  int64_t out_ld;
+  int n_q, group, splits;
 };
 struct DensePromptParams {
   const uint16_t *q, *k, *v;    // k, v: packed rows (not paged)

@@ -310,7 +310,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         *(v4f*)(o_sh + (wave * G + c) * D + ((NJ * (4 * qd + i) + j + 4 * c) & (D - 1))) = v4f{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
   }
   __syncthreads();
-  dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh);
+  dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) { return p.out + ((int64_t)at.b * p.Hkv * G + kv * G) * D + e; });
 }
 
 template <class T, int D, int TOK>

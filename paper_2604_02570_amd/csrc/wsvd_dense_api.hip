@@ -51,6 +51,13 @@ wsvd_status check_workspace(const wsvd_ctx* ctx, const wsvd_dense_desc* desc) {
   if (st != WSVD_OK) return st;
   return !ctx->ws || ctx->ws_bytes < need ? WSVD_E_WORKSPACE : WSVD_OK;
 }
+// The units of rows that stay whole, and those of a chunk at least
+void set_units(const wsvd_ctx* ctx, const wsvd_dense_desc* desc, bool f8, DenseDecodeParams& p) {
+  // (in rows twice as many at half the row length; the min_chunk setting, where given, is taken for both.  8-bit rows: one sequence of heads of 128,
+  // 32 / 32, 32 / 8 and 28 / 4 of them, 768 rows whole 7.1, 7.3 and 7.7 us, cut 7.8, 8.0, 8.8; 1024 whole 8.1, 8.3, 8.6, cut 7.9, 8.0, 9.1.)
+  p.alone_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : (f8 ? 7 : 5) * 128 / desc->d_head;
+  p.min_units = ctx->opt.min_chunk ? p.alone_units : 2 * 128 / desc->d_head;
+}
 wsvd_status launched(hipError_t e) { return e == hipSuccess ? WSVD_OK : WSVD_E_HIP; }
 
 #define WSVD_TRY(expr) do { const wsvd_status st_ = (expr); if (st_ != WSVD_OK) return st_; } while (0)
@@ -124,10 +131,7 @@ static wsvd_status decode(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void
   p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.G = desc->n_q_heads / desc->n_kv_heads;
   p.max_len = max_seq_len; p.waves = dense_waves(p.B, p.Hkv, max_seq_len);
   p.target = dense_target(p.waves, p.Hkv);
-  // (in rows twice as many at half the row length; the min_chunk setting, where given, is taken for both.  8-bit rows: one sequence of heads of 128,
-  // 32 / 32, 32 / 8 and 28 / 4 of them, 768 rows whole 7.1, 7.3 and 7.7 us, cut 7.8, 8.0, 8.8; 1024 whole 8.1, 8.3, 8.6, cut 7.9, 8.0, 9.1.)
-  p.alone_units = ctx->opt.min_chunk ? (ctx->opt.min_chunk + kDenseUnit - 1) / kDenseUnit : (f8 ? 7 : 5) * 128 / desc->d_head;
-  p.min_units = ctx->opt.min_chunk ? p.alone_units : 2 * 128 / desc->d_head;
+  set_units(ctx, desc, f8, p);
   p.alone = dense_units_of(max_seq_len) <= p.alone_units;
   if (!dense_launchable(dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0), 64 * p.waves)) return WSVD_E_SHAPE;
   WSVD_TRY(check_workspace(ctx, desc));
@@ -184,6 +188,21 @@ static wsvd_status chunk(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void*
   if (!aligned4(cu_q)) return WSVD_E_ALIGN;
   if (n_q < 0 || n_q > kMostTokens) return WSVD_E_SHAPE;
   if (n_q == 0) return WSVD_OK;
+  const int group = desc->n_q_heads / desc->n_kv_heads;
+  const DenseF8Columns columns = dense_f8_columns(n_q, desc->batch, desc->n_kv_heads, group);
+  if (f8 && columns.taken) {
+    DenseDecodeParams p = {};
+    p.q = (const uint16_t*)q; p.q_ld = q_ld; p.out = (uint16_t*)out; p.out_ld = out_ld; p.cu_q = cu_q; p.n_q = (int)n_q; p.pages = pages_of(cache);
+    p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.group = group;
+    p.splits = columns.splits;
+    set_units(ctx, desc, true, p);
+    // (16 columns' parts cost more to join than a group's heads: 8 x 4 tokens behind 1000 rows, 32 / 8 heads, in two chunks 14.1 us, in four 16.2)
+    if (!ctx->opt.min_chunk) p.min_units *= 3;
+    WSVD_TRY(check_workspace(ctx, desc));
+    p.parts = (unsigned long long*)((int*)ctx->ws + kWsCounterInts);
+    p.c_scale = scale_of(desc); p.err_word = ctx->err_word; p.scales = scales_of(cache);
+    return launched(wsvd_launch_dense_decode_f8(p, desc->dtype, desc->d_head, (hipStream_t)hip_stream));
+  }
   DensePromptParams p = {};
   p.q = (const uint16_t*)q; p.out = (uint16_t*)out; p.q_ld = q_ld; p.out_ld = out_ld;
   p.cu_q = cu_q; p.pages = pages_of(cache);

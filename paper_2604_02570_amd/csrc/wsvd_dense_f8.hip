@@ -248,25 +248,74 @@ struct F8Tile {
   v4i k[kF8Tile][D / 64], v[kF8Tile][D / 64];        // two blocks
 };
 
-template <class T, int D, int NW, bool ONCE>
+// Several tokens a sequence (TOKENS, where dense_f8_columns says so): the columns are 16 of a sequence's (token, head) pairs, token-major.  A column sees the rows up to its own.
+struct F8Columns { int q_start, row0, n, first_limit; };             // the sequence's first query, pairs before, columns; the last row that the first one sees
+// A workgroup's sequence, columns and chunk: tile number idx of the call, share `split` of its rows.
+WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lane, DensePlace& at, F8Columns& col) {
+  const int most = p.pages.max_pages * p.pages.page_rows;
+  for (int base = 0, before = 0; base < p.B; base += 64) {
+    const int i = base + lane;
+    int qs = 0, n = 0, len = 0;
+    if (i < p.B) {
+      qs = min(max(p.cu_q[i], 0), p.n_q);
+      n = min(max(p.cu_q[i + 1], qs), p.n_q) - qs;
+      len = p.pages.seq_lens[i];
+    }
+    const int tiles = (n * p.group + 15) / 16, end = before + wave_prefix_int(tiles);
+    const unsigned long long m = __ballot(end > idx);
+    before = __builtin_amdgcn_readlane(end, 63);
+    if (!m) continue;
+    const int l = __builtin_ctzll(m);
+    at.b = base + l;
+    n = __builtin_amdgcn_readlane(n, l); len = __builtin_amdgcn_readlane(len, l);
+    if (len > most && threadIdx.x == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+    len = min(max(len, 0), most);
+    col.q_start = __builtin_amdgcn_readlane(qs, l);
+    col.row0 = 16 * (idx - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(tiles, l)));
+    col.n = min(16, n * p.group - col.row0);
+    col.first_limit = len - n + col.row0 / p.group;
+    at.len = max(len - n + (col.row0 + col.n - 1) / p.group + 1, 0);
+    const int units = dense_units_of(at.len);
+    at.n_chunks = units <= p.alone_units ? 1 : min(p.splits, (units + p.min_units - 1) / p.min_units);
+    at.chunk = split;
+    at.rows = (units + at.n_chunks - 1) / at.n_chunks * kDenseUnit;
+    return split < at.n_chunks;
+  }
+  return false;
+}
+
+template <class T, int D, int NW, bool ONCE, bool TOKENS>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode_f8(DenseDecodeParams p) {
   constexpr int ND = D / 64, NK = D / 32, NJ = D / 16, NB = kF8Tile, ROWS = 16 * NB, AHEAD = 64 / NB;        // rows of a tile; tiles looked up at a time
   extern __shared__ __attribute__((aligned(256))) float o_sh[];      // [NW][G][D]
   __shared__ float m_sh[NW][16], l_sh[NW][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, qd = lane >> 4;
-  const int kv = blockIdx.x % p.Hkv, idx = blockIdx.x / p.Hkv;
+  const int kv = blockIdx.x % p.Hkv;
+  int idx = blockIdx.x / p.Hkv;
   DensePlace at;
-  if (!dense_place(p, idx, lane, at)) return;
-  if (at.chunk == 0 && kv == 0 && threadIdx.x == 0 && p.pages.seq_lens[at.b] > p.max_len) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
-  const int G = p.G;
+  F8Columns col = {};
+  if constexpr (TOKENS) {
+    const int tile = idx / p.splits;
+    if (!f8_columns(p, tile, idx - tile * p.splits, lane, at, col)) return;
+    p.parts += (size_t)tile * p.splits * p.Hkv * 16 * (D + 2);       // (a tile's chunks are among themselves)
+    p.G = col.n;
+    idx = at.chunk;
+  } else {
+    if (!dense_place(p, idx, lane, at)) return;
+    if (at.chunk == 0 && kv == 0 && threadIdx.x == 0 && p.pages.seq_lens[at.b] > p.max_len) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+  }
+  const int G = p.G;                                 // columns
   const int first = at.chunk * at.rows, end = min(at.len, first + at.rows);
   const int n_tiles = (max(end - first, 0) + ROWS - 1) / ROWS;
+  // column c's token and head, and the last row that it sees
+  const int pair = col.row0 + min(c, G - 1), token = TOKENS ? pair / p.group : 0, limit = col.first_limit + token - (TOKENS ? col.row0 / p.group : 0);
 
   // queries as the second operand: column c = head of the group, dims in the order in which a lane has a key's
   v4i q[NK];
   {
-    const uint16_t* qp = p.q + (int64_t)at.b * p.q_ld + (kv * G + min(c, G - 1)) * D + qd * 16;
+    const uint16_t* qp = TOKENS ? p.q + (int64_t)(col.q_start + token) * p.q_ld + (kv * p.group + pair - token * p.group) * D + qd * 16
+                                : p.q + (int64_t)at.b * p.q_ld + (kv * G + min(c, G - 1)) * D + qd * 16;
 #pragma unroll
     for (int j = 0; j < NK; j++) {
       const v4i x = *(const v4i*)(qp + (j >> 1) * 64 + (j & 1) * 8);
@@ -319,17 +368,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
       for (int y = 0; y < 4; y++) s[4 * g + y] = x[y] * p.c_scale;
     }
-    if (r0 + ROWS > end) {                           // rows behind the sequence's end: no weight, and no value that could be NaN
+    // Values that are none, of rows that some columns see and others do not (TOKENS): apart, as ones, and what sees one is none.
+    v4i none[TOKENS ? NB : 1][TOKENS ? ND : 1];
+    bool apart = false;
+    if (r0 + ROWS > (TOKENS ? min(end, col.first_limit + 1) : end)) {  // rows behind the sequence's end: no weight, and no value that could be NaN
+      uint32_t found = 0;
 #pragma unroll
       for (int g = 0; g < NB; g++) {
-        const int n = end - (r0 + 16 * g + 4 * qd);
+        const int at = r0 + 16 * g + 4 * qd, n = end - at;
 #pragma unroll
-        for (int y = 0; y < 4; y++) s[4 * g + y] = y < n ? s[4 * g + y] : -INFINITY;
+        for (int y = 0; y < 4; y++) s[4 * g + y] = y < n && (!TOKENS || at + y <= limit) ? s[4 * g + y] : -INFINITY;
 #pragma unroll
         for (int j = 0; j < ND; j++)
 #pragma unroll
-          for (int y = 0; y < 4; y++) tile.v[g][j][y] &= (int)f8_bytes(n);
+          for (int y = 0; y < 4; y++) {
+            tile.v[g][j][y] &= (int)f8_bytes(n);
+            if constexpr (TOKENS) {
+              const uint32_t flags = (((uint32_t)tile.v[g][j][y] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u, all = flags | (flags - (flags >> 7));
+              found |= flags;
+              none[g][j][y] = (int)(all & 0x38383838u);
+              tile.v[g][j][y] &= (int)~all;
+            }
+          }
       }
+      apart = __ballot(found != 0) != 0;
     }
     float most = s[0];
 #pragma unroll
@@ -365,6 +427,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       o[j] = T::mfma16(a, hi, o[j]);
       o[j] = T::mfma16(a, lo, o[j]);
     }
+    if constexpr (TOKENS) {
+      if (apart) {
+        v4i sees;
+#pragma unroll
+        for (int y = 0; y < 4; y++) {
+          const int at = r0 + 16 * (y >> 1) + 4 * qd + 2 * (y & 1);
+          sees[y] = (int)dense_pack<T>(at <= limit ? 1.f : 0.f, at + 1 <= limit ? 1.f : 0.f);
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; j++) {
+          const uint32_t c0 = (uint32_t)none[0][j >> 2][j & 3], c1 = (uint32_t)none[1][j >> 2][j & 3];
+          const v4f x = T::mfma16(v4i{f8_pair<T, false>(c0, 1.f), f8_pair<T, true>(c0, 1.f), f8_pair<T, false>(c1, 1.f), f8_pair<T, true>(c1, 1.f)}, sees, v4f{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int y = 0; y < 4; y++) o[j][y] = x[y] > 0.f ? __builtin_nanf("") : o[j][y];
+        }
+      }
+    }
   };
   for (int t = wave; t < n_tiles; t += AHEAD * NW) {
     look_up(t);
@@ -395,7 +474,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         *(v4f*)(o_sh + (wave * G + c) * D + ((16 * j + 16 * qd + 4 * y + 4 * c) & (D - 1))) = v4f{o[j][y], o[j + 1][y], o[j + 2][y], o[j + 3][y]};
   }
   __syncthreads();
-  dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh);
+  dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) {
+    if constexpr (TOKENS) {
+      const int pair = col.row0 + e / D, token = pair / p.group;
+      return p.out + (int64_t)(col.q_start + token) * p.out_ld + (kv * p.group + pair - token * p.group) * D + e % D;
+    } else {
+      return p.out + ((int64_t)at.b * p.Hkv * G + kv * G) * D + e;
+    }
+  });
 }
 
 template <class T, int D>
@@ -407,23 +493,26 @@ hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
   else k_dense_append_f8<T, D, false><<<grid, 256, 0, s>>>(p, a.splits);
   return hipGetLastError();
 }
-template <class T, int D, int NW, bool ONCE>
-hipError_t launch_decode_form(const DenseDecodeParams& p, hipStream_t s) {
+template <class T, int D, int NW, bool ONCE, bool TOKENS>
+hipError_t launch_decode_form(const DenseDecodeParams& p, int64_t workgroups, hipStream_t s) {
   constexpr int LDS = NW * D * 4 * 16;
   static LdsLimit limit;
   if (LDS + NW * 16 * 8 > 65536) {
-    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode_f8<T, D, NW, ONCE>, LDS);
+    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode_f8<T, D, NW, ONCE, TOKENS>, LDS);
     if (e != hipSuccess) return e;
   }
-  k_dense_decode_f8<T, D, NW, ONCE><<<(unsigned)dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0), 64 * NW, LDS, s>>>(p);
+  k_dense_decode_f8<T, D, NW, ONCE, TOKENS><<<(unsigned)workgroups, 64 * NW, LDS, s>>>(p);
   return hipGetLastError();
 }
 template <class T, int D, bool ONCE>
 hipError_t launch_decode_waves(const DenseDecodeParams& p, hipStream_t s) {
-  return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE>(p, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE>(p, s) : launch_decode_form<T, D, 2, ONCE>(p, s);
+  const int64_t n = dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0);
+  return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE, false>(p, n, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE, false>(p, n, s)
+                                                                          : launch_decode_form<T, D, 2, ONCE, false>(p, n, s);
 }
 template <class T, int D>
 hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
+  if (p.cu_q) return launch_decode_form<T, D, 8, false, true>(p, dense_f8_columns(p.n_q, p.B, p.Hkv, p.group).tiles * p.splits * p.Hkv, s);
   const bool once = (int64_t)p.B * p.max_len * p.Hkv * D * 2 >= 100000000;      // (as k_dense_decode's)
   return once ? launch_decode_waves<T, D, true>(p, s) : launch_decode_waves<T, D, false>(p, s);
 }

@@ -159,9 +159,9 @@ WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n,
 }
 
 // The waves' results in LDS ([NW][G][D], a head's dims 4 of its number further on in their row) joined, and with those of the other chunks
-// of the sequence; the last chunk's workgroup writes the output.
-template <class T, int D, int NW>
-WSVD_DEV void dense_finish(const DenseDecodeParams& p, const DensePlace& at, int idx, int kv, float* o_sh, const float (*m_sh)[16], const float (*l_sh)[16]) {
+// of the sequence; the last chunk's workgroup writes the output: to(e) is where output e = head * D + dim goes.
+template <class T, int D, int NW, class To>
+WSVD_DEV void dense_finish(const DenseDecodeParams& p, const DensePlace& at, int idx, int kv, float* o_sh, const float (*m_sh)[16], const float (*l_sh)[16], To to) {
   const int G = p.G;
   DensePartial<D, NW> r;
 #pragma unroll
@@ -204,7 +204,7 @@ WSVD_DEV void dense_finish(const DenseDecodeParams& p, const DensePlace& at, int
 #pragma unroll
   for (int i = 0; i < DensePartial<D, NW>::N; i++) {
     const int e = threadIdx.x + i * 64 * NW;
-    if (e < G * D) p.out[((int64_t)at.b * p.Hkv * G + kv * G) * D + e] = (uint16_t)dense_pack<T>(r.L[i] == 0.f ? 0.f : r.U[i] / r.L[i], 0.f);
+    if (e < G * D) *to(e) = (uint16_t)dense_pack<T>(r.L[i] == 0.f ? 0.f : r.U[i] / r.L[i], 0.f);
   }
 }
 

@@ -408,6 +408,41 @@ def test_chunk_shared_by_workgroups(hq, hkv, d, dtype):
     chunk_case([3000, 900], [7, 40], hq, hkv, d, dtype, 64)
 
 
+FEW = [([700, 64, 0, 1501, 17], [5, 1, 0, 3, 4], 8, 8, 64, "f16"), ([700, 64, 33, 1501, 5], [5, 1, 0, 3, 5], 8, 2, 128, "bf16"), ([3000], [7], 32, 8, 128, "bf16"),
+       ([2999, 40], [6, 2], 7, 1, 64, "bf16"), ([100, 100], [3, 1], 16, 1, 128, "f16"), ([2500, 7, 9, 64], [40, 0, 0, 1], 4, 2, 64, "f16"), ([9001], [1], 3, 1, 64, "f16"), ([20, 12], [20, 12], 4, 2, 128, "bf16")]
+
+
+@pytest.mark.parametrize("lens,new,hq,hkv,d,dtype", FEW)
+@pytest.mark.parametrize("page_rows", [16, 112])
+def test_chunk_of_a_few_tokens(lens, new, hq, hkv, d, dtype, page_rows):
+    # (token, head) pairs as columns, tiles of 16 that end inside a token's heads
+    chunk_case(lens, new, hq, hkv, d, dtype, page_rows, spare=1, ld_extra=16)
+
+
+@pytest.mark.parametrize("lens,new,hq,hkv,d,dtype", [FEW[1], FEW[2], FEW[4]])
+def test_chunk_of_a_few_tokens_values_that_are_none(lens, new, hq, hkv, d, dtype):
+    """Of rows that some of a tile's columns see and others do not, of rows that all see, and of the same dim twice."""
+    n, m = lens[0], new[0]
+    chunk_case(lens, new, hq, hkv, d, dtype, 16, none=[("v", 0, n - 1, 0, 3, 0x7F), ("v", 0, n - 2, 0, d - 1, 0xFF), ("v", 0, n - m + 1, 0, d - 1, 0x7F), ("v", 0, n - m, 0, 17, 0xFF),
+                                                       ("v", 0, n - 4, hkv - 1, 33, 0x7F), ("v", 0, 2, hkv - 1, 40, 0x7F)])
+
+
+def test_chunk_of_a_few_tokens_gives_a_sequence_the_same_bits_in_every_place():
+    g, lens, new, hq, hkv, d = gen(45), [700, 33, 2100, 0, 64], [3, 2, 4, 0, 1], 8, 2, 128
+    pool = F8Pool(g, lens, hkv, d, 16, "bf16").random(g)
+    q = [randn(g, "bf16", m, hq * d) for m in new]
+    L, outs = Layer(5, hq, hkv, d, "bf16"), []
+    for order in ([0, 1, 2, 3, 4], [4, 2, 0, 1, 3], [0, 1, 2, 3, 4]):
+        cache = L.cache(pool, [lens[i] for i in order])
+        L.table.copy_(pool.table[order])
+        out = torch.empty(10, hq * d, dtype=torch.bfloat16, device="cuda")
+        W.wsvd_dense_prefill_attn_paged_f8(L.ctx, L.desc, torch.cat([q[i] for i in order]).cuda(), hq * d, 10, prefix([new[i] for i in order]).cuda(), cache, out, hq * d)
+        at = dict(zip(order, prefix([new[i] for i in order]).tolist()))
+        outs.append(torch.cat([out.cpu()[at[i]:at[i] + new[i]] for i in range(5)]))
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    L.close()
+
+
 def test_chunk_many_sequences():
     chunk_case([(7 * i) % 90 + 5 for i in range(150)], [i % 6 for i in range(150)], 4, 2, 64, "bf16", 16, spare=1)
 
