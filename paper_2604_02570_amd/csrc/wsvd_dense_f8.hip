@@ -248,9 +248,11 @@ struct F8Tile {
   v4i k[kF8Tile][D / 64], v[kF8Tile][D / 64];        // two blocks
 };
 
-// Several tokens a sequence (TOKENS, where dense_f8_columns says so): the columns are 16 of a sequence's (token, head) pairs, token-major.  A column sees the rows up to its own.
+// Several tokens a sequence (where dense_f8_columns says so): the columns are 16 of a sequence's (token, head) pairs, token-major, or two sets of 16 that
+// share the rows' codes and their conversion (which costs as much as one set's products).  A column sees the rows up to its own.
 struct F8Columns { int q_start, row0, n, first_limit; };             // the sequence's first query, pairs before, columns; the last row that the first one sees
-// A workgroup's sequence, columns and chunk: tile number idx of the call, share `split` of its rows.
+// A workgroup's sequence, columns (of WIDTH) and chunk: tile number idx of the call, share `split` of its rows.
+template <int WIDTH>
 WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lane, DensePlace& at, F8Columns& col) {
   const int most = p.pages.max_pages * p.pages.page_rows;
   for (int base = 0, before = 0; base < p.B; base += 64) {
@@ -261,7 +263,7 @@ WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lan
       n = min(max(p.cu_q[i + 1], qs), p.n_q) - qs;
       len = p.pages.seq_lens[i];
     }
-    const int tiles = (n * p.group + 15) / 16, end = before + wave_prefix_int(tiles);
+    const int tiles = (n * p.group + WIDTH - 1) / WIDTH, end = before + wave_prefix_int(tiles);
     const unsigned long long m = __ballot(end > idx);
     before = __builtin_amdgcn_readlane(end, 63);
     if (!m) continue;
@@ -271,8 +273,8 @@ WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lan
     if (len > most && threadIdx.x == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
     len = min(max(len, 0), most);
     col.q_start = __builtin_amdgcn_readlane(qs, l);
-    col.row0 = 16 * (idx - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(tiles, l)));
-    col.n = min(16, n * p.group - col.row0);
+    col.row0 = WIDTH * (idx - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(tiles, l)));
+    col.n = min(WIDTH, n * p.group - col.row0);
     col.first_limit = len - n + col.row0 / p.group;
     at.len = max(len - n + (col.row0 + col.n - 1) / p.group + 1, 0);
     const int units = dense_units_of(at.len);
@@ -284,43 +286,47 @@ WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lan
   return false;
 }
 
-template <class T, int D, int NW, bool ONCE, bool TOKENS>
+// SETS: of 16 columns of several tokens; 0: one token a sequence, its heads.
+template <class T, int D, int NW, bool ONCE, int SETS>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode_f8(DenseDecodeParams p) {
   constexpr int ND = D / 64, NK = D / 32, NJ = D / 16, NB = kF8Tile, ROWS = 16 * NB, AHEAD = 64 / NB;        // rows of a tile; tiles looked up at a time
   extern __shared__ __attribute__((aligned(256))) float o_sh[];      // [NW][G][D]
   __shared__ float m_sh[NW][16], l_sh[NW][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, qd = lane >> 4;
+  constexpr bool TOKENS = SETS > 0;
+  constexpr int C = TOKENS ? SETS : 1;
   const int kv = blockIdx.x % p.Hkv;
   int idx = blockIdx.x / p.Hkv;
   DensePlace at;
   F8Columns col = {};
   if constexpr (TOKENS) {
     const int tile = idx / p.splits;
-    if (!f8_columns(p, tile, idx - tile * p.splits, lane, at, col)) return;
-    p.parts += (size_t)tile * p.splits * p.Hkv * 16 * (D + 2);       // (a tile's chunks are among themselves)
-    p.G = col.n;
+    if (!f8_columns<16 * C>(p, tile, idx - tile * p.splits, lane, at, col)) return;
+    p.parts += (size_t)tile * p.splits * p.Hkv * (16 * C) * (D + 2); // (a tile's chunks are among themselves)
     idx = at.chunk;
   } else {
     if (!dense_place(p, idx, lane, at)) return;
     if (at.chunk == 0 && kv == 0 && threadIdx.x == 0 && p.pages.seq_lens[at.b] > p.max_len) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
+    col.n = p.G;
   }
-  const int G = p.G;                                 // columns
   const int first = at.chunk * at.rows, end = min(at.len, first + at.rows);
   const int n_tiles = (max(end - first, 0) + ROWS - 1) / ROWS;
-  // column c's token and head, and the last row that it sees
-  const int pair = col.row0 + min(c, G - 1), token = TOKENS ? pair / p.group : 0, limit = col.first_limit + token - (TOKENS ? col.row0 / p.group : 0);
 
-  // queries as the second operand: column c = head of the group, dims in the order in which a lane has a key's
-  v4i q[NK];
-  {
+  // queries as the second operand: column c of a set = head of the group, or pair, dims in the order in which a lane has a key's
+  v4i q[C][NK];
+  int limit[C];                                      // the last row that the column sees
+#pragma unroll
+  for (int x = 0; x < C; x++) {
+    const int pair = col.row0 + min(16 * x + c, col.n - 1), token = TOKENS ? pair / p.group : 0;
+    limit[x] = col.first_limit + token - (TOKENS ? col.row0 / p.group : 0);
     const uint16_t* qp = TOKENS ? p.q + (int64_t)(col.q_start + token) * p.q_ld + (kv * p.group + pair - token * p.group) * D + qd * 16
-                                : p.q + (int64_t)at.b * p.q_ld + (kv * G + min(c, G - 1)) * D + qd * 16;
+                                : p.q + (int64_t)at.b * p.q_ld + (kv * p.G + pair) * D + qd * 16;
 #pragma unroll
     for (int j = 0; j < NK; j++) {
-      const v4i x = *(const v4i*)(qp + (j >> 1) * 64 + (j & 1) * 8);
+      const v4i y = *(const v4i*)(qp + (j >> 1) * 64 + (j & 1) * 8);
 #pragma unroll
-      for (int i = 0; i < 4; i++) q[j][i] = c < G ? x[i] : 0;
+      for (int i = 0; i < 4; i++) q[x][j][i] = 16 * x + c < col.n ? y[i] : 0;
     }
   }
   // Where the wave's next AHEAD tiles lie, a lane for each of a tile's blocks.
@@ -347,26 +353,36 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int j = 0; j < ND; j++) tile.v[g][j] = load_row<ONCE>((const v4i*)(vp + j * 1024 + lane * 16));
     }
   };
-  float m = -INFINITY, l = 0.f;
-  v4f o[NJ];                                         // [64 dims][one of 4]: row 4 qd + i is dim 64 (j / 4) + 16 qd + 4 i + j % 4
+  float m[C], l[C];
+  v4f o[C][NJ];                                      // [64 dims][one of 4]: row 4 qd + i is dim 64 (j / 4) + 16 qd + 4 i + j % 4
 #pragma unroll
-  for (int j = 0; j < NJ; j++) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < C; x++) {
+    m[x] = -INFINITY; l[x] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NJ; j++) o[x][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  }
 
   auto attend = [&](F8Tile<D>& tile, int t, int i) {
 #pragma clang fp contract(off)                       // (a score is the same number against the limit and in its weight)
     const int r0 = first + t * ROWS;
-    float s[4 * NB];
+    float s[C][4 * NB];
 #pragma unroll
     for (int g = 0; g < NB; g++) {
       const float scale = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(k_scale, NB * i + g));
-      v4f x = {0.f, 0.f, 0.f, 0.f};
+      v4f y[C];
+#pragma unroll
+      for (int x = 0; x < C; x++) y[x] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < NK; j++) {
         const uint32_t c0 = (uint32_t)tile.k[g][j >> 1][2 * (j & 1)], c1 = (uint32_t)tile.k[g][j >> 1][2 * (j & 1) + 1];
-        x = T::mfma16(v4i{f8_pair<T, false>(c0, scale), f8_pair<T, true>(c0, scale), f8_pair<T, false>(c1, scale), f8_pair<T, true>(c1, scale)}, q[j], x);
+        const v4i a = {f8_pair<T, false>(c0, scale), f8_pair<T, true>(c0, scale), f8_pair<T, false>(c1, scale), f8_pair<T, true>(c1, scale)};
+#pragma unroll
+        for (int x = 0; x < C; x++) y[x] = T::mfma16(a, q[x][j], y[x]);
       }
 #pragma unroll
-      for (int y = 0; y < 4; y++) s[4 * g + y] = x[y] * p.c_scale;
+      for (int x = 0; x < C; x++)
+#pragma unroll
+        for (int z = 0; z < 4; z++) s[x][4 * g + z] = y[x][z] * p.c_scale;
     }
     // Values that are none, of rows that some columns see and others do not (TOKENS): apart, as ones, and what sees one is none.
     v4i none[TOKENS ? NB : 1][TOKENS ? ND : 1];
@@ -377,7 +393,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int g = 0; g < NB; g++) {
         const int at = r0 + 16 * g + 4 * qd, n = end - at;
 #pragma unroll
-        for (int y = 0; y < 4; y++) s[4 * g + y] = y < n && (!TOKENS || at + y <= limit) ? s[4 * g + y] : -INFINITY;
+        for (int x = 0; x < C; x++)
+#pragma unroll
+          for (int y = 0; y < 4; y++) s[x][4 * g + y] = y < n && (!TOKENS || at + y <= limit[x]) ? s[x][4 * g + y] : -INFINITY;
 #pragma unroll
         for (int j = 0; j < ND; j++)
 #pragma unroll
@@ -393,54 +411,63 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       }
       apart = __ballot(found != 0) != 0;
     }
-    float most = s[0];
-#pragma unroll
-    for (int y = 1; y < 4 * NB; y++) most = fmaxf(most, s[y]);
-    if (__ballot(most - m > T::kTop)) {              // (see the element types)
-      const float top = quarters_max(most), low = top - T::kRaise;
-      const float mn = fmaxf(m, top - low > T::kTop ? top : low);    // (steps of 16, between scores of 2^27 and 2^28)
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      l *= keep;
-#pragma unroll
-      for (int j = 0; j < NJ; j++)
-#pragma unroll
-        for (int y = 0; y < 4; y++) o[j][y] *= keep;
-      m = mn;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
-    float w[8];
-#pragma unroll
-    for (int y = 0; y < 8; y++) { w[y] = __builtin_amdgcn_exp2f(s[y] - ref); l += w[y]; }
     // weights as a pair of 16-bit numbers (bf16: off by at most 2^-17 of the weight; f16: by 2^-23 of it or 2^-36 of the reference's)
-    v4i hi, lo;
+    v4i hi[C], lo[C];
 #pragma unroll
-    for (int y = 0; y < 4; y++) {
-      const uint32_t h = dense_pack<T>(w[2 * y], w[2 * y + 1]);
-      hi[y] = (int)h;
-      lo[y] = (int)dense_pack<T>(w[2 * y] - dense_low<T>(h), w[2 * y + 1] - dense_high<T>(h));
+    for (int x = 0; x < C; x++) {
+      float most = s[x][0];
+#pragma unroll
+      for (int y = 1; y < 4 * NB; y++) most = fmaxf(most, s[x][y]);
+      if (__ballot(most - m[x] > T::kTop)) {         // (see the element types)
+        const float top = quarters_max(most), low = top - T::kRaise;
+        const float mn = fmaxf(m[x], top - low > T::kTop ? top : low);       // (steps of 16, between scores of 2^27 and 2^28)
+        const float keep = m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[x] - mn);
+        l[x] *= keep;
+#pragma unroll
+        for (int j = 0; j < NJ; j++)
+#pragma unroll
+          for (int y = 0; y < 4; y++) o[x][j][y] *= keep;
+        m[x] = mn;
+      }
+      const float ref = m[x] == -INFINITY ? 0.f : m[x];
+      float w[8];
+#pragma unroll
+      for (int y = 0; y < 8; y++) { w[y] = __builtin_amdgcn_exp2f(s[x][y] - ref); l[x] += w[y]; }
+#pragma unroll
+      for (int y = 0; y < 4; y++) {
+        const uint32_t h = dense_pack<T>(w[2 * y], w[2 * y + 1]);
+        hi[x][y] = (int)h;
+        lo[x][y] = (int)dense_pack<T>(w[2 * y] - dense_low<T>(h), w[2 * y + 1] - dense_high<T>(h));
+      }
     }
     const float s0 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_scale, NB * i)), s1 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_scale, NB * i + 1));
 #pragma unroll
     for (int j = 0; j < NJ; j++) {
       const uint32_t c0 = (uint32_t)tile.v[0][j >> 2][j & 3], c1 = (uint32_t)tile.v[1][j >> 2][j & 3];
       const v4i a = {f8_pair<T, false>(c0, s0), f8_pair<T, true>(c0, s0), f8_pair<T, false>(c1, s1), f8_pair<T, true>(c1, s1)};
-      o[j] = T::mfma16(a, hi, o[j]);
-      o[j] = T::mfma16(a, lo, o[j]);
+#pragma unroll
+      for (int x = 0; x < C; x++) {
+        o[x][j] = T::mfma16(a, hi[x], o[x][j]);
+        o[x][j] = T::mfma16(a, lo[x], o[x][j]);
+      }
     }
     if constexpr (TOKENS) {
       if (apart) {
-        v4i sees;
 #pragma unroll
-        for (int y = 0; y < 4; y++) {
-          const int at = r0 + 16 * (y >> 1) + 4 * qd + 2 * (y & 1);
-          sees[y] = (int)dense_pack<T>(at <= limit ? 1.f : 0.f, at + 1 <= limit ? 1.f : 0.f);
-        }
+        for (int x = 0; x < C; x++) {
+          v4i sees;
 #pragma unroll
-        for (int j = 0; j < NJ; j++) {
-          const uint32_t c0 = (uint32_t)none[0][j >> 2][j & 3], c1 = (uint32_t)none[1][j >> 2][j & 3];
-          const v4f x = T::mfma16(v4i{f8_pair<T, false>(c0, 1.f), f8_pair<T, true>(c0, 1.f), f8_pair<T, false>(c1, 1.f), f8_pair<T, true>(c1, 1.f)}, sees, v4f{0.f, 0.f, 0.f, 0.f});
+          for (int y = 0; y < 4; y++) {
+            const int at = r0 + 16 * (y >> 1) + 4 * qd + 2 * (y & 1);
+            sees[y] = (int)dense_pack<T>(at <= limit[x] ? 1.f : 0.f, at + 1 <= limit[x] ? 1.f : 0.f);
+          }
 #pragma unroll
-          for (int y = 0; y < 4; y++) o[j][y] = x[y] > 0.f ? __builtin_nanf("") : o[j][y];
+          for (int j = 0; j < NJ; j++) {
+            const uint32_t c0 = (uint32_t)none[0][j >> 2][j & 3], c1 = (uint32_t)none[1][j >> 2][j & 3];
+            const v4f n = T::mfma16(v4i{f8_pair<T, false>(c0, 1.f), f8_pair<T, true>(c0, 1.f), f8_pair<T, false>(c1, 1.f), f8_pair<T, true>(c1, 1.f)}, sees, v4f{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int y = 0; y < 4; y++) o[x][j][y] = n[y] > 0.f ? __builtin_nanf("") : o[x][j][y];
+          }
         }
       }
     }
@@ -462,26 +489,33 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     if (i + 1 < n) attend(t1, t + NW * (i + 1), i + 1);
   }
   if (__ballot(bad) && lane == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
-  l = quarters_sum(l);
-  __syncthreads();
-  if (c < G) {
-    if (qd == 0) { m_sh[wave][c] = m; l_sh[wave][c] = l; }
-    // (A head's dims start 4 c further on in its row, since the heads' rows begin at one bank.)
 #pragma unroll
-    for (int y = 0; y < 4; y++)
+  for (int x = 0; x < C; x++) {
+    const int G = min(col.n - 16 * x, 16);           // the set's columns
+    if (G <= 0) break;
+    const float sum = quarters_sum(l[x]);
+    __syncthreads();
+    if (c < G) {
+      if (qd == 0) { m_sh[wave][c] = m[x]; l_sh[wave][c] = sum; }
+      // (A head's dims start 4 c further on in its row, since the heads' rows begin at one bank.)
 #pragma unroll
-      for (int j = 0; j < NJ; j += 4)
-        *(v4f*)(o_sh + (wave * G + c) * D + ((16 * j + 16 * qd + 4 * y + 4 * c) & (D - 1))) = v4f{o[j][y], o[j + 1][y], o[j + 2][y], o[j + 3][y]};
-  }
-  __syncthreads();
-  dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) {
-    if constexpr (TOKENS) {
-      const int pair = col.row0 + e / D, token = pair / p.group;
-      return p.out + (int64_t)(col.q_start + token) * p.out_ld + (kv * p.group + pair - token * p.group) * D + e % D;
-    } else {
-      return p.out + ((int64_t)at.b * p.Hkv * G + kv * G) * D + e;
+      for (int y = 0; y < 4; y++)
+#pragma unroll
+        for (int j = 0; j < NJ; j += 4)
+          *(v4f*)(o_sh + (wave * G + c) * D + ((16 * j + 16 * qd + 4 * y + 4 * c) & (D - 1))) = v4f{o[x][j][y], o[x][j + 1][y], o[x][j + 2][y], o[x][j + 3][y]};
     }
-  });
+    __syncthreads();
+    p.G = G;
+    dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) {
+      if constexpr (TOKENS) {
+        const int pair = col.row0 + 16 * x + e / D, token = pair / p.group;
+        return p.out + (int64_t)(col.q_start + token) * p.out_ld + (kv * p.group + pair - token * p.group) * D + e % D;
+      } else {
+        return p.out + ((int64_t)at.b * p.Hkv * G + kv * G) * D + e;
+      }
+    });
+    p.parts += (size_t)p.splits * p.Hkv * 16 * (D + 2);              // (of several tokens: the next set's words)
+  }
 }
 
 template <class T, int D>
@@ -493,26 +527,30 @@ hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
   else k_dense_append_f8<T, D, false><<<grid, 256, 0, s>>>(p, a.splits);
   return hipGetLastError();
 }
-template <class T, int D, int NW, bool ONCE, bool TOKENS>
+template <class T, int D, int NW, bool ONCE, int SETS>
 hipError_t launch_decode_form(const DenseDecodeParams& p, int64_t workgroups, hipStream_t s) {
   constexpr int LDS = NW * D * 4 * 16;
   static LdsLimit limit;
   if (LDS + NW * 16 * 8 > 65536) {
-    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode_f8<T, D, NW, ONCE, TOKENS>, LDS);
+    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode_f8<T, D, NW, ONCE, SETS>, LDS);
     if (e != hipSuccess) return e;
   }
-  k_dense_decode_f8<T, D, NW, ONCE, TOKENS><<<(unsigned)workgroups, 64 * NW, LDS, s>>>(p);
+  k_dense_decode_f8<T, D, NW, ONCE, SETS><<<(unsigned)workgroups, 64 * NW, LDS, s>>>(p);
   return hipGetLastError();
 }
 template <class T, int D, bool ONCE>
 hipError_t launch_decode_waves(const DenseDecodeParams& p, hipStream_t s) {
   const int64_t n = dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0);
-  return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE, false>(p, n, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE, false>(p, n, s)
-                                                                          : launch_decode_form<T, D, 2, ONCE, false>(p, n, s);
+  return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE, 0>(p, n, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE, 0>(p, n, s)
+                                                                          : launch_decode_form<T, D, 2, ONCE, 0>(p, n, s);
 }
 template <class T, int D>
 hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
-  if (p.cu_q) return launch_decode_form<T, D, 8, false, true>(p, dense_f8_columns(p.n_q, p.B, p.Hkv, p.group).tiles * p.splits * p.Hkv, s);
+  if (p.cu_q) {
+    const DenseF8Columns c = dense_f8_columns(p.n_q, p.B, p.Hkv, p.group);
+    const int64_t n = c.tiles * p.splits * p.Hkv;
+    return c.sets == 2 ? launch_decode_form<T, D, 8, false, 2>(p, n, s) : launch_decode_form<T, D, 8, false, 1>(p, n, s);
+  }
   const bool once = (int64_t)p.B * p.max_len * p.Hkv * D * 2 >= 100000000;      // (as k_dense_decode's)
   return once ? launch_decode_waves<T, D, true>(p, s) : launch_decode_waves<T, D, false>(p, s);
 }

@@ -99,18 +99,23 @@ WSVD_HD DenseF8Append dense_f8_append(int64_t n_tokens, int batch, int heads, bo
   return {units, (int)(some < rounds ? some : rounds)};
 }
 // Attention of a few tokens a sequence over 8-bit pages: tiles of 16 (token, head) pairs, the columns of the decode attention, where the prompt
-// attention's of 128 would be mostly empty.  Taken where the call's tokens, spread evenly, make at most 4 tiles a sequence, and no more in all than
+// attention's of 128 would be mostly empty.  Taken where the call's tokens, spread evenly, make at most 64 pairs a sequence, and no more tiles in all than
 // the chip has CUs: a tile reads its rows for itself, at 70 GB/s a CU, and a workgroup of 8 waves costs about 5 us (us as tiles of 128 and of 16; 32 / 8
-// heads of 128 unless told: 4 x 5 tokens behind 700 rows, 8 heads of 64: 12.3 and 6.6; 1 x 7 behind 3000: 18 and 15; 8 x 4 behind 1000: 20 and 14; 32 x 3
+// heads of 128 unless told: 4 x 5 tokens behind 700 rows, 8 heads of 64: 12.3 and 6.6; 1 x 7 behind 3000: 18 and 14; 8 x 4 behind 1000: 20 and 14; 32 x 3
 // behind 2000: 44 and 30; 20 x 5 behind 1500, 28 / 4 heads: 27 and 17; 2 x 64 behind 3000, 8 heads: 21 and 16; past the limits 32 x 8 behind 2000: 44 and 41;
 // 8 x 20 behind 3000: 31 and 37; 64 x 8 behind 300: 16 and 37; 1 x 64 behind 30000: 57 and 112).
+//   sets: of 16 pairs that a tile holds: two where tiles of one would be too many and those of two are not (a tile of two takes 1.6 times as long; us as
+// tiles of 128 and of two sets: 32 x 8 behind 2000: 44 and 37; 32 x 6 behind 2000, 32 / 8 heads of 64: 29 and 18; 64 x 5 behind 1000, 16 / 2 heads of 64: 19
+// and 14; 32 x 5 behind 200: 11.6 and 13.0; two sets where one is few enough, 1 x 7 behind 3000: 22; past 64 pairs 1 x 32 behind 2000: 17 and 23; 8 x 16
+// behind 1000, 28 / 4 heads: 19 and 22; past the CUs 64 x 8 behind 1000: 33 and 50).
 //   tiles: at most, since every sequence with tokens ends inside one.  splits: workgroups that may share a tile's rows, as many as give every CU one, and
 // no more than one fold takes (1 x 7 behind 3000: up to 4 14.2, 8 15.4, 16 18.3; 1 x 4 behind 8000, 28 / 4 heads: 19.0, 18.0, 19.7).
-struct DenseF8Columns { bool taken; int64_t tiles; int splits; };
+struct DenseF8Columns { bool taken; int sets; int64_t tiles; int splits; };
 WSVD_HD DenseF8Columns dense_f8_columns(int64_t n_q, int batch, int Hkv, int group) {
-  const int64_t some = batch < n_q ? batch : n_q, each = ((n_q * group + some - 1) / some + 15) / 16, even = each * some * Hkv;
-  const int64_t n = even <= kDenseCus ? kDenseCus / even : 1;
-  return {each <= 4 && even <= kDenseCus, n_q * group / 16 + some, (int)(n > kDenseFold ? kDenseFold : n)};
+  const int64_t some = batch < n_q ? batch : n_q, pairs = (n_q * group + some - 1) / some;
+  const int sets = (pairs + 15) / 16 * some * Hkv <= kDenseCus ? 1 : 2, width = 16 * sets;
+  const int64_t even = (pairs + width - 1) / width * some * Hkv, n = even <= kDenseCus ? kDenseCus / even : 1;
+  return {pairs <= 64 && even <= kDenseCus, sets, n_q * group / width + some, (int)(n > kDenseFold ? kDenseFold : n)};
 }
 // The page tables' calls: a thread a sequence at a time, and `items` (tokens or table entries) dealt out.
 constexpr int kPagesThreads = 1024;

@@ -154,22 +154,23 @@ int main() {
           CHECK(a.units >= 1 && a.units <= n && a.splits >= 1 && a.splits <= (heads + 3) / 4);
           CHECK(dense_launchable(a.units * a.splits, 256));
         }
-  // a few tokens a sequence as columns: a tile for every 16 pairs of every sequence, and words for their parts in the workspace's 512 parts of 128 rows
+  // a few tokens a sequence as columns: a tile for every 16 or 32 pairs of every sequence, and words for their parts in the workspace's 512 parts of 128 rows
   for (int seed = 1; seed < 20000; seed++) {
     unsigned x = (unsigned)seed * 2654435761u;
     auto next = [&](unsigned most) { x = x * 1664525u + 1013904223u; return (int)((x >> 8) % most); };
     const int batch = 1 + next(seed % 2 ? 8 : 300), group = 1 + next(16), Hkv = 1 << next(11);
-    int64_t n = 0, tiles = 0;
+    int64_t n = 0, tiles[3] = {};
     for (int b = 0; b < batch; b++) {
       const int len = next(7) ? next(seed % 5 ? 4 : 90) : 0;
-      n += len; tiles += (len * group + 15) / 16;
+      n += len; tiles[1] += (len * group + 15) / 16; tiles[2] += (len * group + 31) / 32;
     }
     if (n == 0) continue;
     const DenseF8Columns c = dense_f8_columns(n, batch, Hkv, group);
-    CHECK(c.tiles >= tiles && c.splits >= 1 && c.splits <= kDenseFold);
-    if (c.taken) CHECK(dense_launchable(c.tiles * c.splits * Hkv, 512) && (c.splits == 1 || c.tiles * c.splits * Hkv * 16 * 8 <= (int64_t)kDensePromptParts * kDensePromptRows * 4));
+    CHECK((c.sets == 1 || c.sets == 2) && c.tiles >= tiles[c.sets] && c.splits >= 1 && c.splits <= kDenseFold);
+    if (c.taken) CHECK(dense_launchable(c.tiles * c.splits * Hkv, 512) && (c.splits == 1 || c.tiles * c.splits * Hkv * c.sets * 16 * 8 <= (int64_t)kDensePromptParts * kDensePromptRows * 4));
   }
   CHECK(dense_f8_columns(1, 65536, 1024, 1).tiles == 1 && !dense_f8_columns(1 << 24, 1, 1, 16).taken && dense_f8_columns(20, 4, 8, 1).taken);
+  CHECK(dense_f8_columns(256, 32, 8, 4).taken && dense_f8_columns(256, 32, 8, 4).sets == 2 && dense_f8_columns(20, 4, 8, 1).sets == 1);
   // a unit for every block that a call writes to, however its tokens are spread and wherever its sequences stand
   for (int seed = 1; seed < 3000; seed++) {
     unsigned x = (unsigned)seed * 2654435761u;

@@ -427,6 +427,25 @@ def test_chunk_of_a_few_tokens_values_that_are_none(lens, new, hq, hkv, d, dtype
                                                        ("v", 0, n - 4, hkv - 1, 33, 0x7F), ("v", 0, 2, hkv - 1, 40, 0x7F)])
 
 
+MANY = [(40, 8, 16, 4, 64, "bf16"), (40, 7, 16, 4, 128, "f16"), (20, 16, 16, 8, 128, "bf16"), (150, 5, 7, 1, 64, "f16"), (10, 30, 15, 15, 64, "bf16"), (17, 3, 112, 8, 128, "f16")]
+
+
+@pytest.mark.parametrize("batch,most,hq,hkv,d,dtype", MANY)
+def test_chunk_of_a_few_tokens_of_many_sequences(batch, most, hq, hkv, d, dtype):
+    # tiles of 32 pairs where those of 16 would be more than the chip has CUs: sequences that fill one set and part of the other, one set, one pair, none
+    lens = [(67 * i) % 300 + most for i in range(batch)]
+    lens[1], lens[2] = 2100, most
+    chunk_case(lens, [(1, most, 0, most - 1, most)[i % 5] for i in range(batch)], hq, hkv, d, dtype, 48, spare=1, ld_extra=16)
+
+
+@pytest.mark.parametrize("batch,most,hq,hkv,d,dtype", [MANY[0], MANY[1]])
+def test_chunk_of_a_few_tokens_of_many_sequences_values_that_are_none(batch, most, hq, hkv, d, dtype):
+    lens = [(67 * i) % 300 + most for i in range(batch)]
+    n = lens[1]
+    chunk_case(lens, [most] * batch, hq, hkv, d, dtype, 16, none=[("v", 1, n - 1, 0, 3, 0x7F), ("v", 1, n - 2, 0, d - 1, 0xFF), ("v", 1, n - most + 1, 0, d - 1, 0x7F), ("v", 1, n - most, 0, 17, 0xFF),
+                                                                  ("v", 1, n - 5, hkv - 1, 33, 0x7F), ("v", 1, 2, hkv - 1, 40, 0x7F)])
+
+
 def test_chunk_of_a_few_tokens_gives_a_sequence_the_same_bits_in_every_place():
     g, lens, new, hq, hkv, d = gen(45), [700, 33, 2100, 0, 64], [3, 2, 4, 0, 1], 8, 2, 128
     pool = F8Pool(g, lens, hkv, d, 16, "bf16").random(g)
