@@ -112,6 +112,7 @@ struct DenseDecodeParams {
   const int* cu_q;
   int64_t out_ld;
   int n_q, group, splits;
+  int joins;                    // sequences that have workgroups to join their chunks (8-bit pages)
 };
 struct DensePromptParams {
   const uint16_t *q, *k, *v;    // k, v: packed rows (not paged)

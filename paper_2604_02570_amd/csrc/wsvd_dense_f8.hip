@@ -286,6 +286,70 @@ WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lan
   return false;
 }
 
+// The join of a sequence of many chunks, a workgroup a head: dims in lanes, an eighth of the chunks a wave, all words of a thread asked for at once.
+// The workgroup has a higher number than those it waits for, and the wait is bounded.  Words are cleared where they are read.
+template <class T, int D>
+WSVD_DEV void f8_join(const DenseDecodeParams& p, int idx, int units, int kv, int lane, int wave, float* sh) {
+  constexpr int ND = D / 64, CHUNKS = kDenseFold * kDenseFold / 8;   // a wave's chunks
+  const int n_mine = lane < p.B ? dense_chunks(dense_units_of(dense_length(p, lane)), units) : 0;
+  const unsigned long long many = __ballot(n_mine > kF8Whole);
+  const int which = idx / p.G, g = idx - which * p.G;
+  const unsigned long long sel = __ballot((many >> lane & 1) && __builtin_popcountll(many & ((1ull << lane) - 1)) == which);
+  if (!sel) return;
+  const int b = __builtin_ctzll(sel), n = __builtin_amdgcn_readlane(n_mine, b), c0 = __builtin_amdgcn_readlane(wave_prefix_int(n_mine), b) - n;
+  const DensePartWords part = dense_many(p, c0, n, 0, kv, g, D);
+  const size_t stride = (size_t)p.Hkv * p.G * D;
+  const unsigned long long none = split_word(0.f);
+  auto come = [&](unsigned long long x) { return (uint32_t)(x >> 32) == kSplitTag; };
+  unsigned long long w[ND][CHUNKS], wm = none, wl = none;          // (maxima and sums: the first wave's, a lane a chunk)
+  float *const f_sh = sh, *const l_sh = sh + 64, *const u_sh = sh + 128;       // [chunk], [1], [wave][D]
+  const bool has = wave == 0 && lane < n;
+  bool all = false;
+  for (int budget = 1 << 20; budget && !all; budget--) {
+    if (has) { wm = dense_word(part.max + lane); wl = dense_word(part.max + n + lane); }
+#pragma unroll
+    for (int x = 0; x < ND; x++)
+#pragma unroll
+      for (int k = 0; k < CHUNKS; k++) w[x][k] = wave + 8 * k < n ? dense_word(part.row + (wave + 8 * k) * stride + x * 64 + lane) : none;
+    all = come(wm) && come(wl);
+#pragma unroll
+    for (int x = 0; x < ND; x++)
+#pragma unroll
+      for (int k = 0; k < CHUNKS; k++) all = all && come(w[x][k]);
+    if (!all) __builtin_amdgcn_s_sleep(1);
+  }
+  if (!all) atomicExch(p.err_word, (int)WSVD_E_HIP);               // never seen; keeps the wait finite
+  if (wave == 0) {
+    const float m = has ? __uint_as_float((uint32_t)wm) : -INFINITY, M = wave_max(m);
+    const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);      // (nothing seen: l and u are 0, or NaN)
+    const float L = wave_sum(__uint_as_float((uint32_t)wl) * f);
+    f_sh[lane] = f;
+    if (lane == 0) *l_sh = L;
+    if (has) { dense_clear(part.max + lane); dense_clear(part.max + n + lane); }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < ND; x++) {
+    float U = 0.f;
+#pragma unroll
+    for (int k = 0; k < CHUNKS; k++)
+      if (wave + 8 * k < n) {
+        U += dense_scaled(__uint_as_float((uint32_t)w[x][k]), f_sh[wave + 8 * k]);
+        dense_clear(part.row + (wave + 8 * k) * stride + x * 64 + lane);
+      }
+    u_sh[wave * D + x * 64 + lane] = U;
+  }
+  __syncthreads();
+  const int x = threadIdx.x;
+  if (x < D) {
+    const float L = *l_sh;
+    float U = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; k++) U += u_sh[k * D + x];
+    p.out[(((int64_t)b * p.Hkv + kv) * p.G + g) * D + x] = (uint16_t)dense_pack<T>(L == 0.f ? 0.f : U / L, 0.f);
+  }
+}
+
 // SETS: of 16 columns of several tokens; 0: one token a sequence, its heads.
 template <class T, int D, int NW, bool ONCE, int SETS>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode_f8(DenseDecodeParams p) {
@@ -306,7 +370,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     p.parts += (size_t)tile * p.splits * p.Hkv * (16 * C) * (D + 2); // (a tile's chunks are among themselves)
     idx = at.chunk;
   } else {
-    if (!dense_place(p, idx, lane, at)) return;
+    if (!dense_place(p, idx, lane, at)) {
+      if constexpr (NW == 8) if (p.joins) f8_join<T, D>(p, at.chunk, at.rows, kv, lane, wave, o_sh);
+      return;
+    }
     if (at.chunk == 0 && kv == 0 && threadIdx.x == 0 && p.pages.seq_lens[at.b] > p.max_len) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
     col.n = p.G;
   }
@@ -506,7 +573,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
     __syncthreads();
     p.G = G;
-    dense_finish<T, D, NW>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) {
+    dense_finish<T, D, NW, SETS == 0 && NW == 8 ? kF8Whole : 0>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) {
       if constexpr (TOKENS) {
         const int pair = col.row0 + 16 * x + e / D, token = pair / p.group;
         return p.out + (int64_t)(col.q_start + token) * p.out_ld + (kv * p.group + pair - token * p.group) * D + e % D;
@@ -539,8 +606,9 @@ hipError_t launch_decode_form(const DenseDecodeParams& p, int64_t workgroups, hi
   return hipGetLastError();
 }
 template <class T, int D, bool ONCE>
-hipError_t launch_decode_waves(const DenseDecodeParams& p, hipStream_t s) {
-  const int64_t n = dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0);
+hipError_t launch_decode_waves(DenseDecodeParams p, hipStream_t s) {
+  p.joins = p.alone ? 0 : dense_f8_joins(p.B, p.target, p.waves);
+  const int64_t n = dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0) + (int64_t)p.joins * p.G * p.Hkv;
   return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE, 0>(p, n, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE, 0>(p, n, s)
                                                                           : launch_decode_form<T, D, 2, ONCE, 0>(p, n, s);
 }

@@ -52,6 +52,7 @@ WSVD_DEV bool dense_place(const DenseDecodeParams& p, int idx, int lane, DensePl
     }
     first = __builtin_amdgcn_readlane(end, 63);
   }
+  at.chunk = idx - first; at.rows = units;           // behind the last chunk, and the units of one
   return false;
 }
 
@@ -73,6 +74,13 @@ WSVD_DEV float quarters_sum(float x) {
 // ticket: 2.9.)
 WSVD_DEV unsigned long long* dense_part(const DenseDecodeParams& p, int chunk, int kv, int d) {
   return p.parts + ((size_t)chunk * p.Hkv + kv) * p.G * (d + 2);
+}
+// Of a sequence whose chunks others join (dense_finish): the rows of all its n chunks, and behind them a head's maxima and its sums, chunk by
+// chunk, so that lanes read them side by side (with all in a chunk's words, as above, 64 chunks of 8 heads of 64: 10.9 us in place of 10.4).
+struct DensePartWords { unsigned long long *row, *max; };            // max: and n further on the sum
+WSVD_DEV DensePartWords dense_many(const DenseDecodeParams& p, int c0, int n, int chunk, int kv, int g, int d) {
+  unsigned long long* const first = p.parts + (size_t)c0 * p.Hkv * p.G * (d + 2);
+  return {first + (((size_t)chunk * p.Hkv + kv) * p.G + g) * d, first + (size_t)n * p.Hkv * p.G * d + (size_t)(kv * p.G + g) * 2 * n + chunk};
 }
 WSVD_DEV void dense_push(unsigned long long* to, float v) { __hip_atomic_store(to, split_word(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
@@ -159,8 +167,9 @@ WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n,
 }
 
 // The waves' results in LDS ([NW][G][D], a head's dims 4 of its number further on in their row) joined, and with those of the other chunks
-// of the sequence; the last chunk's workgroup writes the output: to(e) is where output e = head * D + dim goes.
-template <class T, int D, int NW, class To>
+// of the sequence; the last chunk's workgroup writes the output: to(e) is where output e = head * D + dim goes.  WHOLE, where p.joins
+// is set too: the chunks of sequences of more than so many are all handed over, for others to join.
+template <class T, int D, int NW, int WHOLE = 0, class To>
 WSVD_DEV void dense_finish(const DenseDecodeParams& p, const DensePlace& at, int idx, int kv, float* o_sh, const float (*m_sh)[16], const float (*l_sh)[16], To to) {
   const int G = p.G;
   DensePartial<D, NW> r;
@@ -179,23 +188,28 @@ WSVD_DEV void dense_finish(const DenseDecodeParams& p, const DensePlace& at, int
       }
     }
   }
+  const bool apart = WHOLE && p.joins > 0 && at.n_chunks > WHOLE;
   if (at.n_chunks > 1) {
     const int c0 = idx - at.chunk, group = at.chunk / kDenseFold, n_groups = (at.n_chunks + kDenseFold - 1) / kDenseFold;
     const bool last = at.chunk == at.n_chunks - 1, ends = last || at.chunk % kDenseFold == kDenseFold - 1;
     __syncthreads();
-    const int folds = !ends ? 0 : last && n_groups > 1 ? 2 : 1;
+    const int folds = !ends || apart ? 0 : last && n_groups > 1 ? 2 : 1;
 #pragma unroll 1
     for (int i = 0; i < folds; i++)                  // the group's chunks, then the groups' results
       dense_fold<D, NW>(p, i == 0 ? c0 + group * kDenseFold : c0 + kDenseFold - 1, i == 0 ? 1 : kDenseFold,
                     i == 0 ? at.chunk % kDenseFold : n_groups - 1, kv, r, o_sh);
-    if (!last) {
+    if (!last || apart) {
+      const DensePartWords at_part = apart ? dense_many(p, c0, at.n_chunks, at.chunk, kv, 0, D) : DensePartWords{};
       unsigned long long* const part = dense_part(p, idx, kv, D);
 #pragma unroll
       for (int i = 0; i < DensePartial<D, NW>::N; i++) {
         const int e = threadIdx.x + i * 64 * NW, g = e / D, x = e % D;
         if (e < G * D) {
-          dense_push(part + g * (D + 2) + 2 + x, r.U[i]);
-          if (x == 0) { dense_push(part + g * (D + 2), r.M[i]); dense_push(part + g * (D + 2) + 1, r.L[i]); }
+          dense_push(apart ? at_part.row + e : part + g * (D + 2) + 2 + x, r.U[i]);
+          if (x == 0) {
+            dense_push(apart ? at_part.max + 2 * g * at.n_chunks : part + g * (D + 2), r.M[i]);
+            dense_push(apart ? at_part.max + (2 * g + 1) * at.n_chunks : part + g * (D + 2) + 1, r.L[i]);
+          }
         }
       }
       return;

@@ -127,6 +127,14 @@ WSVD_HD PagesLaunch pages_launch(int batch, int64_t items) {
   return {(unsigned)(n < 1 ? 1 : n > 128 ? 128 : n), kPagesThreads};
 }
 WSVD_HD int64_t dense_decode_workgroups(int B, int Hkv, int target, bool alone) { return (alone ? (int64_t)B : (int64_t)target + B) * Hkv; }
+// Over 8-bit pages sequences of more than kF8Whole chunks have workgroups of their own to join them, one a head, behind all others: in place of two
+// folds by the last chunk's, one join of all (us with the folds and so; bf16, heads of 128 unless told: 1 x 65001 rows, 16 / 2 heads of 64: 13.4 and 10.4,
+// of 128: 20.1 and 14.7; 1 x 100000, 16 / 1: 27.7 and 17.1; 1 x 16000, 32 / 8: 16.5 and 14.0; 1 x 2000, 28 / 4, of 8 chunks: 10.3 and 8.6; 4 x up to 9000,
+// 28 / 4: 18.2 and 14.2).  They take a CU each for 1.7 us also where nothing is to be joined, so only where the sequences can have 8 chunks on the average
+// (23 ragged sequences of up to 3001 rows, 8 kv heads, with them 22.9 and without 20.1; at the limit 16 x 4000, 16 / 2 heads of 64: 11.4 without and
+// 11.8, 16 x up to 8000 of 128: 19.1 and 18.4).  How many sequences have them: all or none.
+constexpr int kF8Whole = 4;
+WSVD_HD int dense_f8_joins(int B, int target, int waves) { return waves == 8 && target > 8 && target >= 8 * (int64_t)B ? B : 0; }
 // The prompt attention's, at most: every sequence ends inside a tile.  Two tiles a workgroup where there are many and they differ: the second
 // one's first keys and queries are asked for under the first one's last products, so that every other tile starts without a wait (16 x 2048
 // tokens, 32 heads of 128: 650 -> 632 us, 64 x 300, 32 / 8 heads: 129 -> 121, 4 x 4096 of 16 / 2 heads of 64: 166 -> 158; over 13 causal

@@ -184,6 +184,14 @@ int main() {
     }
     if (n > 0) CHECK(dense_f8_append(n, batch, 12, true).units >= units);
   }
+  // workgroups that join chunks: of every sequence of a wave's lanes, or none
+  for (int Hkv = 1; Hkv <= 1024; Hkv++)
+    for (int batch : {1, 2, 3, 4, 7, 8, 16, 31, 32, 33, 64, 65, 65536})
+      for (int most : {100, 1024, 1025, 100000}) {
+        const int waves = dense_waves(batch, Hkv, most), joins = dense_f8_joins(batch, dense_target(waves, Hkv), waves);
+        CHECK(joins == 0 || (joins == batch && batch <= 32 && waves == 8));
+        CHECK(dense_launchable(dense_decode_workgroups(batch, Hkv, dense_target(waves, Hkv), false) + (int64_t)joins * 16 * Hkv, 512) || joins == 0);
+      }
   for (int batch : {1, 64, 65, 256, 257, 65536})
     for (int64_t n : {0, 1, 256, 257, 1024, 1025, 1 << 20, 1 << 24}) {
       const PagesLaunch l = pages_launch(batch, n);

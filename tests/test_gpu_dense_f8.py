@@ -266,6 +266,51 @@ def test_decode_chunks_of_many_tiles(d, dtype):
     decode_case([9001, 20000, 8192 + 8192], 2, 1, d, dtype, 16, min_chunk=32768)
 
 
+LONG = [([9000, 0, 4000, 17], 8, 2, 64, "f16"), ([3000, 2900], 28, 4, 128, "bf16"), ([2500], 16, 1, 128, "f16"), ([5000, 1, 700, 6001, 6000, 0, 3, 2048], 7, 1, 64, "bf16"),
+        ([33000], 13, 1, 128, "bf16"), ([1700] * 16, 10, 2, 64, "f16"), ([4100], 16, 16, 128, "bf16"), ([2, 40000], 8, 8, 64, "f16")]
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d,dtype", LONG)
+def test_decode_sequences_of_many_chunks(lens, hq, hkv, d, dtype):
+    # joined by workgroups of their own, next to sequences that are not
+    decode_case(lens, hq, hkv, d, dtype, 64, ld_extra=16)
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d,dtype", [LONG[0], LONG[1]])
+def test_decode_sequences_of_many_chunks_values_that_are_none(lens, hq, hkv, d, dtype):
+    g = gen(8)
+    L, pool = Layer(len(lens), hq, hkv, d, dtype), F8Pool(g, lens, hkv, d, 64, dtype).random(g)
+    last = 2 if len(lens) > 2 else 1
+    pool.set("v", 0, lens[0] - 1, hkv - 1, 5, 0x7F), pool.set("v", 0, 3, 0, d - 1, 0xFF), pool.set("k", last, 1500, 0, 7, 0x7F)
+    q, out = randn(g, dtype, len(lens), hq * d), torch.empty(len(lens), hq, d, dtype=DTYPES[dtype], device="cuda")
+    W.wsvd_dense_decode_attn_paged_f8(L.ctx, L.desc, q.cuda(), hq * d, L.cache(pool), max(lens), out)
+    want = torch.zeros(len(lens), hq, d, dtype=torch.bool)
+    want[0, hq - hq // hkv:, 5] = True
+    want[0, : hq // hkv, d - 1] = want[last, : hq // hkv] = True
+    assert torch.equal(out.cpu().isnan(), want)
+    L.close()
+
+
+def test_decode_of_many_chunks_leaves_the_workspace_as_it_was():
+    """Calls of other forms over one workspace, again and again: every call's bits stay what they were, also with the sequences in another order."""
+    g, lens, hq, hkv, d = gen(77), [9000, 64, 4000, 0], 8, 2, 128
+    pool, L = F8Pool(g, lens, hkv, d, 16, "bf16").random(g), Layer(4, hq, hkv, d, "bf16")
+    q, qc, outs = randn(g, "bf16", 4, hq * d), randn(g, "bf16", 40, hq * d), []
+    for order in ([0, 1, 2, 3], [2, 0, 3, 1], [0, 1, 2, 3]):
+        cache = L.cache(pool, [lens[i] for i in order])
+        L.table.copy_(pool.table[order])
+        out, few, chunk = (torch.empty(n, hq * d, dtype=torch.bfloat16, device="cuda") for n in (4, 3, 40))
+        W.wsvd_dense_decode_attn_paged_f8(L.ctx, L.desc, q[order].contiguous().cuda(), hq * d, cache, 9000, out)
+        W.wsvd_dense_prefill_attn_paged_f8(L.ctx, L.desc, qc.cuda(), hq * d, 3, prefix([2, 1, 0, 0]).cuda(), cache, few, hq * d)
+        W.wsvd_dense_prefill_attn_paged_f8(L.ctx, L.desc, qc.cuda(), hq * d, 40, prefix([39, 1, 0, 0]).cuda(), cache, chunk, hq * d)
+        again = torch.empty_like(out)
+        W.wsvd_dense_decode_attn_paged_f8(L.ctx, L.desc, q[order].contiguous().cuda(), hq * d, cache, 9000, again)
+        assert torch.equal(out, again)
+        outs.append((out.cpu()[[order.index(i) for i in range(4)]], few.cpu(), chunk.cpu()))
+    assert torch.equal(outs[0][0], outs[1][0]) and all(torch.equal(a, b) for a, b in zip(outs[0], outs[2]))
+    L.close()
+
+
 def test_decode_of_nothing():
     L, pool = Layer(3, 4, 2, 64, "bf16"), F8Pool(gen(2), [0, 0, 0], 2, 64, 16, "bf16")
     out = torch.full((3, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
