@@ -111,8 +111,7 @@ struct DenseDecodeParams {
   // several tokens a sequence (8-bit pages): packed queries and outputs, heads of a kv head, workgroups that share a tile of 16 (token, head) pairs
   const int* cu_q;
   int64_t out_ld;
-  int n_q, group, splits;
-  int joins;                    // sequences that have workgroups to join their chunks (8-bit pages)
+  int n_q, group, splits, tiles;
 };
 struct DensePromptParams {
   const uint16_t *q, *k, *v;    // k, v: packed rows (not paged)

@@ -196,8 +196,9 @@ static wsvd_status chunk(wsvd_ctx* ctx, const wsvd_dense_desc* desc, const void*
     p.B = desc->batch; p.Hkv = desc->n_kv_heads; p.group = group;
     p.splits = columns.splits;
     set_units(ctx, desc, true, p);
-    // (16 columns' parts cost more to join than a group's heads: 8 x 4 tokens behind 1000 rows, 32 / 8 heads, in two chunks 14.1 us, in four 16.2)
-    if (!ctx->opt.min_chunk) p.min_units *= 3;
+    // (16 columns' parts cost the last chunk's workgroup more to join than a group's heads: 8 x 4 tokens behind 1000 rows, 32 / 8 heads, in two chunks
+    // 14.1 us, in four 16.2)
+    if (!ctx->opt.min_chunk && !columns.joins) p.min_units *= 3;
     WSVD_TRY(check_workspace(ctx, desc));
     p.parts = (unsigned long long*)((int*)ctx->ws + kWsCounterInts);
     p.c_scale = scale_of(desc); p.err_word = ctx->err_word; p.scales = scales_of(cache);

@@ -250,12 +250,13 @@ struct F8Tile {
 
 // Several tokens a sequence (where dense_f8_columns says so): the columns are 16 of a sequence's (token, head) pairs, token-major, or two sets of 16 that
 // share the rows' codes and their conversion (which costs as much as one set's products).  A column sees the rows up to its own.
-struct F8Columns { int q_start, row0, n, first_limit; };             // the sequence's first query, pairs before, columns; the last row that the first one sees
-// A workgroup's sequence, columns (of WIDTH) and chunk: tile number idx of the call, share `split` of its rows.
+// The sequence's first query, pairs before, columns; the last row that the first one sees; the tile's number, and of one column that in the tile.
+struct F8Columns { int q_start, row0, n, first_limit, tile, column; };
+// A workgroup's sequence, columns (of WIDTH) and chunk: tile number idx of the call, share `split` of its rows; or (one) the tile of pair number idx.
 template <int WIDTH>
-WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lane, DensePlace& at, F8Columns& col) {
+WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lane, DensePlace& at, F8Columns& col, bool one = false) {
   const int most = p.pages.max_pages * p.pages.page_rows;
-  for (int base = 0, before = 0; base < p.B; base += 64) {
+  for (int base = 0, before = 0, tiles_before = 0; base < p.B; base += 64) {
     const int i = base + lane;
     int qs = 0, n = 0, len = 0;
     if (i < p.B) {
@@ -263,9 +264,10 @@ WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lan
       n = min(max(p.cu_q[i + 1], qs), p.n_q) - qs;
       len = p.pages.seq_lens[i];
     }
-    const int tiles = (n * p.group + WIDTH - 1) / WIDTH, end = before + wave_prefix_int(tiles);
+    const int tiles = (n * p.group + WIDTH - 1) / WIDTH, tiles_end = tiles_before + wave_prefix_int(tiles);
+    const int mine = one ? n * p.group : tiles, end = one ? before + wave_prefix_int(mine) : tiles_end;
     const unsigned long long m = __ballot(end > idx);
-    before = __builtin_amdgcn_readlane(end, 63);
+    before = __builtin_amdgcn_readlane(end, 63); tiles_before = __builtin_amdgcn_readlane(tiles_end, 63);
     if (!m) continue;
     const int l = __builtin_ctzll(m);
     at.b = base + l;
@@ -273,7 +275,10 @@ WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lan
     if (len > most && threadIdx.x == 0) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
     len = min(max(len, 0), most);
     col.q_start = __builtin_amdgcn_readlane(qs, l);
-    col.row0 = WIDTH * (idx - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(tiles, l)));
+    const int number = idx - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(mine, l)), tile = one ? number / WIDTH : number;
+    col.column = number - tile * WIDTH;
+    col.tile = __builtin_amdgcn_readlane(tiles_end, l) - __builtin_amdgcn_readlane(tiles, l) + tile;
+    col.row0 = WIDTH * tile;
     col.n = min(WIDTH, n * p.group - col.row0);
     col.first_limit = len - n + col.row0 / p.group;
     at.len = max(len - n + (col.row0 + col.n - 1) / p.group + 1, 0);
@@ -286,17 +291,11 @@ WSVD_DEV bool f8_columns(const DenseDecodeParams& p, int idx, int split, int lan
   return false;
 }
 
-// The join of a sequence of many chunks, a workgroup a head: dims in lanes, an eighth of the chunks a wave, all words of a thread asked for at once.
-// The workgroup has a higher number than those it waits for, and the wait is bounded.  Words are cleared where they are read.
+// The join of many chunks, a workgroup a head or pair (g of p.G): dims in lanes, an eighth of the n chunks from c0 on a wave, all words of a thread asked
+// for at once.  The workgroup has a higher number than those it waits for, and the wait is bounded.  Words are cleared where they are read.
 template <class T, int D>
-WSVD_DEV void f8_join(const DenseDecodeParams& p, int idx, int units, int kv, int lane, int wave, float* sh) {
+WSVD_DEV void f8_join(const DenseDecodeParams& p, int c0, int n, int kv, int g, int lane, int wave, float* sh, uint16_t* out) {
   constexpr int ND = D / 64, CHUNKS = kDenseFold * kDenseFold / 8;   // a wave's chunks
-  const int n_mine = lane < p.B ? dense_chunks(dense_units_of(dense_length(p, lane)), units) : 0;
-  const unsigned long long many = __ballot(n_mine > kF8Whole);
-  const int which = idx / p.G, g = idx - which * p.G;
-  const unsigned long long sel = __ballot((many >> lane & 1) && __builtin_popcountll(many & ((1ull << lane) - 1)) == which);
-  if (!sel) return;
-  const int b = __builtin_ctzll(sel), n = __builtin_amdgcn_readlane(n_mine, b), c0 = __builtin_amdgcn_readlane(wave_prefix_int(n_mine), b) - n;
   const DensePartWords part = dense_many(p, c0, n, 0, kv, g, D);
   const size_t stride = (size_t)p.Hkv * p.G * D;
   const unsigned long long none = split_word(0.f);
@@ -346,12 +345,25 @@ WSVD_DEV void f8_join(const DenseDecodeParams& p, int idx, int units, int kv, in
     float U = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; k++) U += u_sh[k * D + x];
-    p.out[(((int64_t)b * p.Hkv + kv) * p.G + g) * D + x] = (uint16_t)dense_pack<T>(L == 0.f ? 0.f : U / L, 0.f);
+    out[x] = (uint16_t)dense_pack<T>(L == 0.f ? 0.f : U / L, 0.f);
   }
 }
 
-// SETS: of 16 columns of several tokens; 0: one token a sequence, its heads.
-template <class T, int D, int NW, bool ONCE, int SETS>
+// The sequence and head of joining workgroup idx, where chunks have `units`.
+template <class T, int D>
+WSVD_DEV void f8_join_sequence(const DenseDecodeParams& p, int idx, int units, int kv, int lane, int wave, float* sh) {
+  const int n_mine = lane < p.B ? dense_chunks(dense_units_of(dense_length(p, lane)), units) : 0;
+  const unsigned long long many = __ballot(n_mine > kF8Whole);
+  const int which = idx / p.G, g = idx - which * p.G;
+  const unsigned long long sel = __ballot((many >> lane & 1) && __builtin_popcountll(many & ((1ull << lane) - 1)) == which);
+  if (!sel) return;
+  const int b = __builtin_ctzll(sel), n = __builtin_amdgcn_readlane(n_mine, b), c0 = __builtin_amdgcn_readlane(wave_prefix_int(n_mine), b) - n;
+  f8_join<T, D>(p, c0, n, kv, g, lane, wave, sh, p.out + (((int64_t)b * p.Hkv + kv) * p.G + g) * D);
+}
+
+// SETS: of 16 columns of several tokens; 0: one token a sequence, its heads.  JOINS: with workgroups that join chunks (a form of its own: 1 x 7 tokens
+// behind 3000 rows without them as part of the same form 15.9 us in place of 14.2).
+template <class T, int D, int NW, bool ONCE, int SETS, bool JOINS>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_decode_f8(DenseDecodeParams p) {
   constexpr int ND = D / 64, NK = D / 32, NJ = D / 16, NB = kF8Tile, ROWS = 16 * NB, AHEAD = 64 / NB;        // rows of a tile; tiles looked up at a time
   extern __shared__ __attribute__((aligned(256))) float o_sh[];      // [NW][G][D]
@@ -365,13 +377,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   DensePlace at;
   F8Columns col = {};
   if constexpr (TOKENS) {
-    const int tile = idx / p.splits;
-    if (!f8_columns<16 * C>(p, tile, idx - tile * p.splits, lane, at, col)) return;
-    p.parts += (size_t)tile * p.splits * p.Hkv * (16 * C) * (D + 2); // (a tile's chunks are among themselves)
+    const int tile = idx / p.splits, pair = idx - p.tiles * p.splits;
+    const bool joins = JOINS && pair >= 0;
+    if (!f8_columns<16 * C>(p, joins ? pair : tile, joins ? 0 : idx - tile * p.splits, lane, at, col, joins)) return;
+    p.parts += (size_t)col.tile * p.splits * p.Hkv * (16 * C) * (D + 2);       // (a tile's chunks are among themselves)
+    if (joins) {
+      if (at.n_chunks <= kF8Whole) return;
+      const int set = col.column / 16, row = col.row0 + col.column, token = row / p.group;
+      p.parts += (size_t)set * p.splits * p.Hkv * 16 * (D + 2);
+      p.G = min(col.n - 16 * set, 16);
+      f8_join<T, D>(p, 0, at.n_chunks, kv, col.column - 16 * set, lane, wave, o_sh,
+                    p.out + (int64_t)(col.q_start + token) * p.out_ld + (kv * p.group + row - token * p.group) * D);
+      return;
+    }
     idx = at.chunk;
   } else {
     if (!dense_place(p, idx, lane, at)) {
-      if constexpr (NW == 8) if (p.joins) f8_join<T, D>(p, at.chunk, at.rows, kv, lane, wave, o_sh);
+      if constexpr (JOINS) f8_join_sequence<T, D>(p, at.chunk, at.rows, kv, lane, wave, o_sh);
       return;
     }
     if (at.chunk == 0 && kv == 0 && threadIdx.x == 0 && p.pages.seq_lens[at.b] > p.max_len) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
@@ -573,7 +595,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
     __syncthreads();
     p.G = G;
-    dense_finish<T, D, NW, SETS == 0 && NW == 8 ? kF8Whole : 0>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) {
+    dense_finish<T, D, NW, JOINS ? kF8Whole : 0>(p, at, idx, kv, o_sh, m_sh, l_sh, [&](int e) {
       if constexpr (TOKENS) {
         const int pair = col.row0 + 16 * x + e / D, token = pair / p.group;
         return p.out + (int64_t)(col.q_start + token) * p.out_ld + (kv * p.group + pair - token * p.group) * D + e % D;
@@ -594,30 +616,32 @@ hipError_t launch_append(const DenseAppendParams& p, hipStream_t s) {
   else k_dense_append_f8<T, D, false><<<grid, 256, 0, s>>>(p, a.splits);
   return hipGetLastError();
 }
-template <class T, int D, int NW, bool ONCE, int SETS>
+template <class T, int D, int NW, bool ONCE, int SETS, bool JOINS>
 hipError_t launch_decode_form(const DenseDecodeParams& p, int64_t workgroups, hipStream_t s) {
   constexpr int LDS = NW * D * 4 * 16;
   static LdsLimit limit;
   if (LDS + NW * 16 * 8 > 65536) {
-    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode_f8<T, D, NW, ONCE, SETS>, LDS);
+    const hipError_t e = wsvd_raise_lds(limit, (const void*)k_dense_decode_f8<T, D, NW, ONCE, SETS, JOINS>, LDS);
     if (e != hipSuccess) return e;
   }
-  k_dense_decode_f8<T, D, NW, ONCE, SETS><<<(unsigned)workgroups, 64 * NW, LDS, s>>>(p);
+  k_dense_decode_f8<T, D, NW, ONCE, SETS, JOINS><<<(unsigned)workgroups, 64 * NW, LDS, s>>>(p);
   return hipGetLastError();
 }
 template <class T, int D, bool ONCE>
-hipError_t launch_decode_waves(DenseDecodeParams p, hipStream_t s) {
-  p.joins = p.alone ? 0 : dense_f8_joins(p.B, p.target, p.waves);
-  const int64_t n = dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0) + (int64_t)p.joins * p.G * p.Hkv;
-  return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE, 0>(p, n, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE, 0>(p, n, s)
-                                                                          : launch_decode_form<T, D, 2, ONCE, 0>(p, n, s);
+hipError_t launch_decode_waves(const DenseDecodeParams& p, hipStream_t s) {
+  const int64_t n = dense_decode_workgroups(p.B, p.Hkv, p.target, p.alone != 0), joins = p.alone ? 0 : dense_f8_joins(p.B, p.target, p.waves);
+  if (joins) return launch_decode_form<T, D, 8, ONCE, 0, true>(p, n + joins * p.G * p.Hkv, s);
+  return p.waves == 8 ? launch_decode_form<T, D, 8, ONCE, 0, false>(p, n, s) : p.waves == 4 ? launch_decode_form<T, D, 4, ONCE, 0, false>(p, n, s)
+                                                                                 : launch_decode_form<T, D, 2, ONCE, 0, false>(p, n, s);
 }
 template <class T, int D>
-hipError_t launch_decode(const DenseDecodeParams& p, hipStream_t s) {
+hipError_t launch_decode(DenseDecodeParams p, hipStream_t s) {
   if (p.cu_q) {
     const DenseF8Columns c = dense_f8_columns(p.n_q, p.B, p.Hkv, p.group);
+    p.tiles = (int)c.tiles;
     const int64_t n = c.tiles * p.splits * p.Hkv;
-    return c.sets == 2 ? launch_decode_form<T, D, 8, false, 2>(p, n, s) : launch_decode_form<T, D, 8, false, 1>(p, n, s);
+    if (c.joins) return launch_decode_form<T, D, 8, false, 1, true>(p, n + (int64_t)p.n_q * p.group * p.Hkv, s);
+    return c.sets == 2 ? launch_decode_form<T, D, 8, false, 2, false>(p, n, s) : launch_decode_form<T, D, 8, false, 1, false>(p, n, s);
   }
   const bool once = (int64_t)p.B * p.max_len * p.Hkv * D * 2 >= 100000000;      // (as k_dense_decode's)
   return once ? launch_decode_waves<T, D, true>(p, s) : launch_decode_waves<T, D, false>(p, s);

@@ -167,8 +167,8 @@ WSVD_DEV void dense_fold(const DenseDecodeParams& p, int chunk, int step, int n,
 }
 
 // The waves' results in LDS ([NW][G][D], a head's dims 4 of its number further on in their row) joined, and with those of the other chunks
-// of the sequence; the last chunk's workgroup writes the output: to(e) is where output e = head * D + dim goes.  WHOLE, where p.joins
-// is set too: the chunks of sequences of more than so many are all handed over, for others to join.
+// of the sequence; the last chunk's workgroup writes the output: to(e) is where output e = head * D + dim goes.  WHOLE, where not
+// 0: the chunks of sequences of more than so many are all handed over, for others to join.
 template <class T, int D, int NW, int WHOLE = 0, class To>
 WSVD_DEV void dense_finish(const DenseDecodeParams& p, const DensePlace& at, int idx, int kv, float* o_sh, const float (*m_sh)[16], const float (*l_sh)[16], To to) {
   const int G = p.G;
@@ -188,7 +188,7 @@ WSVD_DEV void dense_finish(const DenseDecodeParams& p, const DensePlace& at, int
       }
     }
   }
-  const bool apart = WHOLE && p.joins > 0 && at.n_chunks > WHOLE;
+  const bool apart = WHOLE && at.n_chunks > WHOLE;
   if (at.n_chunks > 1) {
     const int c0 = idx - at.chunk, group = at.chunk / kDenseFold, n_groups = (at.n_chunks + kDenseFold - 1) / kDenseFold;
     const bool last = at.chunk == at.n_chunks - 1, ends = last || at.chunk % kDenseFold == kDenseFold - 1;

@@ -110,12 +110,18 @@ WSVD_HD DenseF8Append dense_f8_append(int64_t n_tokens, int batch, int heads, bo
 // behind 1000, 28 / 4 heads: 19 and 22; past the CUs 64 x 8 behind 1000: 33 and 50).
 //   tiles: at most, since every sequence with tokens ends inside one.  splits: workgroups that may share a tile's rows, as many as give every CU one, and
 // no more than one fold takes (1 x 7 behind 3000: up to 4 14.2, 8 15.4, 16 18.3; 1 x 4 behind 8000, 28 / 4 heads: 19.0, 18.0, 19.7).
-struct DenseF8Columns { bool taken; int sets; int64_t tiles; int splits; };
+//   joins: more may share it, and chunks of more than kF8Whole are joined by workgroups of their own, one a pair (1 x 4 behind 8000, 28 / 4 heads: 17.8 and
+// 11.8; 1 x 8 behind 65000, 16 / 2 heads of 64: 30.0 and 14.9; 1 x 5 behind 16000, 16 heads: 19.7 and 18.2), as far as half of the CUs hold those, which they
+// take also where there is nothing to join (1 x 2 behind 640, 32 heads: 8.2 without and 8.4; past that 16 x 2 behind 200, 16 / 2 heads of 64: 5.9 and 9.1).
+constexpr int kF8Whole = 4;
+struct DenseF8Columns { bool taken; int sets; int64_t tiles; int splits; bool joins; };
 WSVD_HD DenseF8Columns dense_f8_columns(int64_t n_q, int batch, int Hkv, int group) {
   const int64_t some = batch < n_q ? batch : n_q, pairs = (n_q * group + some - 1) / some;
   const int sets = (pairs + 15) / 16 * some * Hkv <= kDenseCus ? 1 : 2, width = 16 * sets;
   const int64_t even = (pairs + width - 1) / width * some * Hkv, n = even <= kDenseCus ? kDenseCus / even : 1;
-  return {pairs <= 64 && even <= kDenseCus, sets, n_q * group / width + some, (int)(n > kDenseFold ? kDenseFold : n)};
+  const bool joins = sets == 1 && n > kF8Whole && n_q * group * Hkv <= kDenseCus / 2;
+  const int most = joins ? kDenseFold * kDenseFold : kDenseFold;
+  return {pairs <= 64 && even <= kDenseCus, sets, n_q * group / width + some, (int)(n > most ? most : n), joins};
 }
 // The page tables' calls: a thread a sequence at a time, and `items` (tokens or table entries) dealt out.
 constexpr int kPagesThreads = 1024;
@@ -133,7 +139,6 @@ WSVD_HD int64_t dense_decode_workgroups(int B, int Hkv, int target, bool alone) 
 // 28 / 4: 18.2 and 14.2).  They take a CU each for 1.7 us also where nothing is to be joined, so only where the sequences can have 8 chunks on the average
 // (23 ragged sequences of up to 3001 rows, 8 kv heads, with them 22.9 and without 20.1; at the limit 16 x 4000, 16 / 2 heads of 64: 11.4 without and
 // 11.8, 16 x up to 8000 of 128: 19.1 and 18.4).  How many sequences have them: all or none.
-constexpr int kF8Whole = 4;
 WSVD_HD int dense_f8_joins(int B, int target, int waves) { return waves == 8 && target > 8 && target >= 8 * (int64_t)B ? B : 0; }
 // The prompt attention's, at most: every sequence ends inside a tile.  Two tiles a workgroup where there are many and they differ: the second
 // one's first keys and queries are asked for under the first one's last products, so that every other tile starts without a wait (16 x 2048

@@ -166,7 +166,8 @@ int main() {
     }
     if (n == 0) continue;
     const DenseF8Columns c = dense_f8_columns(n, batch, Hkv, group);
-    CHECK((c.sets == 1 || c.sets == 2) && c.tiles >= tiles[c.sets] && c.splits >= 1 && c.splits <= kDenseFold);
+    CHECK((c.sets == 1 || c.sets == 2) && c.tiles >= tiles[c.sets] && c.splits >= 1 && c.splits <= (c.joins ? kDenseFold * kDenseFold : kDenseFold));
+    CHECK(!c.joins || (c.sets == 1 && n * group * Hkv <= 128));
     if (c.taken) CHECK(dense_launchable(c.tiles * c.splits * Hkv, 512) && (c.splits == 1 || c.tiles * c.splits * Hkv * c.sets * 16 * 8 <= (int64_t)kDensePromptParts * kDensePromptRows * 4));
   }
   CHECK(dense_f8_columns(1, 65536, 1024, 1).tiles == 1 && !dense_f8_columns(1 << 24, 1, 1, 16).taken && dense_f8_columns(20, 4, 8, 1).taken);

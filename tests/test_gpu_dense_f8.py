@@ -472,6 +472,22 @@ def test_chunk_of_a_few_tokens_values_that_are_none(lens, new, hq, hkv, d, dtype
                                                        ("v", 0, n - 4, hkv - 1, 33, 0x7F), ("v", 0, 2, hkv - 1, 40, 0x7F)])
 
 
+JOINED = [([8000], [4], 28, 4, 128, "bf16"), ([9000, 30, 5000, 0], [8, 1, 3, 0], 8, 2, 64, "f16"), ([16000], [5], 16, 16, 64, "bf16"), ([7000, 3], [3, 3], 16, 1, 128, "f16"),
+          ([3001, 3000], [9, 7], 7, 1, 64, "f16"), ([20000], [1], 8, 8, 128, "bf16")]
+
+
+@pytest.mark.parametrize("lens,new,hq,hkv,d,dtype", JOINED)
+def test_chunk_of_a_few_tokens_behind_many_rows(lens, new, hq, hkv, d, dtype):
+    # the chunks of a tile joined by workgroups of their own, a pair each
+    chunk_case(lens, new, hq, hkv, d, dtype, 64, spare=1, ld_extra=16)
+
+
+@pytest.mark.parametrize("lens,new,hq,hkv,d,dtype", [JOINED[0], JOINED[1], JOINED[4]])
+def test_chunk_of_a_few_tokens_behind_many_rows_values_that_are_none(lens, new, hq, hkv, d, dtype):
+    n, m = lens[0], new[0]
+    chunk_case(lens, new, hq, hkv, d, dtype, 64, none=[("v", 0, n - 1, 0, 3, 0x7F), ("v", 0, n - 2, 0, d - 1, 0xFF), ("v", 0, n - m, 0, 17, 0xFF), ("v", 0, n // 2, hkv - 1, 33, 0x7F)])
+
+
 MANY = [(40, 8, 16, 4, 64, "bf16"), (40, 7, 16, 4, 128, "f16"), (20, 16, 16, 8, 128, "bf16"), (150, 5, 7, 1, 64, "f16"), (10, 30, 15, 15, 64, "bf16"), (17, 3, 112, 8, 128, "f16")]
 
 
