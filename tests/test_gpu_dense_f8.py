@@ -311,6 +311,39 @@ def test_decode_of_many_chunks_leaves_the_workspace_as_it_was():
     L.close()
 
 
+def test_joined_calls_in_graphs_that_share_a_workspace():
+    """Two graphs of long sequences' decode and few tokens over one workspace, replayed in turn with eager calls between, lengths changing."""
+    g, hq, hkv, d = gen(91), 8, 2, 64
+    pool, L = F8Pool(g, [9000, 4000], hkv, d, 64, "f16").random(g), Layer(2, hq, hkv, d, "f16")
+    cache, q, cu = L.cache(pool), randn(g, "f16", 6, hq * d).cuda(), prefix([4, 2]).cuda()
+
+    def calls(out, few, stream=None):
+        W.wsvd_dense_decode_attn_paged_f8(L.ctx, L.desc, q, hq * d, cache, 9000, out, stream)
+        W.wsvd_dense_prefill_attn_paged_f8(L.ctx, L.desc, q, hq * d, 6, cu, cache, few, hq * d, stream)
+
+    new = lambda: (torch.zeros(2, hq * d, dtype=torch.float16, device="cuda"), torch.zeros(6, hq * d, dtype=torch.float16, device="cuda"))
+    want = new()
+    calls(*want)
+    graphs = []
+    for _ in range(2):
+        outs, graph = new(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls(*outs, torch.cuda.current_stream())
+        graphs.append((graph, outs))
+    for lens in ([9000, 4000], [9000, 4000], [8999, 30], [2000, 0], [9000, 4000]):
+        L.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        eager = new()
+        calls(*eager)
+        for graph, outs in graphs:
+            for x in outs:
+                x.fill_(3)
+            graph.replay()
+            assert all(torch.equal(a, b) for a, b in zip(outs, eager)), lens
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(eager, want))
+    L.close()
+
+
 def test_decode_of_nothing():
     L, pool = Layer(3, 4, 2, 64, "bf16"), F8Pool(gen(2), [0, 0, 0], 2, 64, 16, "bf16")
     out = torch.full((3, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
