@@ -606,7 +606,7 @@ wsvd_status wsvd_dense_prefill_attn_paged_f8(wsvd_ctx *ctx, const wsvd_dense_des
 /*
  * Page tables kept on the GPU: the free pages are a list on the device, pages of finished sequences go back to it and new tokens take
  * from it, so that a serving step (and a graph of it) needs no table from the host.  For any of the paged caches above (several layers
- * share one table).  Both calls read seq_lens and n_free and write seq_lens_out and n_free_out, which may be the same memory; they
+ * share one table).  The calls read seq_lens and n_free and write seq_lens_out and n_free_out, which may be the same memory; they
  * need no workspace.
  */
 typedef struct {
@@ -639,6 +639,16 @@ wsvd_status wsvd_pages_grow(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int
  */
 wsvd_status wsvd_pages_release(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int32_t *done, const int32_t *seq_lens,
                                const int32_t *n_free, int32_t *seq_lens_out, int32_t *n_free_out, void *hip_stream);
+
+/*
+ * The same for rows that are taken back (draft tokens that are not accepted): of every sequence the first kept_lens[b] rows stay, all of
+ * them where it has no more; the pages that only later rows reach go to the end of the free list, and its length becomes
+ * min(kept_lens[b], seq_lens[b]).  A negative number of rows records WSVD_E_SHAPE and is taken as 0.  A length that is lowered in any
+ * other way has to stay in its last page: the pages behind that would be in no list, and the next wsvd_pages_grow would put others in
+ * their entries.  In 8-bit pages rows that were taken back leave their block the scale that it had with them.
+ */
+wsvd_status wsvd_pages_keep(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int32_t *kept_lens, const int32_t *seq_lens,
+                            const int32_t *n_free, int32_t *seq_lens_out, int32_t *n_free_out, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -32,7 +32,7 @@ EXPORTS = ["wsvd_create", "wsvd_destroy", "wsvd_cache_bytes", "wsvd_workspace_by
            "wsvd_prefill_attn", "wsvd_shared_workspace_bytes", "wsvd_decode_attn_shared", "wsvd_timeline_set_buffer",
            "wsvd_dense_workspace_bytes", "wsvd_dense_append_paged", "wsvd_dense_decode_attn_paged", "wsvd_dense_prefill_attn",
            "wsvd_dense_prefill_attn_paged", "wsvd_dense_f8_cache_bytes", "wsvd_dense_append_paged_f8", "wsvd_dense_decode_attn_paged_f8",
-           "wsvd_dense_prefill_attn_paged_f8", "wsvd_pages_grow", "wsvd_pages_release"]
+           "wsvd_dense_prefill_attn_paged_f8", "wsvd_pages_grow", "wsvd_pages_release", "wsvd_pages_keep"]
 
 
 class WsvdError(RuntimeError):
@@ -167,7 +167,7 @@ def lib():
         for name in ("append_paged", "decode_attn_paged", "prefill_attn_paged"):
             getattr(L, f"wsvd_dense_{name}_f8").argtypes = getattr(L, f"wsvd_dense_{name}").argtypes
         L.wsvd_pages_grow.argtypes = [c_void_p, POINTER(PagePool), c_void_p, c_int64] + [c_void_p] * 8
-        L.wsvd_pages_release.argtypes = [c_void_p, POINTER(PagePool)] + [c_void_p] * 6
+        L.wsvd_pages_release.argtypes = L.wsvd_pages_keep.argtypes = [c_void_p, POINTER(PagePool)] + [c_void_p] * 6
         for name in EXPORTS:
             if name not in ("wsvd_status_str",):
                 getattr(L, name).restype = c_int
@@ -570,3 +570,13 @@ def wsvd_pages_release(ctx, pool, done, seq_lens, n_free, seq_lens_out, n_free_o
         status = call(*_addresses(ctx, pool, done, seq_lens, n_free, seq_lens_out, n_free_out, on))
     if status:
         raise WsvdError(status, "wsvd_pages_release")
+
+
+def wsvd_pages_keep(ctx, pool, kept_lens, seq_lens, n_free, seq_lens_out, n_free_out, stream=None):
+    call, on = (_lib or lib()).wsvd_pages_keep, stream if stream.__class__ is int else _stream_addr(stream)
+    try:
+        status = call(ctx, pool, kept_lens.data_ptr(), seq_lens.data_ptr(), n_free.data_ptr(), seq_lens_out.data_ptr(), n_free_out.data_ptr(), on)
+    except AttributeError:
+        status = call(*_addresses(ctx, pool, kept_lens, seq_lens, n_free, seq_lens_out, n_free_out, on))
+    if status:
+        raise WsvdError(status, "wsvd_pages_keep")

@@ -1,5 +1,5 @@
-// Page tables kept on the GPU: the pages of finished sequences back to a free list, and pages from it for the new tokens of a step, with the
-// tokens' prefix sums, positions and slots.  Latency is what counts: a step's tables are a few KB to a MB.
+// Page tables kept on the GPU: the pages of finished sequences, and of rows that are taken back, to a free list, and pages from it for the new
+// tokens of a step, with the tokens' prefix sums, positions and slots.  Latency is what counts: a step's tables are a few KB to a MB.
 #include "wsvd_dense.h"
 
 namespace {
@@ -8,13 +8,14 @@ constexpr int kSeqs = kPagesThreads;                 // sequences at a time, at 
 
 struct PagesParams {
   int *table, *free_pages;
-  const int *lens, *n_free, *what;                   // what: new tokens, or which sequences are done
+  const int *lens, *n_free, *what;                   // what: new tokens, which sequences are done, or the rows they keep
   int *lens_out, *n_free_out;
   int *cu, *positions, *slots;
   int B, R, max_pages, n_pages, n_tokens;
   int* err_word;
   int* counter;                                      // of workgroups, zero between launches
   int apart;                                         // what is written is not what is read
+  int keeps;                                         // `what` is rows that are kept
 };
 
 // Exclusive prefix sum of one number a thread over the workgroup, and the sum of all.  Numbers are at most 2^24, and no more than that many
@@ -130,25 +131,34 @@ __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
   }
 }
 
-// Pages of the sequences that are done, in the order of sequences and rows, behind the free list's last.  An entry's place is its number
-// among those of the done sequences, as long as all are pages; that some are not (a free list that ended left -1) is rare, and then the last
+// The table entries of sequence b whose pages go: first, and how many.  Of a sequence that is done all, of one that keeps rows those that only
+// later rows reach.
+struct Gone { int first, n; };
+WSVD_DEV Gone pages_gone(const PagesParams& p, int b) {
+  if (b >= p.B) return {0, 0};
+  const int len = min(max(p.lens[b], 0), p.max_pages * p.R), what = p.what[b];
+  const int kept = !p.keeps ? (what != 0 ? 0 : len) : min(max(what, 0), len), first = (kept + p.R - 1) / p.R;
+  return {first, (len + p.R - 1) / p.R - first};
+}
+// Pages that go, in the order of sequences and rows, behind the free list's last.  An entry's place is its number
+// among those that go, as long as all are pages; that some are not (a free list that ended left -1) is rare, and then the last
 // workgroup to come does it all once more, leaving those out.  (1024 sequences, 99 of them done with 26661 pages: 32 us as one workgroup that
 // counts the pages first.)
-WSVD_DEV void pages_left_out(const PagesParams& p, int n_free, int& end, int* first_sh, int* count_sh, Scan& scan) {
+WSVD_DEV void pages_left_out(const PagesParams& p, int n_free, int& end, int* first_sh, int* from_sh, int* count_sh, Scan& scan) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   end = n_free;
   for (int base = 0; base < p.B; base += (int)blockDim.x) {
-    const int b = base + tid, n_here = min(p.B - base, (int)blockDim.x);
-    const int len = b < p.B ? min(max(p.lens[b], 0), p.max_pages * p.R) : 0;
+    const int n_here = min(p.B - base, (int)blockDim.x);
+    const Gone gone = pages_gone(p, base + tid);
     __syncthreads();
-    count_sh[tid] = b < p.B && p.what[b] != 0 ? (len + p.R - 1) / p.R : 0;
+    from_sh[tid] = gone.first; count_sh[tid] = gone.n;
     __syncthreads();
     // a wave a sequence: its pages counted, and written once it is known where they begin
     auto each = [&](int s, auto put) {
-      const int n = __builtin_amdgcn_readfirstlane(count_sh[s]);
+      const int n = __builtin_amdgcn_readfirstlane(count_sh[s]), from = __builtin_amdgcn_readfirstlane(from_sh[s]);
       int before = 0;
       for (int i0 = 0; i0 < n; i0 += 64) {
-        const int i = i0 + lane, page = i < n ? p.table[(size_t)(base + s) * p.max_pages + i] : -1;
+        const int i = i0 + lane, page = i < n ? p.table[(size_t)(base + s) * p.max_pages + from + i] : -1;
         const bool valid = page >= 0 && page < p.n_pages;
         const unsigned long long m = __ballot(valid);
         if (valid) put(before + __builtin_popcountll(m & ((1ull << lane) - 1)), page);
@@ -174,22 +184,22 @@ WSVD_DEV void pages_left_out(const PagesParams& p, int n_free, int& end, int* fi
 }
 __global__ __launch_bounds__(kSeqs) void k_pages_release(PagesParams p) {
   __shared__ Scan scan;
-  __shared__ int first_sh[kSeqs], count_sh[kSeqs];
+  __shared__ int first_sh[kSeqs], from_sh[kSeqs], count_sh[kSeqs];
   __shared__ int last_sh, none_sh;
   const int tid = threadIdx.x, wg = blockIdx.x, wgs = gridDim.x;
   const int n_free = min(max(*p.n_free, 0), p.n_pages);
   int end = n_free, none = 0;
   if (tid == 0) none_sh = 0;
   for (int base = 0; base < p.B; base += (int)blockDim.x) {
-    const int b = base + tid, n_here = min(p.B - base, (int)blockDim.x);
-    const int len = b < p.B ? min(max(p.lens[b], 0), p.max_pages * p.R) : 0;
+    const int n_here = min(p.B - base, (int)blockDim.x);
+    const Gone gone = pages_gone(p, base + tid);
     int total;
-    const int first = end + scan_exclusive(scan, b < p.B && p.what[b] != 0 ? (len + p.R - 1) / p.R : 0, total);
-    first_sh[tid] = first;
+    const int first = end + scan_exclusive(scan, gone.n, total);
+    first_sh[tid] = first; from_sh[tid] = gone.first;
     __syncthreads();
     for (int i = end + wg * (int)blockDim.x + tid; i < min(end + total, p.n_pages); i += wgs * (int)blockDim.x) {
       const int s = last_at_most(first_sh, n_here, i);
-      const int page = p.table[(size_t)(base + s) * p.max_pages + i - first_sh[s]];
+      const int page = p.table[(size_t)(base + s) * p.max_pages + from_sh[s] + i - first_sh[s]];
       if (page < 0 || page >= p.n_pages) none = 1; else put_page(p.free_pages + i, page);
     }
     end = min(end + total, p.n_pages + 1);           // (that many, or too many)
@@ -214,10 +224,15 @@ __global__ __launch_bounds__(kSeqs) void k_pages_release(PagesParams p) {
   __syncthreads();
   if (none_sh) {
     wait_vmem_done();
-    pages_left_out(p, n_free, end, first_sh, count_sh, scan);
+    pages_left_out(p, n_free, end, first_sh, from_sh, count_sh, scan);
   }
-  if (end > p.n_pages) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
-  for (int b = tid; b < p.B; b += (int)blockDim.x) p.lens_out[b] = p.what[b] != 0 ? 0 : p.lens[b];
+  bool err = end > p.n_pages;
+  for (int b = tid; b < p.B; b += (int)blockDim.x) {
+    const int len = p.lens[b], what = p.what[b];
+    err = err || (p.keeps && what < 0);
+    p.lens_out[b] = p.keeps ? min(max(what, 0), len) : what != 0 ? 0 : len;
+  }
+  if (err) atomicExch(p.err_word, (int)WSVD_E_SHAPE);
   if (tid == 0) *p.n_free_out = min(end, p.n_pages);
 }
 
@@ -260,18 +275,26 @@ wsvd_status wsvd_pages_grow(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int
   return hipGetLastError() == hipSuccess ? WSVD_OK : WSVD_E_HIP;
 }
 
-wsvd_status wsvd_pages_release(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int32_t* done, const int32_t* seq_lens, const int32_t* n_free,
-                               int32_t* seq_lens_out, int32_t* n_free_out, void* hip_stream) {
-  if (!ctx || !done || !seq_lens || !n_free || !seq_lens_out || !n_free_out) return WSVD_E_NULL;
+static wsvd_status give_back(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int32_t* what, bool keeps, const int32_t* seq_lens, const int32_t* n_free,
+                             int32_t* seq_lens_out, int32_t* n_free_out, void* hip_stream) {
+  if (!ctx || !what || !seq_lens || !n_free || !seq_lens_out || !n_free_out) return WSVD_E_NULL;
   const wsvd_status st = check_pool(pool);
   if (st != WSVD_OK) return st;
-  for (const void* x : {(const void*)done, (const void*)seq_lens, (const void*)n_free, (const void*)seq_lens_out, (const void*)n_free_out})
+  for (const void* x : {(const void*)what, (const void*)seq_lens, (const void*)n_free, (const void*)seq_lens_out, (const void*)n_free_out})
     if (!aligned4(x)) return WSVD_E_ALIGN;
   PagesParams p = params_of(ctx, pool);
-  p.lens = seq_lens; p.n_free = n_free; p.what = done; p.lens_out = seq_lens_out; p.n_free_out = n_free_out;
+  p.lens = seq_lens; p.n_free = n_free; p.what = what; p.keeps = keeps; p.lens_out = seq_lens_out; p.n_free_out = n_free_out;
   const PagesLaunch l = pages_launch(pool->batch, (int64_t)pool->batch * pool->max_pages / 16);
   k_pages_release<<<l.workgroups, l.threads, 0, (hipStream_t)hip_stream>>>(p);
   return hipGetLastError() == hipSuccess ? WSVD_OK : WSVD_E_HIP;
+}
+wsvd_status wsvd_pages_release(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int32_t* done, const int32_t* seq_lens, const int32_t* n_free,
+                               int32_t* seq_lens_out, int32_t* n_free_out, void* hip_stream) {
+  return give_back(ctx, pool, done, false, seq_lens, n_free, seq_lens_out, n_free_out, hip_stream);
+}
+wsvd_status wsvd_pages_keep(wsvd_ctx* ctx, const wsvd_page_pool* pool, const int32_t* kept_lens, const int32_t* seq_lens, const int32_t* n_free,
+                            int32_t* seq_lens_out, int32_t* n_free_out, void* hip_stream) {
+  return give_back(ctx, pool, kept_lens, true, seq_lens, n_free, seq_lens_out, n_free_out, hip_stream);
 }
 
 }  // extern "C"
