@@ -625,8 +625,8 @@ typedef struct {
  * n_tokens, at most 2^24, is what positions and slots have room for; entries behind the last token are left as they are.
  * Where the free list ends, the entries that it cannot serve are -1, as are their tokens' slots, and WSVD_E_CAPACITY is recorded in the
  * status word (wsvd_check): appends store nothing there and report it.  Rows above max_pages * page_rows have no page: -1 and
- * WSVD_E_CAPACITY likewise.  More tokens than n_tokens, negative numbers, lengths above max_pages * page_rows and entries that are no
- * page record WSVD_E_SHAPE (numbers are taken as the nearest that is allowed).
+ * WSVD_E_CAPACITY likewise.  More tokens than n_tokens, negative numbers, lengths above max_pages * page_rows, a free list of more than
+ * n_pages pages and entries that are no page record WSVD_E_SHAPE (numbers are taken as the nearest that is allowed).
  */
 wsvd_status wsvd_pages_grow(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int32_t *new_lens, int64_t n_tokens,
                             const int32_t *seq_lens, const int32_t *n_free, int32_t *seq_lens_out, int32_t *n_free_out,
@@ -635,7 +635,7 @@ wsvd_status wsvd_pages_grow(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int
 /*
  * The pages of every sequence with done[b] != 0 go to the end of the free list, in the order of sequences and rows, and its length
  * becomes 0; table entries outside [0, n_pages) are left out.  The entries themselves stay as they are.  A list that would hold more
- * than n_pages pages (one given back twice) ends there, and WSVD_E_SHAPE is recorded.
+ * than n_pages pages (one given back twice) ends there, and WSVD_E_SHAPE is recorded, as for an *n_free that is none.
  */
 wsvd_status wsvd_pages_release(wsvd_ctx *ctx, const wsvd_page_pool *pool, const int32_t *done, const int32_t *seq_lens,
                                const int32_t *n_free, int32_t *seq_lens_out, int32_t *n_free_out, void *hip_stream);

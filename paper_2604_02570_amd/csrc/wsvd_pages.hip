@@ -51,8 +51,8 @@ __global__ __launch_bounds__(kSeqs) void k_pages_grow(PagesParams p) {
   __shared__ int last_sh;
   const int tid = threadIdx.x, wg = blockIdx.x, wgs = gridDim.x;
   const int R = p.R, cap = p.max_pages * R;
-  const int n_free = min(max(*p.n_free, 0), p.n_pages);
-  int err = 0;
+  const int listed = *p.n_free, n_free = min(max(listed, 0), p.n_pages);
+  int err = listed != n_free ? (int)WSVD_E_SHAPE : 0;
   auto free_page = [&](int i) {
     if (i >= n_free) { err = err ? err : (int)WSVD_E_CAPACITY; return -1; }
     const int page = p.free_pages[n_free - 1 - i];
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kSeqs) void k_pages_release(PagesParams p) {
   __shared__ int first_sh[kSeqs], from_sh[kSeqs], count_sh[kSeqs];
   __shared__ int last_sh, none_sh;
   const int tid = threadIdx.x, wg = blockIdx.x, wgs = gridDim.x;
-  const int n_free = min(max(*p.n_free, 0), p.n_pages);
+  const int listed = *p.n_free, n_free = min(max(listed, 0), p.n_pages);
   int end = n_free, none = 0;
   if (tid == 0) none_sh = 0;
   for (int base = 0; base < p.B; base += (int)blockDim.x) {
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kSeqs) void k_pages_release(PagesParams p) {
     wait_vmem_done();
     pages_left_out(p, n_free, end, first_sh, from_sh, count_sh, scan);
   }
-  bool err = end > p.n_pages;
+  bool err = end > p.n_pages || listed != n_free;
   for (int b = tid; b < p.B; b += (int)blockDim.x) {
     const int len = p.lens[b], what = p.what[b];
     err = err || (p.keeps && what < 0);
