@@ -608,6 +608,12 @@ wsvd_status wsvd_dense_prefill_attn_paged_f8(wsvd_ctx *ctx, const wsvd_dense_des
  * from it, so that a serving step (and a graph of it) needs no table from the host.  For any of the paged caches above (several layers
  * share one table).  The calls read seq_lens and n_free and write seq_lens_out and n_free_out, which may be the same memory; they
  * need no workspace.
+ *   Lengths   The dense layers' calls take lengths that count a step's tokens: seq_lens_out, which may be the caches' own, grown in place.
+ *           wsvd_latent_append_paged and wsvd_prefill_append_paged advance their cache's lengths themselves, from those BEFORE the step:
+ *           where a latent layer shares the table, its lengths are seq_lens and seq_lens_out is other memory.  (Grown in place they
+ *           would count every token twice, and its rows would lie behind a gap.)  Each latent layer has lengths of its own.
+ *   Owners  A page is one sequence's: nobody counts how many have it.  Where sequences share a prefix's pages, all but one of them
+ *           are to be released over a table whose entries of these pages are -1 (they are left out), or it is listed twice.
  */
 typedef struct {
   int32_t *block_table;      /* DEVICE [batch][max_pages] */
