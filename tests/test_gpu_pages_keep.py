@@ -151,16 +151,18 @@ def test_drafts_through_append_and_attention(hq, hkv, d, dtype):
     L.close()
 
 
-def test_in_a_graph():
-    """A step of drafts captured on another stream and replayed with eager work between: every replay as the rules have it."""
-    B, R, P = 12, 16, 40
+@pytest.mark.parametrize("B,P", [(12, 40), (300, 60)])
+def test_in_a_graph(B, P):
+    """A step of drafts captured on another stream and replayed with eager work between, as one workgroup and as several: every replay as the rules
+    have it."""
+    R = 16
     D = Device(B, R, P, B * P, B * P)
     new, kept = (torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(2))
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         on = torch.cuda.current_stream()
-        W.wsvd_pages_grow(D.ctx, D.pool, new, 300, D.lens, D.n_free, D.lens, D.n_free, stream=on)
+        W.wsvd_pages_grow(D.ctx, D.pool, new, 20 * B, D.lens, D.n_free, D.lens, D.n_free, stream=on)
         W.wsvd_pages_keep(D.ctx, D.pool, kept, D.lens, D.n_free, D.lens, D.n_free, on)
     rng = random.Random(3)
     for step in range(8):
