@@ -577,6 +577,9 @@ wsvd_status wsvd_dense_prefill_attn_paged(wsvd_ctx *ctx, const wsvd_dense_desc *
  *             values  (x / 64) * 1024 + (r / 4) * 256 + (x % 64) * 4 + r % 4
  *           A caller that fills pools itself keeps to scale bytes 27 .. 247 and to values that the type holds.  All else about the
  *           cache, its lengths, table and errors, is as for the 16-bit calls; k_meta / v_meta may not be NULL.
+ *           No result depends on bytes that no row was written to, but the time of the attention of packed tokens does: NaN codes among a last
+ *           block's values make tiles run a second time (3 x 333 tokens behind 1501 rows, 32 / 8 heads of 128: 48 us, and 154).  A pool
+ *           that is cleared once, when it is allocated, has none there but those of values that were none.
  */
 
 /* Bytes of ONE code pool and ONE scale pool (K or V) of n_pages pages (HOST outputs). */
@@ -596,7 +599,10 @@ wsvd_status wsvd_dense_append_paged_f8(wsvd_ctx *ctx, const wsvd_dense_desc *des
                                        void *k_out, int64_t k_out_ld, wsvd_paged_cache *cache, void *hip_stream);
 
 /* wsvd_dense_decode_attn_paged and wsvd_dense_prefill_attn_paged over such pages: keys and values are code * scale, exact as numbers of
- * dtype; precision, workspace and everything else as there.  A value that is none makes none of every output that sees its row. */
+ * dtype; workspace and everything else as there.  A value that is none makes none of every output that sees its row.  Precision: the weights
+ * are pairs in the decode attention.  In that of packed tokens they are rounded once, as a prompt's, or pairs where the tokens are so few that
+ * they run as columns of the decode attention (chosen by n_q, also where fewer tokens are there, batch and heads: up to 64 (token,
+ * head) pairs of a kv head a sequence, spread evenly, and 256 tiles of 16 or 32 of them). */
 wsvd_status wsvd_dense_decode_attn_paged_f8(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld,
                                             const wsvd_paged_cache *cache, int32_t max_seq_len, void *out, void *hip_stream);
 wsvd_status wsvd_dense_prefill_attn_paged_f8(wsvd_ctx *ctx, const wsvd_dense_desc *desc, const void *q, int64_t q_ld, int64_t n_q,
@@ -627,7 +633,8 @@ typedef struct {
  *   seq_lens_out[b] = seq_lens[b] + new_lens[b]; table entries of the pages that these rows reach and the earlier ones did not are
  *   taken from the end of the free list, sequence by sequence and page by page; n_free_out = what is left.
  *   cu_tokens [batch + 1]: prefix sums of new_lens, the packed tokens' borders.  positions [n_tokens]: a token's row in its sequence.
- *   slots [n_tokens]: page * page_rows + row in the page.  Each of the three may be NULL.
+ *   slots [n_tokens]: page * page_rows + row in the page, for a caller's own kernels (the calls above take the table itself).  Each of the
+ *   three may be NULL.
  * n_tokens, at most 2^24, is what positions and slots have room for; entries behind the last token are left as they are.
  * Where the free list ends, the entries that it cannot serve are -1, as are their tokens' slots, and WSVD_E_CAPACITY is recorded in the
  * status word (wsvd_check): appends store nothing there and report it.  Rows above max_pages * page_rows have no page: -1 and

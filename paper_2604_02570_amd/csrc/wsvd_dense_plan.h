@@ -35,6 +35,7 @@ WSVD_HD uint64_t dense_pool_row(int page, int granule, int pg, int kv, int Hkv, 
 // rows, 2 of 4 or 4 of 2, so that units begin side by side (44 sequences of one row, 32 heads: 23.5 -> 11.0 us, 64 ragged of up to
 // 500 rows, 8 heads: 20.6 -> 17.4; 32 x 2000 rows of 32 heads with workgroups of 2 waves: 166 -> 172).
 constexpr int kDenseWavesPerCu = 8, kDenseCus = 256, kDenseUnit = 128;
+// (16-bit rows; over 8-bit ones, of half the bytes, the same numbers are taken, and set_units' least chunk.)
 WSVD_HD int dense_waves(int B, int Hkv, int max_len) {
   const int64_t units = (int64_t)B * Hkv;
   return max_len > 1024 || units < 2 * kDenseCus ? 8 : units < 4 * kDenseCus ? 4 : 2;
@@ -59,6 +60,8 @@ constexpr int kDenseFold = 8;
 // four 9.5, 8.1, 9.0); else at least min_units, and for up to 64 sequences the least at which there
 // are at most `target` chunks (a chunk too many is a second round of workgroups: 23 ragged sequences of up to 3001 rows, 8 kv
 // heads: 43.8 -> 36.5 us).  count(units): the chunks of all sequences.
+// A long sequence among B - 1 short ones has target - B + 1 chunks then, few where B is near `target` (one of 60000 rows, the others of 500, 32 / 8 heads of
+// 128, target 32, 8-bit rows: B 24 48 us, 31 149, 32 281, 33 32).
 template <class Count>
 WSVD_HD int dense_units(int total, int most, int B, int target, int alone_units, int min_units, Count count) {
   if (most <= alone_units) return alone_units;
@@ -100,16 +103,19 @@ WSVD_HD DenseF8Append dense_f8_append(int64_t n_tokens, int batch, int heads, bo
 }
 // Attention of a few tokens a sequence over 8-bit pages: tiles of 16 (token, head) pairs, the columns of the decode attention, where the prompt
 // attention's of 128 would be mostly empty.  Taken where the call's tokens, spread evenly, make at most 64 pairs a sequence, and no more tiles in all than
-// the chip has CUs: a tile reads its rows for itself, at 70 GB/s a CU, and a workgroup of 8 waves costs about 5 us (us as tiles of 128 and of 16; 32 / 8
+// the chip has CUs (a call whose tokens lie otherwise has up to twice as many): a tile reads its rows for itself, at 70 GB/s a CU, and a workgroup of 8 waves costs about 5 us (us as tiles of 128 and of 16; 32 / 8
 // heads of 128 unless told: 4 x 5 tokens behind 700 rows, 8 heads of 64: 12.3 and 6.6; 1 x 7 behind 3000: 18 and 14; 8 x 4 behind 1000: 20 and 14; 32 x 3
 // behind 2000: 44 and 30; 20 x 5 behind 1500, 28 / 4 heads: 27 and 17; 2 x 64 behind 3000, 8 heads: 21 and 16; past the limits 32 x 8 behind 2000: 44 and 41;
-// 8 x 20 behind 3000: 31 and 37; 64 x 8 behind 300: 16 and 37; 1 x 64 behind 30000: 57 and 112).
+// 8 x 20 behind 3000: 31 and 37; 64 x 8 behind 300: 16 and 37; 1 x 64 behind 30000: 57 and 112).  Pieces of prompts beside single tokens, behind 1000 rows each:
+// 256 + 63 x 1, 12 / 1 heads: 26 and 13; 512 + 63 x 1, 7 / 1: 26 and 20; 128 + 7 x 1, 8 / 8 of 64: 14 and 8; 100 + 31 x 1: 32 and 25; the piece behind 8000: 44
+// and 38, 45 and 38, 25 and 19, 144 and 58; 200 tokens of one of 32 slots, 16 / 2 heads of 64, behind 8000: 30 and 26.
 //   sets: of 16 pairs that a tile holds: two where tiles of one would be too many and those of two are not (a tile of two takes 1.6 times as long; us as
 // tiles of 128 and of two sets: 32 x 8 behind 2000: 44 and 37; 32 x 6 behind 2000, 32 / 8 heads of 64: 29 and 18; 64 x 5 behind 1000, 16 / 2 heads of 64: 19
 // and 14; 32 x 5 behind 200: 11.6 and 13.0; two sets where one is few enough, 1 x 7 behind 3000: 22; past 64 pairs 1 x 32 behind 2000: 17 and 23; 8 x 16
 // behind 1000, 28 / 4 heads: 19 and 22; past the CUs 64 x 8 behind 1000: 33 and 50).
 //   tiles: at most, since every sequence with tokens ends inside one.  splits: workgroups that may share a tile's rows, as many as give every CU one, and
-// no more than one fold takes (1 x 7 behind 3000: up to 4 14.2, 8 15.4, 16 18.3; 1 x 4 behind 8000, 28 / 4 heads: 19.0, 18.0, 19.7).
+// no more than one fold takes (1 x 7 behind 3000: up to 4 14.2, 8 15.4, 16 18.3; 1 x 4 behind 8000, 28 / 4 heads: 19.0, 18.0, 19.7).  From the host's numbers
+// alone: one long sequence among many has a share like theirs (32 x 2 behind 500: 12; one of them behind 8000: 37, behind 60000: 282, as tiles of 128 1012).
 //   joins: more may share it, and chunks of more than kF8Whole are joined by workgroups of their own, one a pair (1 x 4 behind 8000, 28 / 4 heads: 17.8 and
 // 11.8; 1 x 8 behind 65000, 16 / 2 heads of 64: 30.0 and 14.9; 1 x 5 behind 16000, 16 heads: 19.7 and 18.2), as far as half of the CUs hold those, which they
 // take also where there is nothing to join (1 x 2 behind 640, 32 heads: 8.2 without and 8.4; past that 16 x 2 behind 200, 16 / 2 heads of 64: 5.9 and 9.1).

@@ -43,8 +43,8 @@ constexpr int kKeys = 64;                            // keys of a staged block
 // Blocks that a workgroup of several for one tile has at least: the join is a second launch of 4 to 5 us, a block takes 1 to 1.5.
 constexpr int kLeastBlocks = 6;
 // Over 8-bit pages more workgroups share a tile that several share at all: a block takes about as long, but the codes of a workgroup's first
-// blocks are there sooner (7 tokens behind 3000 rows, 32 / 8 heads: 19.1 us with 6 blocks at least, 17.9 with 4, 17.8 with 3, 19.4 with 2; 8 x 16 behind
-// 1000, 28 / 4: 21.4, 19.1, 20.1, 21.3; 2 x 200 behind 300, of up to 8 blocks: 17.0 for tiles left whole, 19.8 for those of 8 in two).
+// blocks are there sooner (8 x 16 tokens behind 1000 rows, 28 / 4 heads: 21.4 us with 6 blocks at least, 19.1 with 4, 20.1 with 3, 21.3 with 2; 2 x 200
+// behind 300, of up to 8 blocks: 17.0 for tiles left whole, 19.8 for those of 8 in two).
 constexpr int kLeastBlocksF8 = 4;
 template <bool F8>
 WSVD_HD int prompt_shares(int blocks) { return F8 ? (blocks < 2 * kLeastBlocks ? 1 : blocks / kLeastBlocksF8) : blocks / kLeastBlocks; }
